@@ -334,6 +334,129 @@ hifa4_status hifa4_decode_fwd(const hifa4_problem* p, const hifa4_fwd_options* o
                               void* o, float* lse, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The paged key-value cache of a serving loop: sequences grow a page of 64
+ * tokens at a time, pages come from one pool in any order, and a table names
+ * each sequence's pages.  The paper evaluates prefill only; these entry points
+ * keep what its attention quantizes (K^ with Smooth-QK, V^ in groups of 64
+ * tokens) and attend over it.
+ *
+ *   operands     what a page holds: HIFA4_OPERANDS_HIF4 (4.5 bits a value) or
+ *                HIFA4_OPERANDS_FP16;
+ *   pool         DEVICE, num_pages * hifa4_paged_page_bytes() bytes, 16-byte
+ *                aligned.  A page is one record per kv head, in the order of
+ *                the matrix instructions' registers: it is written by
+ *                hifa4_paged_append and read by the other entry points;
+ *   block_table  DEVICE int32 [batch, max_pages]: the page of each 64 tokens.
+ *                An entry outside [0, num_pages) names no page: its tokens are
+ *                not stored, attended to or read back.  Sequences may share
+ *                pages for reading; two that append into one page race;
+ *   seq_lens     DEVICE int32 [batch]: the cached tokens of each sequence,
+ *                those that an append brings included; 0 for an unused row
+ *                (values outside [0, 64 max_pages] are cut to that range);
+ *   v_tail       DEVICE fp16 [batch, 64, num_heads_kv, head_dim]: V of the
+ *                tokens in each sequence's last page, kept by
+ *                hifa4_paged_append for HIFA4_OPERANDS_HIF4 (a group of V^ is
+ *                quantized again when a token joins it); may be NULL otherwise
+ *                and for the other entry points.
+ * head_dim is 64, 128 or 256.  Every entry point reads the table and the
+ * lengths on the device, enqueues a fixed number of kernels whose grid follows
+ * from host values alone, and may be captured into a graph and replayed with
+ * other lengths and tables. */
+typedef struct {
+  int32_t batch;
+  int32_t num_heads_kv;
+  int32_t head_dim;
+  int32_t operands;
+  int32_t num_pages;
+  int32_t max_pages;
+  void* pool;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  void* v_tail;
+} hifa4_paged_cache;
+
+/* Bytes of one page: 64 tokens of K and V, every kv head (0 on invalid
+ * arguments). */
+size_t hifa4_paged_page_bytes(int32_t num_heads_kv, int32_t head_dim, int32_t operands);
+
+/* Appends new tokens.  The new tokens of sequence b are the rows
+ * [cu_new[b], cu_new[b+1]) of k and v and the last ones of its seq_lens[b]
+ * tokens; cu_new NULL: one token for each sequence, rows of length 0 skipped.
+ * k, v: DEVICE fp16 [total_new, num_heads_kv, head_dim]; s: DEVICE fp32
+ * [num_heads_kv, head_dim] or NULL.  K~ = fp16(k/s), rounded once; with HIF4
+ * pages K~ and V become the codes of hifa4_quantize_qk and hifa4_quantize_v:
+ * the pages hold at any time the codes of quantizing the whole sequence (the
+ * group of an open page zero padded), whatever pieces it came in.
+ * max_new: a host bound of the tokens that one sequence gets (it sizes the
+ * launch; further tokens are not stored).  An append may begin inside a page
+ * and end in another; earlier tokens of the page must have come through
+ * hifa4_paged_append, with the same v_tail.  Asynchronous. */
+hifa4_status hifa4_paged_append(const hifa4_paged_cache* c, int32_t total_new, int32_t max_new,
+                                const int32_t* cu_new, const void* k, const void* v,
+                                const float* s, void* stream);
+
+/* Reads tokens back: of sequence b the tokens starts[b], starts[b]+1, ... into
+ * the rows [cu_tokens[b], cu_tokens[b+1]) of k and v (DEVICE fp16
+ * [total_tokens, num_heads_kv, head_dim]), K^ as it is cached (Smooth-QK not
+ * undone) and V^, HIF4 values rounded to fp16 (exact unless they fall below
+ * its normal range).  Tokens at or behind seq_lens[b] are zeros; rows that
+ * cu_tokens does not name are left as they are.  starts: DEVICE int32 [batch]
+ * or NULL (0).  max_tokens: a host bound of the rows per sequence (it sizes
+ * the launch; further rows are not written).  Asynchronous. */
+hifa4_status hifa4_paged_gather(const hifa4_paged_cache* c, int32_t total_tokens, int32_t max_tokens,
+                                const int32_t* cu_tokens, const int32_t* starts, void* k, void* v,
+                                void* stream);
+
+/* Bytes of device workspace hifa4_paged_decode_fwd needs (0 on invalid
+ * arguments); page_weights != 0 where the call accumulates page weights.  It
+ * grows with batch * num_heads_q and, with page weights, with
+ * batch * max_pages * num_heads_q; it does not depend on the lengths. */
+size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q,
+                                          int32_t page_weights);
+
+/* One decode step: the attention of each sequence's newest token over its
+ * cached tokens (its own among them, appended before).
+ * q: DEVICE fp16 [batch, num_heads_q, head_dim], smoothed with s when s is not
+ * NULL (q~ = fp16(q*s)); query head h reads kv head h / (num_heads_q /
+ * num_heads_kv).  With S_j = q~ k_j / sqrt(D) over the cached values:
+ * p = softmax(S), o = sum_j p_j v_j (DEVICE fp16 [batch, num_heads_q,
+ * head_dim]), lse = log sum_j exp(S_j) (DEVICE fp32 [num_heads_q, batch]).
+ * Unlike hifa4_decode_fwd, which repeats a row of the prefill code for code,
+ * only the cache is quantized here: a step's time is the cache's bytes, and
+ * the query, the scores, the softmax state (fp32) and p keep their precision.
+ * Sequences without tokens get o = 0 and lse = -inf.
+ * page_weights (DEVICE fp32 [batch, max_pages], may be NULL): then
+ * weights_out[b][j] = decay * page_weights[b][j] + the sum of p over every
+ * query head and the tokens of page j, for the pages that sequence b uses, and
+ * page_weights[b][j] for the others.  weights_out may be page_weights itself;
+ * both are NULL or neither.
+ * workspace: DEVICE, >= hifa4_paged_decode_workspace_bytes(); nothing in it
+ * has to start at zero and nothing is kept in it.  Sums are taken in a fixed
+ * order: equal inputs give equal bits.  Asynchronous. */
+hifa4_status hifa4_paged_decode_fwd(const hifa4_paged_cache* c, int32_t num_heads_q, const void* q,
+                                    const float* s, void* o, float* lse, const float* page_weights,
+                                    float* weights_out, float decay, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated attention weight: a sequence of more than `budget`
+ * pages keeps its `first` first pages, its `last` last pages and, of those
+ * between, the ones of the largest weight until it has `budget` (equal weights:
+ * the earlier page stays; NaN counts as the smallest).  Whole pages leave, so
+ * that no group of V^ is broken up and nothing in the pool moves; the pages
+ * that stay close ranks in order (cached keys carry their position).
+ * 0 <= first, 1 <= last (the open page stays), first + last <= budget.
+ * block_table, seq_lens, page_weights: as above (read); out_table, out_lens,
+ * out_weights: the same after the eviction (entries behind the pages that stay
+ * are -1 and 0; 64 tokens less for each page evicted); each may be its input's
+ * own buffer, and must not overlap any other.  freed: DEVICE int32
+ * [batch, max_pages], the evicted pages' entries in order, then -1; num_freed:
+ * DEVICE int32 [batch].  Asynchronous. */
+hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* block_table,
+                               const int32_t* seq_lens, const float* page_weights, int32_t budget,
+                               int32_t first, int32_t last, int32_t* out_table, int32_t* out_lens,
+                               float* out_weights, int32_t* freed, int32_t* num_freed, void* stream);
+
 /* Device self-test of the kernels' fp16 exponential: y[i] = fp16(2^x[i]) for
  * n fp16 inputs x (DEVICE, fp16 bits), evaluated by the same device routine
  * the attention kernel uses.  Asynchronous. */

@@ -9,7 +9,9 @@ fallback implementation.
 Names mirror the C entry points:
   hifa4_calibrate_smooth_qk, hifa4_calibrate_smooth_qk_layers, hifa4_quantize_qk, hifa4_quantize_v,
   hifa4_attention_fwd, hifa4_workspace_bytes, hifa4_decode_fwd,
-  hifa4_decode_workspace_bytes, hifa4_selftest_exp2, hifa4_last_error.
+  hifa4_decode_workspace_bytes, hifa4_paged_page_bytes, hifa4_paged_append,
+  hifa4_paged_gather, hifa4_paged_decode_fwd, hifa4_paged_decode_workspace_bytes,
+  hifa4_paged_evict, hifa4_selftest_exp2, hifa4_last_error.
 """
 from __future__ import annotations
 
@@ -30,8 +32,10 @@ STATUS = {0: "HIFA4_OK", -1: "HIFA4_ERR_INVALID_ARGUMENT", -2: "HIFA4_ERR_UNSUPP
 EXPORTED = ("hifa4_workspace_bytes", "hifa4_calibrate_workspace_bytes", "hifa4_calibrate_smooth_qk",
             "hifa4_calibrate_smooth_qk_layers",
             "hifa4_quantize_qk", "hifa4_quantize_v", "hifa4_attention_fwd", "hifa4_decode_workspace_bytes",
-            "hifa4_decode_fwd", "hifa4_selftest_exp2", "hifa4_last_error", "hifa4_attention_fwd_noalloc")
+            "hifa4_decode_fwd", "hifa4_paged_page_bytes", "hifa4_paged_append", "hifa4_paged_gather",
+            "hifa4_paged_decode_workspace_bytes", "hifa4_paged_decode_fwd", "hifa4_paged_evict", "hifa4_selftest_exp2", "hifa4_last_error", "hifa4_attention_fwd_noalloc")
 NOALLOC_SCRATCH_BYTES = 32 << 20
+PAGE_TOKENS = 64
 
 
 class Problem(ctypes.Structure):
@@ -48,6 +52,13 @@ class FwdOptions(ctypes.Structure):
                 ("test_decode_no_publish", ctypes.c_int32),
                 ("debug_head_begin", ctypes.c_int32), ("debug_head_count", ctypes.c_int32),
                 ("debug_token_begin", ctypes.c_int32), ("debug_token_count", ctypes.c_int32)]
+
+
+class PagedCacheDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("operands", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("pool", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("v_tail", ctypes.c_void_p)]
 
 
 class CalibReport(ctypes.Structure):
@@ -95,6 +106,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.hifa4_decode_workspace_bytes.argtypes = [P(Problem)]
     lib.hifa4_decode_fwd.restype = ctypes.c_int
     lib.hifa4_decode_fwd.argtypes = [P(Problem), P(FwdOptions), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    i32 = ctypes.c_int32
+    lib.hifa4_paged_page_bytes.restype = sz
+    lib.hifa4_paged_page_bytes.argtypes = [i32, i32, i32]
+    lib.hifa4_paged_append.restype = ctypes.c_int
+    lib.hifa4_paged_append.argtypes = [P(PagedCacheDesc), i32, i32, vp, vp, vp, vp, vp]
+    lib.hifa4_paged_gather.restype = ctypes.c_int
+    lib.hifa4_paged_gather.argtypes = [P(PagedCacheDesc), i32, i32, vp, vp, vp, vp, vp]
+    lib.hifa4_paged_decode_workspace_bytes.restype = sz
+    lib.hifa4_paged_decode_workspace_bytes.argtypes = [P(PagedCacheDesc), i32, i32]
+    lib.hifa4_paged_decode_fwd.restype = ctypes.c_int
+    lib.hifa4_paged_decode_fwd.argtypes = [P(PagedCacheDesc), i32, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]
+    lib.hifa4_paged_evict.restype = ctypes.c_int
+    lib.hifa4_paged_evict.argtypes = [i32, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.hifa4_selftest_exp2.restype = ctypes.c_int
     lib.hifa4_selftest_exp2.argtypes = [vp, vp, ctypes.c_int64, vp]
     lib.hifa4_last_error.restype = ctypes.c_char_p
@@ -458,6 +482,234 @@ def hifa4_decode_fwd(q, k_codes, k_meta, v_codes, v_meta, s=None, cu_seqlens=Non
     if debug_p:
         return o, l, pc, pm
     return o, l
+
+
+# ---------------------------------------------------------------------------
+# The paged cache.
+def _shaped(t, dtype, shape, device, name):
+    _require(t, dtype, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+
+
+class _OnDevice:
+    """Makes `device` the current one for a call, where it is another."""
+
+    def __init__(self, device):
+        cuda = _torch()._C
+        self.back = cuda._cuda_getDevice()
+        if self.back != device.index:
+            cuda._cuda_setDevice(device.index)
+        else:
+            self.back = -1
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *_):
+        if self.back >= 0:
+            _torch()._C._cuda_setDevice(self.back)
+
+
+def hifa4_paged_page_bytes(heads_kv: int, head_dim: int, operands: int = OPERANDS_HIF4) -> int:
+    """Bytes of a page: 64 tokens of K and V, every kv head."""
+    n = int(load_library().hifa4_paged_page_bytes(heads_kv, head_dim, operands))
+    if not n:
+        raise Hifa4Error(f"hifa4_paged_page_bytes: {hifa4_last_error()}")
+    return n
+
+
+class PagedCache:
+    """The handle of a paged K/V cache: pages of 64 tokens in one pool.
+
+    pool         uint8 [num_pages, heads_kv, bytes] (bytes * heads_kv =
+                 hifa4_paged_page_bytes; the contents are the library's)
+    block_table  int32 [batch, max_pages], the page of each 64 tokens (an entry
+                 that is no page of the pool, such as -1, holds no tokens)
+    seq_lens     int32 [batch], cached tokens; 0 for an unused row
+    v_tail       fp16 [batch, 64, heads_kv, head_dim], V of each sequence's
+                 last page (hifa4_paged_append on HIF4 pages needs it)
+
+    The tensors stay the caller's: tables and lengths are changed in place,
+    also between replays of a captured call.  PagedCache.empty allocates them."""
+
+    def __init__(self, pool, block_table, seq_lens, head_dim: int, operands: int = OPERANDS_HIF4, v_tail=None):
+        torch = _torch()
+        _require(pool, torch.uint8, "pool")
+        if pool.dim() != 3:
+            raise ValueError("pool is [num_pages, heads_kv, bytes]")
+        heads_kv, dev = pool.shape[1], pool.device
+        if hifa4_paged_page_bytes(heads_kv, head_dim, operands) != heads_kv * pool.shape[2]:
+            raise ValueError(f"a page of {heads_kv} heads holds {hifa4_paged_page_bytes(heads_kv, head_dim, operands)} "
+                             f"bytes, the pool has {heads_kv * pool.shape[2]}")
+        if block_table.dim() != 2:
+            raise ValueError("block_table is [batch, max_pages]")
+        batch, max_pages = block_table.shape
+        _shaped(block_table, torch.int32, (batch, max_pages), dev, "block_table")
+        _shaped(seq_lens, torch.int32, (batch,), dev, "seq_lens")
+        if v_tail is not None:
+            _shaped(v_tail, torch.float16, (batch, PAGE_TOKENS, heads_kv, head_dim), dev, "v_tail")
+        self._tensors = (pool, block_table, seq_lens, v_tail)
+        self.device, self.batch, self.heads_kv, self.head_dim = dev, batch, heads_kv, head_dim
+        self.operands, self.max_pages = operands, max_pages
+        self._desc = PagedCacheDesc(batch, heads_kv, head_dim, operands, pool.shape[0], max_pages, _ptr(pool),
+                                    _ptr(block_table), _ptr(seq_lens), _ptr(v_tail))
+        self._ref = ctypes.byref(self._desc)
+        self._workspace_bytes = {}
+
+    pool = property(lambda self: self._tensors[0])
+    block_table = property(lambda self: self._tensors[1])
+    seq_lens = property(lambda self: self._tensors[2])
+    v_tail = property(lambda self: self._tensors[3])
+
+    @classmethod
+    def empty(cls, num_pages: int, batch: int, max_pages: int, heads_kv: int, head_dim: int,
+              operands: int = OPERANDS_HIF4, device="cuda"):
+        """A cache whose rows are all empty (no pages, length 0)."""
+        torch = _torch()
+        record = hifa4_paged_page_bytes(heads_kv, head_dim, operands) // heads_kv
+        pool = torch.empty((num_pages, heads_kv, record), dtype=torch.uint8, device=device)
+        table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
+        lens = torch.zeros(batch, dtype=torch.int32, device=device)
+        tail = None
+        if operands == OPERANDS_HIF4:
+            tail = torch.zeros((batch, PAGE_TOKENS, heads_kv, head_dim), dtype=torch.float16, device=device)
+        return cls(pool, table, lens, head_dim, operands, tail)
+
+
+def hifa4_paged_append(cache: PagedCache, k, v, s=None, cu_new=None, max_new: Optional[int] = None):
+    """Appends new tokens: k, v fp16 [total, heads_kv, head_dim]; without
+    cu_new one token per row of the batch, else sequence b gets the rows
+    [cu_new[b], cu_new[b+1]).  cache.seq_lens counts the new tokens already.
+    s: the Smooth-QK scales (the pages then hold k/s).  max_new: an upper bound
+    of the tokens per sequence (default: all of them)."""
+    torch, dev = _torch(), cache.device
+    total = k.shape[0]
+    _shaped(k, torch.float16, (total, cache.heads_kv, cache.head_dim), dev, "k")
+    _shaped(v, torch.float16, (total, cache.heads_kv, cache.head_dim), dev, "v")
+    if s is not None:
+        _shaped(s, torch.float32, (cache.heads_kv, cache.head_dim), dev, "s")
+    if cu_new is not None:
+        _shaped(cu_new, torch.int32, (cache.batch + 1,), dev, "cu_new")
+    if max_new is None:
+        max_new = total if cu_new is not None else 1
+    with _OnDevice(dev):
+        _check(load_library().hifa4_paged_append(cache._ref, total, max_new, _ptr(cu_new), _ptr(k), _ptr(v), _ptr(s),
+                                                 _stream(dev)), "hifa4_paged_append")
+
+
+def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_tokens: Optional[int] = None, starts=None,
+                       k=None, v=None):
+    """Reads tokens back: of sequence b the tokens from starts[b] (default 0)
+    on into the rows [cu_tokens[b], cu_tokens[b+1]).  Returns (k, v) fp16
+    [total_tokens, heads_kv, head_dim] (allocated unless given), K as it is
+    cached.  max_tokens: an upper bound of the rows per sequence (default: all
+    of them)."""
+    torch, dev = _torch(), cache.device
+    shape = (total_tokens, cache.heads_kv, cache.head_dim)
+    _shaped(cu_tokens, torch.int32, (cache.batch + 1,), dev, "cu_tokens")
+    if starts is not None:
+        _shaped(starts, torch.int32, (cache.batch,), dev, "starts")
+    if k is None:
+        k = torch.empty(shape, dtype=torch.float16, device=dev)
+    else:
+        _shaped(k, torch.float16, shape, dev, "k")
+    if v is None:
+        v = torch.empty(shape, dtype=torch.float16, device=dev)
+    else:
+        _shaped(v, torch.float16, shape, dev, "v")
+    with _OnDevice(dev):
+        _check(load_library().hifa4_paged_gather(cache._ref, total_tokens, total_tokens if max_tokens is None else max_tokens,
+                                                 _ptr(cu_tokens), _ptr(starts), _ptr(k), _ptr(v), _stream(dev)),
+               "hifa4_paged_gather")
+    return k, v
+
+
+def hifa4_paged_decode_workspace_bytes(cache: PagedCache, heads_q: int, page_weights: bool = False) -> int:
+    n = int(load_library().hifa4_paged_decode_workspace_bytes(cache._ref, heads_q, 1 if page_weights else 0))
+    if not n:
+        raise Hifa4Error(f"hifa4_paged_decode_workspace_bytes: {hifa4_last_error()}")
+    return n
+
+
+def hifa4_paged_decode_fwd(cache: PagedCache, q, s=None, page_weights=None, decay: float = 1.0, weights_out=None,
+                           out=None, lse=None, workspace: Optional[Workspace] = None):
+    """One decode step over the pages: q [batch, heads_q, head_dim] fp16, the
+    query of each sequence's newest token.  Returns (o like q, lse fp32
+    [heads_q, batch]); empty rows get 0 and -inf.  page_weights fp32 [batch,
+    max_pages]: becomes decay * page_weights + this step's attention weight of
+    each page (in place, or in weights_out)."""
+    torch, dev = _torch(), cache.device
+    if q.dim() != 3:
+        raise ValueError("q is [batch, heads_q, head_dim]")
+    hq = q.shape[1]
+    _shaped(q, torch.float16, (cache.batch, hq, cache.head_dim), dev, "q")
+    if s is not None:
+        _shaped(s, torch.float32, (cache.heads_kv, cache.head_dim), dev, "s")
+    weighs = page_weights is not None
+    if weighs:
+        _shaped(page_weights, torch.float32, (cache.batch, cache.max_pages), dev, "page_weights")
+        if weights_out is None:
+            weights_out = page_weights
+        else:
+            _shaped(weights_out, torch.float32, (cache.batch, cache.max_pages), dev, "weights_out")
+    elif weights_out is not None:
+        raise ValueError("weights_out needs page_weights")
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _shaped(out, torch.float16, q.shape, dev, "out")
+    if lse is None:
+        lse = torch.empty((hq, cache.batch), dtype=torch.float32, device=dev)
+    else:
+        _shaped(lse, torch.float32, (hq, cache.batch), dev, "lse")
+    need = cache._workspace_bytes.get((hq, weighs))
+    if need is None:
+        need = cache._workspace_bytes[hq, weighs] = hifa4_paged_decode_workspace_bytes(cache, hq, weighs)
+    stream = _stream(dev)
+    with _OnDevice(dev):
+        ws = _scratch(need, dev, stream) if workspace is None else workspace.get(need, dev)
+        _check(load_library().hifa4_paged_decode_fwd(cache._ref, hq, _ptr(q), _ptr(s), _ptr(out), _ptr(lse),
+                                                     _ptr(page_weights), _ptr(weights_out), decay, _ptr(ws), ws.numel(),
+                                                     stream), "hifa4_paged_decode_fwd")
+    return out, lse
+
+
+def hifa4_paged_evict(block_table, seq_lens, page_weights, budget: int, first: int = 0, last: int = 1, out_table=None,
+                      out_lens=None, out_weights=None, freed=None, num_freed=None):
+    """Evicts the pages of the least weight from every sequence that holds more
+    than `budget`; its `first` first and `last` last pages stay.  Works in place
+    unless out_table, out_lens, out_weights are given.  Returns (freed int32
+    [batch, max_pages]: the evicted pages in order, then -1; num_freed int32
+    [batch])."""
+    torch, dev = _torch(), block_table.device
+    if block_table.dim() != 2:
+        raise ValueError("block_table is [batch, max_pages]")
+    shape = tuple(block_table.shape)
+    rows = shape[:1]
+    _shaped(block_table, torch.int32, shape, dev, "block_table")
+    _shaped(seq_lens, torch.int32, rows, dev, "seq_lens")
+    _shaped(page_weights, torch.float32, shape, dev, "page_weights")
+    out = []
+    for t, dtype, size, inplace, name in ((out_table, torch.int32, shape, block_table, "out_table"),
+                                          (out_lens, torch.int32, rows, seq_lens, "out_lens"),
+                                          (out_weights, torch.float32, shape, page_weights, "out_weights"),
+                                          (freed, torch.int32, shape, None, "freed"),
+                                          (num_freed, torch.int32, rows, None, "num_freed")):
+        if t is not None:
+            _shaped(t, dtype, size, dev, name)
+        elif inplace is not None:
+            t = inplace
+        else:
+            t = torch.empty(size, dtype=dtype, device=dev)
+        out.append(t)
+    with _OnDevice(dev):
+        _check(load_library().hifa4_paged_evict(shape[0], shape[1], _ptr(block_table), _ptr(seq_lens), _ptr(page_weights),
+                                                budget, first, last, *[_ptr(t) for t in out], _stream(dev)),
+               "hifa4_paged_evict")
+    return out[3], out[4]
 
 
 def hifa4_selftest_exp2(x):

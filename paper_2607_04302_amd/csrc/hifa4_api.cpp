@@ -15,6 +15,7 @@
 
 #include "hifa4_decode.h"
 #include "hifa4_internal.h"
+#include "hifa4_paged.h"
 
 namespace {
 
@@ -268,6 +269,192 @@ hifa4_status hifa4_decode_fwd(const hifa4_problem* p, const hifa4_fwd_options* o
   e = hifa4::launch_decode(dl, hs);
   if (e != hipSuccess) return hip_fail(e, "decode kernels");
   if (ev && (e = hipEventRecord(ev[2], hs)) != hipSuccess) return hip_fail(e, "timing event");
+  return HIFA4_OK;
+}
+
+// ---------------------------------------------------------------------------
+// The paged cache.
+namespace {
+
+hifa4_status check_paged_shape(int32_t heads_kv, int32_t D, int32_t operands) {
+  if (heads_kv <= 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "num_heads_kv must be > 0");
+  if (D != 64 && D != 128 && D != 256) return fail(HIFA4_ERR_UNSUPPORTED, "head_dim %d not in {64, 128, 256}", D);
+  if (operands != HIFA4_OPERANDS_HIF4 && operands != HIFA4_OPERANDS_FP16)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "pages hold HIF4 or FP16 operands, not %d", operands);
+  return HIFA4_OK;
+}
+
+// `touches`: the entry point reads or writes pages (else only sizes are asked for)
+hifa4_status check_paged(const hifa4_paged_cache* c, bool touches, hifa4::PagedCache* out) {
+  if (!c) return fail(HIFA4_ERR_INVALID_ARGUMENT, "cache is NULL");
+  hifa4_status st = check_paged_shape(c->num_heads_kv, c->head_dim, c->operands);
+  if (st != HIFA4_OK) return st;
+  if (c->batch <= 0 || c->num_pages < 0 || c->max_pages <= 0)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch and max_pages must be > 0 and num_pages >= 0");
+  if (c->max_pages >= (1 << 25) || (int64_t)c->batch * c->max_pages >= (1LL << 31))
+    return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", c->batch, c->max_pages);
+  if (touches) {
+    if (!c->pool || !c->block_table || !c->seq_lens) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null cache pointer");
+    if ((st = check_aligned16({c->pool, c->v_tail})) != HIFA4_OK) return st;
+    if ((st = check_aligned4({c->block_table, c->seq_lens})) != HIFA4_OK) return st;
+  }
+  out->pool = (uint8_t*)c->pool;
+  out->table = c->block_table;
+  out->lens = c->seq_lens;
+  out->tail = (hifa4::half_t*)c->v_tail;
+  out->batch = c->batch;
+  out->hkv = c->num_heads_kv;
+  out->D = c->head_dim;
+  out->num_pages = c->num_pages;
+  out->max_pages = c->max_pages;
+  out->fp16 = c->operands == HIFA4_OPERANDS_FP16;
+  return HIFA4_OK;
+}
+
+hifa4_status check_query_heads(int32_t hq, int32_t batch, int32_t hkv) {
+  if (hq <= 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "num_heads_q must be > 0");
+  if (hq % hkv) return fail(HIFA4_ERR_UNSUPPORTED, "num_heads_q (%d) must be a multiple of num_heads_kv (%d)", hq, hkv);
+  if ((int64_t)batch * hq >= (1LL << 24))
+    return fail(HIFA4_ERR_UNSUPPORTED, "problem too large for 32-bit row indexing");
+  return HIFA4_OK;
+}
+
+// workgroups of a launch over (sequence, page, head)
+hifa4_status check_page_grid(const hifa4_paged_cache* c, int32_t tokens) {
+  const int64_t blocks = ((int64_t)tokens + 62) / 64 + 1;
+  if (blocks * c->batch * c->num_heads_kv >= (1LL << 31))
+    return fail(HIFA4_ERR_UNSUPPORTED, "too many pages for one launch");
+  return HIFA4_OK;
+}
+
+}  // namespace
+
+size_t hifa4_paged_page_bytes(int32_t num_heads_kv, int32_t head_dim, int32_t operands) {
+  if (check_paged_shape(num_heads_kv, head_dim, operands) != HIFA4_OK) return 0;
+  return (size_t)num_heads_kv * hifa4::paged_record_bytes(head_dim, operands == HIFA4_OPERANDS_FP16);
+}
+
+hifa4_status hifa4_paged_append(const hifa4_paged_cache* c, int32_t total_new, int32_t max_new, const int32_t* cu_new,
+                                const void* k, const void* v, const float* s, void* stream) {
+  hifa4::PagedAppend a;
+  hifa4_status st = check_paged(c, true, &a.c);
+  if (st != HIFA4_OK) return st;
+  if (total_new < 0 || max_new < 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "total_new and max_new must be >= 0");
+  if (!cu_new && total_new != c->batch)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "without cu_new there is one new token per sequence (%d), not %d in all",
+                c->batch, total_new);
+  if (total_new == 0 || max_new == 0) return HIFA4_OK;
+  if (!k || !v) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if (!a.c.fp16 && !c->v_tail) return fail(HIFA4_ERR_INVALID_ARGUMENT, "HIF4 pages need v_tail");
+  if ((st = check_aligned16({k, v, s})) != HIFA4_OK) return st;
+  if ((st = check_aligned4({cu_new})) != HIFA4_OK) return st;
+  a.max_new = cu_new ? std::min(max_new, total_new) : 1;
+  if ((st = check_page_grid(c, a.max_new)) != HIFA4_OK) return st;
+  a.k = (const hifa4::half_t*)k;
+  a.v = (const hifa4::half_t*)v;
+  a.s = s;
+  a.cu = cu_new;
+  a.total = total_new;
+  const hipError_t e = hifa4::launch_paged_append(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged append");
+  return HIFA4_OK;
+}
+
+hifa4_status hifa4_paged_gather(const hifa4_paged_cache* c, int32_t total_tokens, int32_t max_tokens,
+                                const int32_t* cu_tokens, const int32_t* starts, void* k, void* v, void* stream) {
+  hifa4::PagedGather a;
+  hifa4_status st = check_paged(c, true, &a.c);
+  if (st != HIFA4_OK) return st;
+  if (total_tokens < 0 || max_tokens < 0)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "total_tokens and max_tokens must be >= 0");
+  if (!cu_tokens) return fail(HIFA4_ERR_INVALID_ARGUMENT, "cu_tokens is NULL");
+  if (total_tokens == 0 || max_tokens == 0) return HIFA4_OK;
+  if (!k || !v) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if ((st = check_aligned16({k, v})) != HIFA4_OK) return st;
+  if ((st = check_aligned4({cu_tokens, starts})) != HIFA4_OK) return st;
+  a.max_tokens = std::min(max_tokens, total_tokens);
+  if ((st = check_page_grid(c, a.max_tokens)) != HIFA4_OK) return st;
+  a.cu = cu_tokens;
+  a.starts = starts;
+  a.k = (hifa4::half_t*)k;
+  a.v = (hifa4::half_t*)v;
+  a.total = total_tokens;
+  const hipError_t e = hifa4::launch_paged_gather(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged gather");
+  return HIFA4_OK;
+}
+
+size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q, int32_t page_weights) {
+  hifa4::PagedCache pc;
+  if (check_paged(c, false, &pc) != HIFA4_OK || check_query_heads(num_heads_q, c->batch, c->num_heads_kv) != HIFA4_OK)
+    return 0;
+  return hifa4::paged_decode_workspace(c->batch, num_heads_q, c->num_heads_kv, c->head_dim, c->max_pages,
+                                       page_weights != 0);
+}
+
+hifa4_status hifa4_paged_decode_fwd(const hifa4_paged_cache* c, int32_t num_heads_q, const void* q, const float* s,
+                                    void* o, float* lse, const float* page_weights, float* weights_out, float decay,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  hifa4::PagedDecode a;
+  hifa4_status st = check_paged(c, true, &a.c);
+  if (st != HIFA4_OK) return st;
+  if ((st = check_query_heads(num_heads_q, c->batch, c->num_heads_kv)) != HIFA4_OK) return st;
+  if (!q || !o || !lse) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if ((page_weights == nullptr) != (weights_out == nullptr))
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "page_weights and weights_out must both be set or both be NULL");
+  if (page_weights && !std::isfinite(decay)) return fail(HIFA4_ERR_INVALID_ARGUMENT, "decay must be finite");
+  if ((st = check_aligned16({q, s, o, workspace})) != HIFA4_OK) return st;
+  if ((st = check_aligned4({lse, page_weights, weights_out})) != HIFA4_OK) return st;
+  const size_t need = hifa4::paged_decode_workspace(c->batch, num_heads_q, c->num_heads_kv, c->head_dim, c->max_pages,
+                                                    page_weights != nullptr);
+  if (!workspace || workspace_bytes < need)
+    return fail(HIFA4_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
+  a.hq = num_heads_q;
+  a.q = (const hifa4::half_t*)q;
+  a.s = s;
+  a.o = (hifa4::half_t*)o;
+  a.lse = lse;
+  a.w_in = page_weights;
+  a.w_out = weights_out;
+  a.decay = decay;
+  a.scale = (float)(1.4426950408889634 / std::sqrt((double)c->head_dim));
+  a.ws = (uint8_t*)workspace;
+  const hipError_t e = hifa4::launch_paged_decode(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged decode kernels");
+  return HIFA4_OK;
+}
+
+hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* block_table, const int32_t* seq_lens,
+                               const float* page_weights, int32_t budget, int32_t first, int32_t last,
+                               int32_t* out_table, int32_t* out_lens, float* out_weights, int32_t* freed,
+                               int32_t* num_freed, void* stream) {
+  if (batch <= 0 || max_pages <= 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch and max_pages must be > 0");
+  if (max_pages >= (1 << 25) || (int64_t)batch * max_pages >= (1LL << 31))
+    return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", batch, max_pages);
+  if (first < 0 || last < 1 || (int64_t)first + last > budget)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "needs first >= 0, last >= 1 and first + last <= budget (%d, %d, %d)", first,
+                last, budget);
+  if (!block_table || !seq_lens || !page_weights || !out_table || !out_lens || !out_weights || !freed || !num_freed)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  const hifa4_status st = check_aligned4(
+      {block_table, seq_lens, page_weights, out_table, out_lens, out_weights, freed, num_freed});
+  if (st != HIFA4_OK) return st;
+  hifa4::PagedEvict a;
+  a.batch = batch;
+  a.max_pages = max_pages;
+  a.budget = budget;
+  a.first = first;
+  a.last = last;
+  a.table = block_table;
+  a.lens = seq_lens;
+  a.w = page_weights;
+  a.out_table = out_table;
+  a.out_lens = out_lens;
+  a.out_w = out_weights;
+  a.freed = freed;
+  a.num_freed = num_freed;
+  const hipError_t e = hifa4::launch_paged_evict(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged evict");
   return HIFA4_OK;
 }
 

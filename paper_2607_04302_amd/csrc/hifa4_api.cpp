@@ -289,8 +289,8 @@ hifa4_status check_paged(const hifa4_paged_cache* c, bool touches, hifa4::PagedC
   if (!c) return fail(HIFA4_ERR_INVALID_ARGUMENT, "cache is NULL");
   hifa4_status st = check_paged_shape(c->num_heads_kv, c->head_dim, c->operands);
   if (st != HIFA4_OK) return st;
-  if (c->batch <= 0 || c->num_pages < 0 || c->max_pages <= 0)
-    return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch and max_pages must be > 0 and num_pages >= 0");
+  if (c->batch <= 0 || c->num_pages <= 0 || c->max_pages <= 0)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch, num_pages and max_pages must be > 0");
   if (c->max_pages >= (1 << 25) || (int64_t)c->batch * c->max_pages >= (1LL << 31))
     return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", c->batch, c->max_pages);
   if (touches) {

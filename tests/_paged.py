@@ -134,7 +134,12 @@ def decode(q, pool, table, lens, fmt, s=None, weights=None, decay=1.0):
 
     Score error: D + 8 roundings of 2^-24 relative to sum |q k| / sqrt(D), in the worst order.  An error e of the
     scores moves p and the sums by e each way; p's own rounding is 2^-11 at most, o's 2^-11 of the result (and half
-    a subnormal step); exponentials, partial sums and joins add 2^-18."""
+    a subnormal step); exponentials, partial sums and joins add 2^-18.
+
+    On HIF4 pages a query value and a weight p are whole numbers of 32^-3 after scaling by a power of two that brings
+    the largest of their 64 (a group of channels, a page's keys) to 8 or more, below or at 16.  Rounding to nearest
+    moves one by half a step, 2^-16 of at least 8: by 2^-19 of that largest value.  So a score moves by 2^-19 of
+    sum over the groups of max |q| sum |k| / sqrt(D) more, and o by 2^-19 of sum over the pages of max p sum |v|."""
     b_, hq, d = q.shape
     hkv = pool.shape[1]
     grp = hq // hkv
@@ -161,7 +166,13 @@ def decode(q, pool, table, lens, fmt, s=None, weights=None, decay=1.0):
             o[b, h] = p @ vv
             lse[h, b] = m + math.log(e.sum())
             es = (d + 8) * 2.0 ** -24 * (np.abs(kk) @ np.abs(x)).max() / math.sqrt(d)
-            bo[b, h] = (2.0 ** -11 + 2 * es + 2.0 ** -18) * (p @ np.abs(vv)) + 2.0 ** -11 * np.abs(o[b, h]) + 2.0 ** -25
+            if fmt == HIF4:
+                qm = np.repeat(np.abs(x).reshape(-1, 64).max(1), 64)
+                es += 2.0 ** -19 * (np.abs(kk) @ qm).max() / math.sqrt(d)
+                page = np.flatnonzero(there) // PAGE
+                for j in set(page.tolist()):
+                    bo[b, h] += 2.0 ** -19 * p[page == j].max() * np.abs(vv[page == j]).sum(0)
+            bo[b, h] += (2.0 ** -11 + 2 * es + 2.0 ** -18) * (p @ np.abs(vv)) + 2.0 ** -11 * np.abs(o[b, h]) + 2.0 ** -25
             bl[h, b] = es + 2.0 ** -18 + 2.0 ** -22 * abs(lse[h, b])
             if w is not None:
                 full = np.zeros(-(-n // PAGE) * PAGE)

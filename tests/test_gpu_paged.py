@@ -47,7 +47,7 @@ def _check(got, want, bound, what):
     assert np.array_equal(got[~fin], want[~fin]), what
     err = np.abs(got - np.where(fin, want, 0.0))[fin]
     bad = err > bound[fin]
-    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} out of bounds, worst {np.max(err / bound[fin]):.2f} times"
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} out of bounds, worst {np.max(err[bad] / bound[fin][bad]):.2f} times"
 
 
 # --------------------------------------------------------------------------- decode

@@ -60,7 +60,7 @@ def test_cache_is_checked(lib, call):
     assert call(lib, _cache(operands=2)) == -1
     assert call(lib, _cache(batch=0)) == -1
     assert call(lib, _cache(max_pages=0)) == -1
-    assert call(lib, _cache(num_pages=-1)) == -1
+    assert call(lib, _cache(num_pages=0)) == -1
     assert call(lib, _cache(max_pages=1 << 25)) == -2
     assert call(lib, _cache(max_pages=1 << 24, batch=1 << 8)) == -2
     for name in ("pool", "block_table", "seq_lens"):

@@ -16,12 +16,17 @@
 #include "hifa4_device.h"
 #include "hifa4_packed.h"
 #include "hifa4_paged.h"
+#include "hifa4_words.h"
 
 #include <algorithm>
 
 namespace hifa4 {
 
-constexpr int kWaves = 2048;      // waves that share the work of a call
+typedef int i8v_t __attribute__((ext_vector_type(8)));
+typedef float f4v_t __attribute__((ext_vector_type(4)));
+typedef short s2v_t __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 3072;      // waves that share the work of a call
 
 // How the pages are cut: a run has at most `per` pages, every sequence is cut
 // into equal parts, and all of them are numbered densely: at most
@@ -36,49 +41,46 @@ struct Run {
   int first, count;               // the sequence's runs: [first, first + count)
 };
 
-__device__ __forceinline__ int wave_sum(int x) {
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-  return x;
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // lane 15 of each row to the next
+  return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
 }
 __device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
   return b < c.batch ? (paged_len(c, b) + kPage - 1) / kPage : 0;
 }
-__device__ __forceinline__ int pages_per_run(const PagedCache& c, int lane) {
-  int total = 0;
-  for (int b0 = 0; b0 < c.batch; b0 += 64) total += pages_of(c, b0 + lane);
-  total = wave_sum(total);
-  const int target = run_target(c.hkv);
-  return max(1, (total + target - 1) / target);
-}
 // The run numbered r (found by a whole wave), or with r < 0 the runs of
 // sequence `want`.
 __device__ __forceinline__ Run find_run(const PagedCache& c, int r, int want, int lane) {
-  const int per = pages_per_run(c, lane);
+  const int n0 = pages_of(c, lane);
+  int total = __builtin_amdgcn_readlane(wave_scan(n0), 63);
+  for (int b0 = 64; b0 < c.batch; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(pages_of(c, b0 + lane)), 63);
+  const int target = run_target(c.hkv), per = max(1, (total + target - 1) / target);
   Run out = {-1, 0, 0, 0, 0};
   int before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    const int b = b0 + lane, n = pages_of(c, b), cnt = (n + per - 1) / per;
-    int upto = cnt;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(upto, d);
-      if (lane >= d) upto += y;
-    }
-    const int mine = before + upto - cnt;
-    const bool hit = r >= 0 ? (r >= mine && r < mine + cnt) : b == want;
-    const unsigned long long who = __ballot(hit);
+    const int n = b0 ? pages_of(c, b0 + lane) : n0, cnt = (n + per - 1) / per;
+    const int upto = wave_scan(cnt), mine = before + upto - cnt;
+    const bool hit = r >= 0 ? (r >= mine && r < mine + cnt) : b0 + lane == want;
+    const unsigned long long who = __builtin_amdgcn_ballot_w64(hit);
     if (who) {
-      const int src = __ffsll(who) - 1;
+      const int src = __builtin_ctzll(who);
       out.b = b0 + src;
-      out.first = __shfl(mine, src);
-      out.count = __shfl(cnt, src);
-      const int pages = __shfl(n, src);
-      if (r >= 0) {
-        out.begin = (int)((long)(r - out.first) * pages / out.count);
-        out.end = (int)((long)(r - out.first + 1) * pages / out.count);
+      out.first = __builtin_amdgcn_readlane(mine, src);
+      out.count = __builtin_amdgcn_readlane(cnt, src);
+      const int pages = __builtin_amdgcn_readlane(n, src);
+      if (r >= 0) {                  // the first runs get one page more where the count does not divide
+        const int i = r - out.first, some = pages / out.count, more = pages % out.count;
+        out.begin = i * some + min(i, more);
+        out.end = out.begin + some + (i < more);
       }
       return out;
     }
-    before += __shfl(upto, 63);
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
   return out;
 }
@@ -103,11 +105,20 @@ size_t paged_decode_workspace(int batch, int hq, int hkv, int D, int max_pages, 
   return slots * hq * (D + 2) * 4 + (weights ? (size_t)batch * max_pages * hq * 8 : 0);
 }
 
-// fp16(q s): the exact product rounded once.
+// q s to fp16, the exact product rounded once: the fp32 product made odd where
+// it is not exact, so that the second rounding is the only one.
+__device__ __forceinline__ half_t round_product(half_t q, float s) {
+  const float p = (float)q * s, e = fmaf((float)q, s, -p);
+  uint32_t b = __float_as_uint(p);
+  if ((__float_as_uint(e) ^ b) & 0x80000000u) b -= e != 0.0f;      // |p| is above the product: one step toward zero
+  return (half_t)__uint_as_float(e != 0.0f ? b | 1u : b);
+}
+
+// The smoothed query value.
 __device__ __forceinline__ half_t smoothed_q(const PagedDecode& a, int b, int h, int d) {
   const half_t q = a.q[((size_t)b * a.hq + h) * a.c.D + d];
   if (!a.s) return q;
-  return rn16_from_f64((double)q * (double)a.s[(size_t)(h / (a.hq / a.c.hkv)) * a.c.D + d]);
+  return round_product(q, a.s[(size_t)(h / (a.hq / a.c.hkv)) * a.c.D + d]);
 }
 
 __device__ __forceinline__ float record_value(const uint8_t* rec, int D, bool fp16, bool v, int key, int ch) {
@@ -156,10 +167,6 @@ __device__ __forceinline__ float record_value(const uint8_t* rec, int D, bool fp
 // exchanged, which makes the words of FP4 lanes j and 2 + j the keys whose
 // scores lanes 2j and 2j + 1 have: one exchange between neighbouring rows of
 // 16 lanes brings p into place.
-typedef int i8v_t __attribute__((ext_vector_type(8)));
-typedef float f4v_t __attribute__((ext_vector_type(4)));
-typedef short s2v_t __attribute__((ext_vector_type(2)));
-
 constexpr int kFp4 = 4, kFp8 = 0;            // operand formats of the instruction
 // The reference of the softmax is a whole power of two and moves only when a
 // page's largest score passes it by this many binades: fp32 sums do not mind.
@@ -209,26 +216,45 @@ struct Part {
   uint32_t e2;
   uint4 base[G];           // word t: the four rows whose products the lane holds
 };
+// A scalar address that the compiler takes as given: sums with a lane's 32-bit
+// offset stay in that form instead of becoming 64-bit vector additions.
+typedef const __attribute__((address_space(1))) uint8_t* global_ptr;
+__device__ __forceinline__ global_ptr scalar_address(const uint8_t* p) {
+  global_ptr g = (global_ptr)p;
+  asm("" : "+s"(g));
+  return g;
+}
+template <typename T>
+__device__ __forceinline__ T load_at(global_ptr p, uint32_t offset) {
+  return *(const __attribute__((address_space(1))) T*)(p + offset);
+}
 template <int G>
-__device__ __forceinline__ void load_part(Part<G>& p, const uint8_t* part, int lane, int k) {
+__device__ __forceinline__ void load_part(Part<G>& p, const uint8_t* part, uint32_t lane, uint32_t k) {
+  typedef unsigned u4v_t __attribute__((ext_vector_type(4)));
+  const global_ptr meta = scalar_address(part + 2048 * G);
 #pragma unroll
-  for (int i = 0; i < 2 * G; ++i) p.code[i] = *reinterpret_cast<const uint4*>(part + 1024 * i + 16 * lane);
-  const uint8_t* e3 = part + 2048 * G + 2 * G * lane;
-  const uint8_t* e2 = part + 2176 * G + G * lane;
+  for (int h = 0; h < (G + 1) / 2; ++h) {
+    const global_ptr code = scalar_address(part + 4096 * h);
+#pragma unroll
+    for (int i = 0; i < (G == 1 ? 2 : 4); ++i)
+      p.code[4 * h + i] = __builtin_bit_cast(uint4, load_at<u4v_t>(code, 16 * lane + 1024 * i));
+  }
   if (G == 1) {
-    p.e3[0] = *reinterpret_cast<const uint16_t*>(e3);
-    p.e2 = *e2;
+    p.e3[0] = load_at<uint16_t>(meta, 2 * lane);
+    p.e2 = load_at<uint8_t>(meta, lane + 128);
   } else if (G == 2) {
-    p.e3[0] = *reinterpret_cast<const uint32_t*>(e3);
-    p.e2 = *reinterpret_cast<const uint16_t*>(e2);
+    p.e3[0] = load_at<uint32_t>(meta, 4 * lane);
+    p.e2 = load_at<uint16_t>(meta, 2 * lane + 256);
   } else {
-    const uint2 x = *reinterpret_cast<const uint2*>(e3);
-    p.e3[0] = x.x;
-    p.e3[G == 4 ? 1 : 0] = x.y;
-    p.e2 = *reinterpret_cast<const uint32_t*>(e2);
+    typedef unsigned u2v_t __attribute__((ext_vector_type(2)));
+    const u2v_t x = load_at<u2v_t>(meta, 8 * lane);
+    p.e3[0] = x[0];
+    p.e3[G == 4 ? 1 : 0] = x[1];
+    p.e2 = load_at<uint32_t>(meta, 4 * lane + 512);
   }
 #pragma unroll
-  for (int i = 0; i < G; ++i) p.base[i] = *reinterpret_cast<const uint4*>(part + 2240 * G + 16 * G * k + 16 * i);
+  for (int i = 0; i < G; ++i)
+    p.base[i] = __builtin_bit_cast(uint4, load_at<u4v_t>(meta, 16 * G * k + 192 * G + 16 * i));
 }
 
 // 0xFFFF in each half-word of word (t, c) of `tile` with E3 = 0; x: the
@@ -250,15 +276,6 @@ __device__ __forceinline__ f4v_t mfma_word(uint32_t w, uint32_t keep, uint32_t s
   const i8v_t a = {(int)lo, (int)hi, (int)(lo & keep), (int)(hi & keep), 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, kFp4, kFp8, T, (int)scale, 0, (int)b_scale);
 }
-// Products of a tile's rows 16 T + 4k + v with the columns of b (both words).
-template <int G, int T>
-__device__ __forceinline__ f4v_t tile_product(const Part<G>& p, int tile, uint32_t x, uint32_t s0, uint32_t s1,
-                                              const i8v_t& b0, const i8v_t& b1, uint32_t b_scale) {
-  const uint4 w = p.code[2 * tile + T / 2];
-  f4v_t c = {0.0f, 0.0f, 0.0f, 0.0f};
-  c = mfma_word<T>(T & 1 ? w.z : w.x, e3_keep<G>(x, tile, T, 0), s0, b0, b_scale, c);
-  return mfma_word<T>(T & 1 ? w.w : w.y, e3_keep<G>(x, tile, T, 1), s1, b1, b_scale, c);
-}
 template <int G>
 __device__ __forceinline__ uint32_t e3_halves(const Part<G>& p, int tile) {
   const uint32_t x = ~p.e3[tile / 2];
@@ -268,17 +285,38 @@ __device__ __forceinline__ f4v_t bases(uint32_t w) {
   return f4v_t{__uint_as_float((w & 0xFFu) << 21), __uint_as_float((w >> 8 & 0xFFu) << 21),
                __uint_as_float((w >> 16 & 0xFFu) << 21), __uint_as_float((w >> 24) << 21)};
 }
-template <int G, typename F>
-__device__ __forceinline__ void products(const Part<G>& p, const i8v_t* b0, const i8v_t* b1, const uint32_t* b_scale, F use) {
+// use(tile, t, products, bases): products of a tile's rows 16 t + 4k + v with
+// the columns of the other operand, which get(tile, b0, b1, scale) fetches
+// (its two words' parts).
+template <int G, typename Get, typename Use>
+__device__ __forceinline__ void products(const Part<G>& p, Get get, Use use) {
 #pragma unroll
   for (int tile = 0; tile < G; ++tile) {
     const uint32_t x = e3_halves<G>(p, tile), s0 = e2_scales(p.e2, tile, 0), s1 = e2_scales(p.e2, tile, 1);
+    i8v_t b0, b1;
+    uint32_t scale;
+    get(tile, b0, b1, scale);
+    const uint4 w0 = p.code[2 * tile], w1 = p.code[2 * tile + 1];
+    const f4v_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+    // four chains of two, side by side
+    f4v_t c0 = mfma_word<0>(w0.x, e3_keep<G>(x, tile, 0, 0), s0, b0, scale, z);
+    f4v_t c1 = mfma_word<1>(w0.z, e3_keep<G>(x, tile, 1, 0), s0, b0, scale, z);
+    f4v_t c2 = mfma_word<2>(w1.x, e3_keep<G>(x, tile, 2, 0), s0, b0, scale, z);
+    f4v_t c3 = mfma_word<3>(w1.z, e3_keep<G>(x, tile, 3, 0), s0, b0, scale, z);
+    c0 = mfma_word<0>(w0.y, e3_keep<G>(x, tile, 0, 1), s1, b1, scale, c0);
+    c1 = mfma_word<1>(w0.w, e3_keep<G>(x, tile, 1, 1), s1, b1, scale, c1);
+    c2 = mfma_word<2>(w1.y, e3_keep<G>(x, tile, 2, 1), s1, b1, scale, c2);
+    c3 = mfma_word<3>(w1.w, e3_keep<G>(x, tile, 3, 1), s1, b1, scale, c3);
     const uint4 bw = p.base[tile];
-    use(tile, 0, tile_product<G, 0>(p, tile, x, s0, s1, b0[tile], b1[tile], b_scale[tile]), bases(bw.x));
-    use(tile, 1, tile_product<G, 1>(p, tile, x, s0, s1, b0[tile], b1[tile], b_scale[tile]), bases(bw.y));
-    use(tile, 2, tile_product<G, 2>(p, tile, x, s0, s1, b0[tile], b1[tile], b_scale[tile]), bases(bw.z));
-    use(tile, 3, tile_product<G, 3>(p, tile, x, s0, s1, b0[tile], b1[tile], b_scale[tile]), bases(bw.w));
+    use(tile, 0, c0, bases(bw.x));
+    use(tile, 1, c1, bases(bw.y));
+    use(tile, 2, c2, bases(bw.z));
+    use(tile, 3, c3, bases(bw.w));
   }
+}
+// The FP8 operand of two words (x: its FP4 lane j's, y: lane 2 + j's), each twice.
+__device__ __forceinline__ i8v_t fp8_operand(uint2 x, uint2 y) {
+  return i8v_t{(int)x.x, (int)x.y, (int)x.x, (int)x.y, (int)y.x, (int)y.y, (int)y.x, (int)y.y};
 }
 
 // The pages of a run, as their records: 64 table entries at a time, one a lane.
@@ -290,18 +328,68 @@ __device__ __forceinline__ void load_pages(Pages& p, const PagedCache& c, const 
   p.mine = from + lane < r.end ? c.table[(size_t)r.b * c.max_pages + from + lane] : -1;
 }
 
+// The digits of four query heads' rows (q: the first of them, `rows` exist) in
+// LDS: [channel group][c][FP4 lane][column 4 query + digit][8 channels]; and
+// the exponent that each group of 64 was scaled by.
 template <int G>
-__global__ void __launch_bounds__(64) k_runs_hif4(PagedDecode a, int tiles) {
+struct QueryDigits {
+  uint2 word[G][2][4][16];
+  int exponent[G][4];
+};
+template <int G>
+__device__ __forceinline__ void query_digits(QueryDigits<G>& out, const half_t* q, int rows, const float* s, int lane) {
+#pragma unroll
+  for (int i = lane; i < 32 * G; i += 64) {
+    const int row = i / (8 * G), g = i / 8 % G, w = i & 7;
+    uint4 in = make_uint4(0, 0, 0, 0);
+    if (row < rows) in = *reinterpret_cast<const uint4*>(q + (size_t)row * 64 * G + 64 * g + 8 * w);
+    const h2_t y[4] = {__builtin_bit_cast(h2_t, in.x), __builtin_bit_cast(h2_t, in.y), __builtin_bit_cast(h2_t, in.z),
+                       __builtin_bit_cast(h2_t, in.w)};
+    float x[8];
+    if (s) {
+      const f4v_t s0 = *reinterpret_cast<const f4v_t*>(s + 64 * g + 8 * w);
+      const f4v_t s1 = *reinterpret_cast<const f4v_t*>(s + 64 * g + 8 * w + 4);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = (float)round_product(y[u >> 1][u & 1], u < 4 ? s0[u & 3] : s1[u & 3]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = (float)y[u >> 1][u & 1];
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) top = fmaxf(top, fabsf(x[u]));
+    top = __uint_as_float(reduce8(__float_as_uint(top), [](uint32_t a, uint32_t b) {
+      return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+    // 2^e <= top < 2^(e+1): 2^(3-e) x lies below 16
+    const int e = top > 0.0f ? (int)(__float_as_uint(top) >> 23) - 127 : 0;
+    const float up = __uint_as_float((uint32_t)(127 + 3 - e) << 23);
+    if (w == 0) out.exponent[g][row] = e;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const DigitScale ds = digit_scale(k);
+      float d[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) d[u] = digit(x[u] * up, ds);
+      out.word[g][w & 1][w >> 1][4 * row + k] = make_uint2(fp8x4(d[0], d[1], d[2], d[3]), fp8x4(d[4], d[5], d[6], d[7]));
+    }
+  }
+}
+
+template <int G>
+__global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a, int tiles) {
   constexpr int D = 64 * G;
+  __shared__ QueryDigits<G> qd;
   const int lane = threadIdx.x, n = lane & 15, k = lane >> 4, piece = n & 3;
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
   const Run run = find_run(a.c, r, 0, lane);
   if (run.b < 0) return;
-  const int len = paged_len(a.c, run.b);
+  const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
   const DecodeWs ws = decode_ws(a.ws, a.c.batch, a.hq, a.c.hkv, D, a.c.max_pages);
   const size_t rec_bytes = (size_t)72 * D;
   const int v_lane = 16 * ((k & 1) * 2 + (k >> 1)) + n;        // lanes k = 1, 2 exchanged
+  const int q_in = 4 * tile + (n >> 2), h = head * group + q_in;
 
   Pages pg;
   load_pages(pg, a.c, run, run.begin, lane);
@@ -313,60 +401,17 @@ __global__ void __launch_bounds__(64) k_runs_hif4(PagedDecode a, int tiles) {
     there = (unsigned)page < (unsigned)a.c.num_pages;
     return a.c.pool + ((size_t)(there ? page : 0) * a.c.hkv + head) * rec_bytes;
   };
+  query_digits<G>(qd, a.q + ((size_t)run.b * a.hq + head * group + 4 * tile) * D, group - 4 * tile,
+                  a.s ? a.s + (size_t)head * D : nullptr, lane);
   Part<G> kp, vp;
   const uint8_t* rec = record(run.begin, has);
   load_part<G>(kp, rec, lane, k);
   load_part<G>(vp, rec + 2304 * G, v_lane, k);
-
-  // the query's pieces
-  const int q_in = 4 * tile + (n >> 2), h = head * group + q_in;
+  __syncthreads();
   const DigitScale ds = digit_scale(piece);
-  i8v_t qa[G], qb[G];
   uint32_t q_scale[G];
-  {
-    const int j = k >> 1;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      float x[2][2][8];                // [c][FP4 lane j, 2 + j][value]
-      float top = 0.0f;
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const int ch = 64 * g + 8 * (2 * (j + 2 * f) + c);
-          uint4 in = make_uint4(0, 0, 0, 0);
-          if (q_in < group) in = *reinterpret_cast<const uint4*>(a.q + ((size_t)run.b * a.hq + h) * D + ch);
-          const h2_t y[4] = {__builtin_bit_cast(h2_t, in.x), __builtin_bit_cast(h2_t, in.y),
-                             __builtin_bit_cast(h2_t, in.z), __builtin_bit_cast(h2_t, in.w)};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            half_t z = y[i >> 1][i & 1];
-            if (a.s) z = rn16_from_f64((double)z * (double)a.s[(size_t)head * D + ch + i]);
-            x[c][f][i] = (float)z;
-            top = fmaxf(top, fabsf((float)z));
-          }
-        }
-      top = max_across_rows(top);
-      // 2^e <= top < 2^(e+1): 2^(3-e) x lies below 16
-      const int e = top > 0.0f ? (int)(__float_as_uint(top) >> 23) - 127 : 0;
-      const float up = __uint_as_float((uint32_t)(127 + 3 - e) << 23);
-      q_scale[g] = (uint32_t)(127 + e - 3 - 5 * piece);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        int w[2][2];
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float y[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) y[u] = digit(x[c][f][4 * i + u] * up, ds);
-            w[f][i] = (int)fp8x4(y[0], y[1], y[2], y[3]);
-          }
-        (c ? qb : qa)[g] = i8v_t{w[0][0], w[0][1], w[0][0], w[0][1], w[1][0], w[1][1], w[1][0], w[1][1]};
-      }
-    }
-  }
+  for (int g = 0; g < G; ++g) q_scale[g] = (uint32_t)(127 - 3 - 5 * piece + qd.exponent[g][n >> 2]);
 
   // scores in log2 units; sums are of p = 2^(score - ref), ref a whole number
   float ref = -1e30f, l = 0.0f;
@@ -378,22 +423,28 @@ __global__ void __launch_bounds__(64) k_runs_hif4(PagedDecode a, int tiles) {
 
   for (int j = run.begin; j < run.end; ++j) {
     f4v_t s[4];
-    products<G>(kp, qa, qb, q_scale, [&](int g, int t, f4v_t d, f4v_t b) {
+    asm volatile("" ::: "memory");       // the query's operands come from LDS in every page, not from registers
+    products<G>(kp, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+      const int j2 = k >> 1;
+      b0 = fp8_operand(qd.word[g][0][j2][n], qd.word[g][0][2 + j2][n]);
+      b1 = fp8_operand(qd.word[g][1][j2][n], qd.word[g][1][2 + j2][n]);
+      scale = q_scale[g];
+    }, [&](int g, int t, f4v_t d, f4v_t b) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) s[t][v] = g == 0 ? d[v] * b[v] : fmaf(d[v], b[v], s[t][v]);
     });
     // the next page's K loads while this page's softmax and V go on
-    const uint8_t* next = nullptr;
-    if (j + 1 < run.end) {
-      next = record(j + 1, has_next);
-      load_part<G>(kp, next, lane, k);
-    }
+    // (the last page's own again at the end, which nothing waits for: a load that may not
+    // happen would keep both pages' registers)
+    const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
+    load_part<G>(kp, next, lane, k);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v) s[t][v] = sum_pieces(s[t][v]) * a.scale;
     const int held = has ? len - j * kPage : 0;
     if (held < kPage) {
+      asm volatile("");                  // (kept a branch)
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -444,21 +495,17 @@ __global__ void __launch_bounds__(64) k_runs_hif4(PagedDecode a, int tiles) {
     for (int c = 0; c < 2; ++c) {
       const auto x = __builtin_amdgcn_permlane16_swap(pw[2 * c], pw[2 * c], false, false);
       const auto y = __builtin_amdgcn_permlane16_swap(pw[2 * c + 1], pw[2 * c + 1], false, false);
-      pa[c] = i8v_t{(int)x[0], (int)y[0], (int)x[0], (int)y[0], (int)x[1], (int)y[1], (int)x[1], (int)y[1]};
+      pa[c] = fp8_operand(make_uint2(x[0], y[0]), make_uint2(x[1], y[1]));
     }
-    i8v_t p0[G], p1[G];
-    uint32_t ps[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      p0[g] = pa[0];
-      p1[g] = pa[1];
-      ps[g] = p_scale;
-    }
-    products<G>(vp, p0, p1, ps, [&](int g, int t, f4v_t d, f4v_t b) {
+    products<G>(vp, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+      b0 = pa[0];
+      b1 = pa[1];
+      scale = p_scale;
+    }, [&](int g, int t, f4v_t d, f4v_t b) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) o[g][t][v] = fmaf(d[v], b[v], o[g][t][v]);
     });
-    if (next) load_part<G>(vp, next + 2304 * G, v_lane, k);
+    load_part<G>(vp, next + 2304 * G, v_lane, k);
     has = has_next;
   }
 
@@ -524,55 +571,103 @@ __global__ void __launch_bounds__(64) k_runs_fp16(PagedDecode a) {
   if (lane == 0) ws.ml[slot] = make_float2(m, l);
 }
 
-// LSE (log2) of row (b, h) from its runs.
-__device__ __forceinline__ float2 row_lse(const DecodeWs& ws, int hq, const Run& run, int h, int lane) {
+// ---------------------------------------------------------------------------
+// Joining the runs of a row: with m the largest of their references,
+// o = sum o_i 2^(m_i - m) / l, l = sum l_i 2^(m_i - m).  One workgroup per row
+// and kWidth channels (a row's channels are shared out where there are few
+// rows); behind those, with page weights, one per 64 pages of a sequence.
+constexpr int kJoin = 256;
+
+// (m, l) of row h over the runs; every thread of the workgroup gets it.
+__device__ __forceinline__ float2 join_row(const float2* ml, int hq, const Run& run, int h, float* red) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   float m = -INFINITY;
-  for (int i = lane; i < run.count; i += 64) m = fmaxf(m, ws.ml[(size_t)(run.first + i) * hq + h].x);
+  for (int i = tid; i < run.count; i += kJoin) m = fmaxf(m, ml[(size_t)(run.first + i) * hq + h].x);
   for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  const float ref = m == -INFINITY ? 0.0f : m;
+  if (lane == 0) red[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  if (m == -INFINITY) m = 0.0f;
   float l = 0.0f;
-  for (int i = lane; i < run.count; i += 64) {
-    const float2 x = ws.ml[(size_t)(run.first + i) * hq + h];
-    l += x.y * exp2f(x.x - ref);
+  for (int i = tid; i < run.count; i += kJoin) {
+    const float2 x = ml[(size_t)(run.first + i) * hq + h];
+    l += x.y * __builtin_amdgcn_exp2f(x.x - m);
   }
   for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-  return make_float2(ref, l);
+  if (lane == 0) red[4 + wave] = l;
+  __syncthreads();
+  return make_float2(m, (red[4] + red[5]) + (red[6] + red[7]));
 }
 
-// One wave per row (b, h); behind them one wave per 64 pages of a sequence.
-__global__ void __launch_bounds__(64) k_paged_join(PagedDecode a, int rows) {
-  const int lane = threadIdx.x, D = a.c.D;
+template <int kWidth>
+__global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
+  constexpr int kCols = kWidth / 4, kSets = kJoin / kCols;
+  __shared__ float red[8];
+  __shared__ f4v_t part[kSets][kCols];
+  __shared__ float2 joined[4][64];
+  const int tid = threadIdx.x, lane = tid & 63, D = a.c.D;
   const DecodeWs ws = decode_ws(a.ws, a.c.batch, a.hq, a.c.hkv, D, a.c.max_pages);
   if ((int)blockIdx.x < rows) {
-    const int b = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
+    const int slices = D / kWidth, row = blockIdx.x / slices, d0 = blockIdx.x % slices * kWidth;
+    const int b = row / a.hq, h = row % a.hq;
     const Run run = find_run(a.c, -1, b, lane);
-    const float2 x = row_lse(ws, a.hq, run, h, lane);
-    for (int d = lane; d < D; d += 64) {
-      float o = 0.0f;
-      for (int i = 0; i < run.count; ++i) {
-        const size_t slot = (size_t)(run.first + i) * a.hq + h;
-        o += ws.o[slot * D + d] * exp2f(ws.ml[slot].x - x.x);
-      }
-      a.o[(size_t)blockIdx.x * D + d] = (half_t)(x.y == 0.0f ? 0.0f : o / x.y);
+    const float2 x = join_row(ws.ml, a.hq, run, h, red);
+    const int col = tid % kCols, set = tid / kCols;
+    f4v_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int i = set; i < run.count; i += kSets) {
+      const size_t slot = (size_t)(run.first + i) * a.hq + h;
+      o += *reinterpret_cast<const f4v_t*>(ws.o + slot * D + d0 + 4 * col) * __builtin_amdgcn_exp2f(ws.ml[slot].x - x.x);
     }
-    if (lane == 0)
-      a.lse[(size_t)h * a.c.batch + b] = x.y == 0.0f ? -INFINITY : (float)((x.x + log2f(x.y)) * 0.6931471805599453);
+    part[set][col] = o;
+    __syncthreads();
+    if (tid < kWidth) {
+      float sum = 0.0f;
+      for (int i = 0; i < kSets; ++i) sum += part[i][tid / 4][tid & 3];
+      a.o[(size_t)row * D + d0 + tid] = (half_t)(x.y == 0.0f ? 0.0f : sum / x.y);
+    }
+    if (tid == 0 && d0 == 0)
+      a.lse[(size_t)h * a.c.batch + b] =
+          x.y == 0.0f ? -INFINITY : (float)(((double)x.x + (double)__log2f(x.y)) * 0.6931471805599453);
     return;
   }
+  // page weights: (m, l) of 64 heads at a time, then a sequence's pages, four threads a page
   const int chunks = (a.c.max_pages + 63) / 64, at = blockIdx.x - rows;
-  const int b = at / chunks, j = 64 * (at % chunks) + lane;
+  const int b = at / chunks, j0 = 64 * (at % chunks), wave = tid >> 6;
   const Run run = find_run(a.c, -1, b, lane);
-  const int pages = pages_of(a.c, b);
-  if (j - lane >= a.c.max_pages) return;
+  const int pages = pages_of(a.c, b), j = j0 + tid / 4;
   float w = 0.0f;
-  for (int h = 0; h < a.hq && pages > j - lane; ++h) {
-    const float2 x = row_lse(ws, a.hq, run, h, lane);
-    if (j < pages && x.y != 0.0f) {
-      const float2 y = ws.page[((size_t)b * a.c.max_pages + j) * a.hq + h];
-      w += y.y * exp2f(y.x - x.x) / x.y;
+  for (int h0 = 0; h0 < a.hq && j0 < pages; h0 += 64) {
+    float m = -INFINITY, l = 0.0f;
+    if (h0 + lane < a.hq)
+      for (int i = wave; i < run.count; i += 4) {
+        const float2 x = ws.ml[(size_t)(run.first + i) * a.hq + h0 + lane];
+        const float to = fmaxf(m, x.x), ref = to == -INFINITY ? 0.0f : to;
+        l = l * __builtin_amdgcn_exp2f(m - ref) + x.y * __builtin_amdgcn_exp2f(x.x - ref);
+        m = to;
+      }
+    joined[wave][lane] = make_float2(m, l);
+    __syncthreads();
+    if (wave == 0) {
+      float2 x[4];
+      for (int i = 0; i < 4; ++i) x[i] = joined[i][lane];
+      m = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+      if (m == -INFINITY) m = 0.0f;
+      l = 0.0f;
+      for (int i = 0; i < 4; ++i) l += x[i].y * __builtin_amdgcn_exp2f(x[i].x - m);
+      joined[0][lane] = make_float2(m, l == 0.0f ? 0.0f : 1.0f / l);
     }
+    __syncthreads();
+    if (j < pages)
+      for (int h = tid & 3; h < min(64, a.hq - h0); h += 4) {
+        const float2 x = joined[0][h], y = ws.page[((size_t)b * a.c.max_pages + j) * a.hq + h0 + h];
+        w += y.y * __builtin_amdgcn_exp2f(y.x - x.x) * x.y;
+      }
+    __syncthreads();
   }
-  if (j < a.c.max_pages) {
+  w += __shfl_xor(w, 1);
+  w += __shfl_xor(w, 2);
+  if ((tid & 3) == 0 && j < a.c.max_pages) {
     const size_t i = (size_t)b * a.c.max_pages + j;
     a.w_out[i] = j < pages ? a.decay * a.w_in[i] + w : a.w_in[i];
   }
@@ -592,9 +687,20 @@ hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
     k_runs_hif4<4><<<grid, 64, 0, st>>>(a, tiles);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int rows = a.c.batch * a.hq;
+  // channels shared out while there are fewer rows than compute units
   const size_t extra = a.w_in ? (size_t)a.c.batch * ((a.c.max_pages + 63) / 64) : 0;
-  k_paged_join<<<dim3((unsigned)(rows + extra)), 64, 0, st>>>(a, rows);
+  const int rows = a.c.batch * a.hq;
+  const bool few = rows < 256;
+  const int groups = few ? rows * (a.c.D / 32) : rows;
+  const dim3 join((unsigned)(groups + extra));
+  if (few)
+    k_paged_join<32><<<join, kJoin, 0, st>>>(a, groups);
+  else if (a.c.D == 64)
+    k_paged_join<64><<<join, kJoin, 0, st>>>(a, groups);
+  else if (a.c.D == 128)
+    k_paged_join<128><<<join, kJoin, 0, st>>>(a, groups);
+  else
+    k_paged_join<256><<<join, kJoin, 0, st>>>(a, groups);
   return hipGetLastError();
 }
 

@@ -388,8 +388,7 @@ size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t nu
   hifa4::PagedCache pc;
   if (check_paged(c, false, &pc) != HIFA4_OK || check_query_heads(num_heads_q, c->batch, c->num_heads_kv) != HIFA4_OK)
     return 0;
-  return hifa4::paged_decode_workspace(c->batch, num_heads_q, c->num_heads_kv, c->head_dim, c->max_pages,
-                                       page_weights != 0);
+  return hifa4::paged_decode_workspace(pc, num_heads_q, page_weights != 0);
 }
 
 hifa4_status hifa4_paged_decode_fwd(const hifa4_paged_cache* c, int32_t num_heads_q, const void* q, const float* s,
@@ -405,8 +404,7 @@ hifa4_status hifa4_paged_decode_fwd(const hifa4_paged_cache* c, int32_t num_head
   if (page_weights && !std::isfinite(decay)) return fail(HIFA4_ERR_INVALID_ARGUMENT, "decay must be finite");
   if ((st = check_aligned16({q, s, o, workspace})) != HIFA4_OK) return st;
   if ((st = check_aligned4({lse, page_weights, weights_out})) != HIFA4_OK) return st;
-  const size_t need = hifa4::paged_decode_workspace(c->batch, num_heads_q, c->num_heads_kv, c->head_dim, c->max_pages,
-                                                    page_weights != nullptr);
+  const size_t need = hifa4::paged_decode_workspace(a.c, num_heads_q, page_weights != nullptr);
   if (!workspace || workspace_bytes < need)
     return fail(HIFA4_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
   a.hq = num_heads_q;

@@ -110,7 +110,7 @@ struct PagedDecode {
   uint8_t* ws;
 };
 
-size_t paged_decode_workspace(int batch, int hq, int hkv, int D, int max_pages, bool weights);
+size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights);
 
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st);
 hipError_t launch_paged_gather(const PagedGather& a, hipStream_t st);

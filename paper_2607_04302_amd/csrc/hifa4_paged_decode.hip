@@ -26,14 +26,23 @@ typedef int i8v_t __attribute__((ext_vector_type(8)));
 typedef float f4v_t __attribute__((ext_vector_type(4)));
 typedef short s2v_t __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 3072;      // waves that share the work of a call
-
-// How the pages are cut: a run has at most `per` pages, every sequence is cut
-// into equal parts, and all of them are numbered densely: at most
-// run_slots() runs.
-__host__ __device__ __forceinline__ int run_target(int hkv) { return (kWaves + hkv - 1) / hkv; }
-__host__ __device__ __forceinline__ size_t run_slots(int batch, int hkv, int max_pages) {
-  const size_t all = (size_t)batch * max_pages, most = (size_t)run_target(hkv) + batch;
+// Query heads that a wave takes: the 16 columns of a matrix product, four for
+// each query on HIF4 pages.
+__host__ __device__ __forceinline__ int query_tiles(int hq, int hkv, bool fp16) {
+  const int per = fp16 ? 16 : 4;
+  return (hq / hkv + per - 1) / per;
+}
+// How the pages are cut: into as many runs as give every SIMD the waves that
+// its registers hold.  Every sequence is cut into equal parts of at most
+// ceil(pages / target) pages, numbered densely over the sequences: at most
+// target + batch runs.
+__host__ __device__ __forceinline__ int run_target(int hq, int hkv, int D, bool fp16) {
+  const int waves = fp16 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : (D == 256 ? 1 : 3);
+  const int each = hkv * query_tiles(hq, hkv, fp16);
+  return (1024 * waves + each - 1) / each;
+}
+__host__ __device__ __forceinline__ size_t run_slots(int batch, int target, int max_pages) {
+  const size_t all = (size_t)batch * max_pages, most = (size_t)target + batch;
   return all < most ? all : most;
 }
 struct Run {
@@ -55,11 +64,11 @@ __device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
 }
 // The run numbered r (found by a whole wave), or with r < 0 the runs of
 // sequence `want`.
-__device__ __forceinline__ Run find_run(const PagedCache& c, int r, int want, int lane) {
+__device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, int want, int lane) {
   const int n0 = pages_of(c, lane);
   int total = __builtin_amdgcn_readlane(wave_scan(n0), 63);
   for (int b0 = 64; b0 < c.batch; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(pages_of(c, b0 + lane)), 63);
-  const int target = run_target(c.hkv), per = max(1, (total + target - 1) / target);
+  const int per = max(1, (total + target - 1) / target);
   Run out = {-1, 0, 0, 0, 0};
   int before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
@@ -92,17 +101,17 @@ struct DecodeWs {
   float2* ml;
   float2* page;
 };
-__host__ __device__ __forceinline__ DecodeWs decode_ws(uint8_t* ws, int batch, int hq, int hkv, int D, int max_pages) {
-  const size_t slots = run_slots(batch, hkv, max_pages);
+__host__ __device__ __forceinline__ DecodeWs decode_ws(uint8_t* ws, const PagedCache& c, int target, int hq) {
+  const size_t slots = run_slots(c.batch, target, c.max_pages);
   DecodeWs w;
   w.o = reinterpret_cast<float*>(ws);
-  w.ml = reinterpret_cast<float2*>(w.o + slots * hq * D);
+  w.ml = reinterpret_cast<float2*>(w.o + slots * hq * c.D);
   w.page = w.ml + slots * hq;
   return w;
 }
-size_t paged_decode_workspace(int batch, int hq, int hkv, int D, int max_pages, bool weights) {
-  const size_t slots = run_slots(batch, hkv, max_pages);
-  return slots * hq * (D + 2) * 4 + (weights ? (size_t)batch * max_pages * hq * 8 : 0);
+size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights) {
+  const size_t slots = run_slots(c.batch, run_target(hq, c.hkv, c.D, c.fp16), c.max_pages);
+  return slots * hq * (c.D + 2) * 4 + (weights ? (size_t)c.batch * c.max_pages * hq * 8 : 0);
 }
 
 // q s to fp16, the exact product rounded once: the fp32 product made odd where
@@ -112,30 +121,6 @@ __device__ __forceinline__ half_t round_product(half_t q, float s) {
   uint32_t b = __float_as_uint(p);
   if ((__float_as_uint(e) ^ b) & 0x80000000u) b -= e != 0.0f;      // |p| is above the product: one step toward zero
   return (half_t)__uint_as_float(e != 0.0f ? b | 1u : b);
-}
-
-// The smoothed query value.
-__device__ __forceinline__ half_t smoothed_q(const PagedDecode& a, int b, int h, int d) {
-  const half_t q = a.q[((size_t)b * a.hq + h) * a.c.D + d];
-  if (!a.s) return q;
-  return round_product(q, a.s[(size_t)(h / (a.hq / a.c.hkv)) * a.c.D + d]);
-}
-
-__device__ __forceinline__ float record_value(const uint8_t* rec, int D, bool fp16, bool v, int key, int ch) {
-  const int t = key_t(key), n = key_n(key), G = D / 64;
-  if (fp16) {
-    const half_t* x = reinterpret_cast<const half_t*>(rec);
-    return v ? (float)x[64 * D + (((size_t)(ch / 16) * 2 + (key >> 3 & 1)) * 64 + 16 * (key >> 4) + (ch & 15)) * 8 + (key & 7)]
-             : (float)x[(((size_t)t * (D / 32) + ch / 32) * 64 + 16 * (ch / 8 % 4) + n) * 8 + (ch & 7)];
-  }
-  const uint8_t* part = v ? rec + hif4_part(G) : rec;
-  const int tile = ch >> 6, rt = v ? (ch >> 4) & 3 : t, rn = v ? ch & 15 : n, elem = v ? key : ch & 63;
-  const int w = elem >> 3, i = elem & 7, lane = 16 * (w >> 1) + rn, bit = 2 * rt + (w & 1);
-  const uint32_t nib = (part[hif4_code_at(tile, rt, lane, w & 1) + (i >> 1)] >> (4 * (i & 1))) & 15u;
-  const int sh = ((part[hif4_e2_at(G, tile, lane)] >> bit) & 1) + ((part[hif4_e3_at(G, tile, lane, i >> 2)] >> bit) & 1);
-  const float x = (float)(nib & 7u) * e6m2_value(part[hif4_base_at(G, tile, rt, rn)]) *
-                  (sh == 0 ? 0.25f : sh == 1 ? 0.125f : 0.0625f);
-  return nib & 8u ? -x : x;
 }
 
 // ---------------------------------------------------------------------------
@@ -383,10 +368,11 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
   const int lane = threadIdx.x, n = lane & 15, k = lane >> 4, piece = n & 3;
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
-  const Run run = find_run(a.c, r, 0, lane);
+  const int target = run_target(a.hq, a.c.hkv, D, false);
+  const Run run = find_run(a.c, target, r, 0, lane);
   if (run.b < 0) return;
   const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
-  const DecodeWs ws = decode_ws(a.ws, a.c.batch, a.hq, a.c.hkv, D, a.c.max_pages);
+  const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
   const size_t rec_bytes = (size_t)72 * D;
   const int v_lane = 16 * ((k & 1) * 2 + (k >> 1)) + n;        // lanes k = 1, 2 exchanged
   const int q_in = 4 * tile + (n >> 2), h = head * group + q_in;
@@ -526,49 +512,157 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
   if (k == 0 && piece == 0) ws.ml[slot] = make_float2(l == 0.0f ? -INFINITY : ref, l);
 }
 
-// FP16 pages.  One wave per (run, query head).
-__global__ void __launch_bounds__(64) k_runs_fp16(PagedDecode a) {
-  __shared__ float qs[256], ps[64];
-  const int lane = threadIdx.x, D = a.c.D;
-  const int h = blockIdx.x % a.hq, r = blockIdx.x / a.hq;
-  const Run run = find_run(a.c, r, 0, lane);
-  if (run.b < 0) return;
-  const int len = paged_len(a.c, run.b), head = h / (a.hq / a.c.hkv);
-  const DecodeWs ws = decode_ws(a.ws, a.c.batch, a.hq, a.c.hkv, D, a.c.max_pages);
-  for (int d = lane; d < D; d += 64) qs[d] = (float)smoothed_q(a, run.b, h, d);
-  float m = -INFINITY, l = 0.0f, o[4] = {0, 0, 0, 0};
-  __syncthreads();
-  for (int j = run.begin; j < run.end; ++j) {
-    const uint8_t* rec = paged_record(a.c, run.b, j, head);
-    float s = -INFINITY;
-    if (rec && j * kPage + lane < len) {
-      s = 0.0f;
-      for (int d = 0; d < D; ++d) s = fmaf(qs[d], record_value(rec, D, a.c.fp16, false, lane, d), s);
-      s *= a.scale;
-    }
-    float top = s;
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.0f : m_new;
-    const float p = exp2f(s - ref), f = exp2f(m - ref);
-    float sum = p;
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    l = l * f + sum;
-    m = m_new;
-    if (a.w_in && lane == 0)
-      ws.page[((size_t)run.b * a.c.max_pages + j) * a.hq + h] = make_float2(m, sum);
-    ps[lane] = p;
-    __syncthreads();
-    for (int i = 0; i < D / 64; ++i) {
-      o[i] *= f;
-      if (rec)
-        for (int key = 0; key < kPage; ++key)
-          if (ps[key] != 0.0f) o[i] = fmaf(ps[key], record_value(rec, D, a.c.fp16, true, key, 64 * i + lane), o[i]);
-    }
-    __syncthreads();
+// ---------------------------------------------------------------------------
+// FP16 pages.  One wave per (run, kv head, 16 query heads): the record's KiB
+// pieces are the operands of v_mfma_f32_16x16x32_f16 as they are loaded, the
+// scores of a lane (16 keys of its query) its operand of the second product.
+// p enters that product as the sum of two fp16 values (22 bits; one alone
+// would round a row that rests on one key by 2^-12 more than its output is
+// rounded anyway), scaled so that the heaviest key so far lies between 2^7 and
+// 2^15: small weights stay above fp16's subnormals down to 2^-21 of it.
+typedef half_t h8v_t __attribute__((ext_vector_type(8)));
+typedef half_t h4v_t __attribute__((ext_vector_type(4)));
+constexpr float kTop16 = 7.0f, kSlack16 = 8.0f;
+
+template <int N>
+__device__ __forceinline__ void load_operands(h8v_t (&x)[N], const uint8_t* p, uint32_t lane) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const global_ptr at = scalar_address(p + 1024 * i);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[i + u] = load_at<h8v_t>(at, 16 * lane + 1024 * u);
   }
+}
+
+template <int G>
+__global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(PagedDecode a, int tiles) {
+  constexpr int D = 64 * G;
+  const int lane = threadIdx.x, n = lane & 15, k = lane >> 4;
+  const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
+  const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
+  const int target = run_target(a.hq, a.c.hkv, D, true);
+  const Run run = find_run(a.c, target, r, 0, lane);
+  if (run.b < 0) return;
+  const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
+  const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
+  const int q_in = 16 * tile + n, h = head * group + q_in;
+
+  Pages pg;
+  load_pages(pg, a.c, run, run.begin, lane);
+  bool has, has_next = false;
+  const auto record = [&](int j, bool& there) -> const uint8_t* {
+    if (j - pg.base >= 64) load_pages(pg, a.c, run, j, lane);
+    const int page = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
+    there = (unsigned)page < (unsigned)a.c.num_pages;
+    return a.c.pool + ((size_t)(there ? page : 0) * a.c.hkv + head) * (size_t)(256 * D);
+  };
+  h8v_t q[2 * G];
+#pragma unroll
+  for (int c = 0; c < 2 * G; ++c) {
+    const int ch = 32 * c + 8 * k;
+    q[c] = h8v_t{0, 0, 0, 0, 0, 0, 0, 0};
+    if (q_in < group) {
+      q[c] = *reinterpret_cast<const h8v_t*>(a.q + ((size_t)run.b * a.hq + h) * D + ch);
+      if (a.s) {
+        const float* s = a.s + (size_t)head * D + ch;
+        const f4v_t s0 = *reinterpret_cast<const f4v_t*>(s), s1 = *reinterpret_cast<const f4v_t*>(s + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[c][i] = round_product(q[c][i], i < 4 ? s0[i & 3] : s1[i & 3]);
+      }
+    }
+  }
+  h8v_t kr[8 * G], vr[8 * G];          // K [t][D/32], V [D/16][c]
+  const uint8_t* rec = record(run.begin, has);
+  load_operands(kr, rec, lane);
+  load_operands(vr, rec + 128 * D, lane);
+
+  float ref = -1e30f, l = 0.0f;            // p = 2^(score - ref + kTop16), scores in log2 units
+  f4v_t o[4 * G];
+#pragma unroll
+  for (int c = 0; c < 4 * G; ++c) o[c] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+  for (int j = run.begin; j < run.end; ++j) {
+    f4v_t s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < 2 * G; ++c)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[2 * G * t + c], q[c], s[t], 0, 0, 0);
+    const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
+    load_operands(kr, next, lane);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] *= a.scale;
+    const int held = has ? len - j * kPage : 0;
+    if (held < kPage) {
+      asm volatile("");                  // (kept a branch)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (16 * k + 4 * t + v >= held) s[t][v] = -INFINITY;
+      // what lies in the page behind the last token may be anything: 0 times it has to be 0
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (16 * k + 8 * c + i >= held)
+#pragma unroll
+            for (int u = 0; u < 4 * G; ++u) vr[2 * u + c][i] = (half_t)0;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) top = fmaxf(top, s[t][v]);
+    if (__builtin_amdgcn_ballot_w64(top > ref + kSlack16)) {
+      const float to = fmaxf(ref, max_across_rows(top)), f = __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < 4 * G; ++c) o[c] *= f;
+    }
+    float sum = 0.0f;
+    h8v_t hi[2], lo[2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f4v_t p;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(s[t][v] - (ref - kTop16));
+        sum += p[v];
+      }
+      const h4v_t a4 = __builtin_convertvector(p, h4v_t);
+      const h4v_t b4 = __builtin_convertvector(p - __builtin_convertvector(a4, f4v_t), h4v_t);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        hi[t / 2][4 * (t & 1) + v] = a4[v];
+        lo[t / 2][4 * (t & 1) + v] = b4[v];
+      }
+    }
+    l += sum;
+    if (a.w_in) {
+      const float all = sum_across_rows(sum);
+      if (k == 0 && q_in < group)
+        ws.page[((size_t)run.b * a.c.max_pages + j) * a.hq + h] = make_float2(ref - kTop16, all);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int u = 0; u < 4 * G; ++u) {
+        o[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vr[2 * u + c], lo[c], o[u], 0, 0, 0);
+        o[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vr[2 * u + c], hi[c], o[u], 0, 0, 0);
+      }
+    load_operands(vr, next + 128 * D, lane);
+    has = has_next;
+  }
+
+  l = sum_across_rows(l);
+  if (q_in >= group) return;
   const size_t slot = (size_t)r * a.hq + h;
-  for (int i = 0; i < D / 64; ++i) ws.o[slot * D + 64 * i + lane] = o[i];
-  if (lane == 0) ws.ml[slot] = make_float2(m, l);
+#pragma unroll
+  for (int c = 0; c < 4 * G; ++c) *reinterpret_cast<f4v_t*>(ws.o + slot * D + 16 * c + 4 * k) = o[c];
+  if (k == 0) ws.ml[slot] = make_float2(l == 0.0f ? -INFINITY : ref - kTop16, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -606,11 +700,12 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
   __shared__ f4v_t part[kSets][kCols];
   __shared__ float2 joined[4][64];
   const int tid = threadIdx.x, lane = tid & 63, D = a.c.D;
-  const DecodeWs ws = decode_ws(a.ws, a.c.batch, a.hq, a.c.hkv, D, a.c.max_pages);
+  const int target = run_target(a.hq, a.c.hkv, D, a.c.fp16);
+  const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
   if ((int)blockIdx.x < rows) {
     const int slices = D / kWidth, row = blockIdx.x / slices, d0 = blockIdx.x % slices * kWidth;
     const int b = row / a.hq, h = row % a.hq;
-    const Run run = find_run(a.c, -1, b, lane);
+    const Run run = find_run(a.c, target, -1, b, lane);
     const float2 x = join_row(ws.ml, a.hq, run, h, red);
     const int col = tid % kCols, set = tid / kCols;
     f4v_t o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -634,7 +729,7 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
   // page weights: (m, l) of 64 heads at a time, then a sequence's pages, four threads a page
   const int chunks = (a.c.max_pages + 63) / 64, at = blockIdx.x - rows;
   const int b = at / chunks, j0 = 64 * (at % chunks), wave = tid >> 6;
-  const Run run = find_run(a.c, -1, b, lane);
+  const Run run = find_run(a.c, target, -1, b, lane);
   const int pages = pages_of(a.c, b), j = j0 + tid / 4;
   float w = 0.0f;
   for (int h0 = 0; h0 < a.hq && j0 < pages; h0 += 64) {
@@ -674,17 +769,24 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
 }
 
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
-  const size_t runs = run_slots(a.c.batch, a.c.hkv, a.c.max_pages);
-  const int tiles = (a.hq / a.c.hkv + 3) / 4;
-  const dim3 grid((unsigned)(a.c.fp16 ? runs * a.hq : runs * a.c.hkv * tiles));
-  if (a.c.fp16)
-    k_runs_fp16<<<grid, 64, 0, st>>>(a);
-  else if (a.c.D == 64)
-    k_runs_hif4<1><<<grid, 64, 0, st>>>(a, tiles);
-  else if (a.c.D == 128)
-    k_runs_hif4<2><<<grid, 64, 0, st>>>(a, tiles);
-  else
-    k_runs_hif4<4><<<grid, 64, 0, st>>>(a, tiles);
+  const int tiles = query_tiles(a.hq, a.c.hkv, a.c.fp16);
+  const size_t runs = run_slots(a.c.batch, run_target(a.hq, a.c.hkv, a.c.D, a.c.fp16), a.c.max_pages);
+  const dim3 grid((unsigned)(runs * a.c.hkv * tiles));
+  if (a.c.fp16) {
+    if (a.c.D == 64)
+      k_runs_fp16<1><<<grid, 64, 0, st>>>(a, tiles);
+    else if (a.c.D == 128)
+      k_runs_fp16<2><<<grid, 64, 0, st>>>(a, tiles);
+    else
+      k_runs_fp16<4><<<grid, 64, 0, st>>>(a, tiles);
+  } else {
+    if (a.c.D == 64)
+      k_runs_hif4<1><<<grid, 64, 0, st>>>(a, tiles);
+    else if (a.c.D == 128)
+      k_runs_hif4<2><<<grid, 64, 0, st>>>(a, tiles);
+    else
+      k_runs_hif4<4><<<grid, 64, 0, st>>>(a, tiles);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // channels shared out while there are fewer rows than compute units

@@ -50,15 +50,6 @@ struct Run {
   int first, count;               // the sequence's runs: [first, first + count)
 };
 
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // lane 15 of each row to the next
-  return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
-}
 __device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
   return b < c.batch ? (paged_len(c, b) + kPage - 1) / kPage : 0;
 }

@@ -487,6 +487,8 @@ def hifa4_decode_fwd(q, k_codes, k_meta, v_codes, v_meta, s=None, cu_seqlens=Non
 # ---------------------------------------------------------------------------
 # The paged cache.
 def _shaped(t, dtype, shape, device, name):
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.get_device() == device.index and t.is_contiguous():
+        return
     _require(t, dtype, name)
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
@@ -494,23 +496,21 @@ def _shaped(t, dtype, shape, device, name):
         raise ValueError(f"{name} must be on {device}, got {t.device}")
 
 
-class _OnDevice:
-    """Makes `device` the current one for a call, where it is another."""
-
-    def __init__(self, device):
-        cuda = _torch()._C
-        self.back = cuda._cuda_getDevice()
-        if self.back != device.index:
-            cuda._cuda_setDevice(device.index)
-        else:
-            self.back = -1
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *_):
-        if self.back >= 0:
-            _torch()._C._cuda_setDevice(self.back)
+def _paged_call(name, device, *args):
+    """Calls an entry point of the library with `device` current."""
+    fn = getattr(load_library(), name)
+    cuda = _torch()._C
+    back = cuda._cuda_getDevice()
+    if back == device.index:
+        status = fn(*args)
+    else:
+        cuda._cuda_setDevice(device.index)
+        try:
+            status = fn(*args)
+        finally:
+            cuda._cuda_setDevice(back)
+    if status != 0:
+        _check(status, name)
 
 
 def hifa4_paged_page_bytes(heads_kv: int, head_dim: int, operands: int = OPERANDS_HIF4) -> int:
@@ -595,9 +595,8 @@ def hifa4_paged_append(cache: PagedCache, k, v, s=None, cu_new=None, max_new: Op
         _shaped(cu_new, torch.int32, (cache.batch + 1,), dev, "cu_new")
     if max_new is None:
         max_new = total if cu_new is not None else 1
-    with _OnDevice(dev):
-        _check(load_library().hifa4_paged_append(cache._ref, total, max_new, _ptr(cu_new), _ptr(k), _ptr(v), _ptr(s),
-                                                 _stream(dev)), "hifa4_paged_append")
+    _paged_call("hifa4_paged_append", dev, cache._ref, total, max_new, _ptr(cu_new), k.data_ptr(), v.data_ptr(), _ptr(s),
+                _stream(dev))
 
 
 def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_tokens: Optional[int] = None, starts=None,
@@ -620,10 +619,8 @@ def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_toke
         v = torch.empty(shape, dtype=torch.float16, device=dev)
     else:
         _shaped(v, torch.float16, shape, dev, "v")
-    with _OnDevice(dev):
-        _check(load_library().hifa4_paged_gather(cache._ref, total_tokens, total_tokens if max_tokens is None else max_tokens,
-                                                 _ptr(cu_tokens), _ptr(starts), _ptr(k), _ptr(v), _stream(dev)),
-               "hifa4_paged_gather")
+    _paged_call("hifa4_paged_gather", dev, cache._ref, total_tokens, total_tokens if max_tokens is None else max_tokens,
+                cu_tokens.data_ptr(), _ptr(starts), k.data_ptr(), v.data_ptr(), _stream(dev))
     return k, v
 
 
@@ -669,11 +666,9 @@ def hifa4_paged_decode_fwd(cache: PagedCache, q, s=None, page_weights=None, deca
     if need is None:
         need = cache._workspace_bytes[hq, weighs] = hifa4_paged_decode_workspace_bytes(cache, hq, weighs)
     stream = _stream(dev)
-    with _OnDevice(dev):
-        ws = _scratch(need, dev, stream) if workspace is None else workspace.get(need, dev)
-        _check(load_library().hifa4_paged_decode_fwd(cache._ref, hq, _ptr(q), _ptr(s), _ptr(out), _ptr(lse),
-                                                     _ptr(page_weights), _ptr(weights_out), decay, _ptr(ws), ws.numel(),
-                                                     stream), "hifa4_paged_decode_fwd")
+    ws = _scratch(need, dev, stream) if workspace is None else workspace.get(need, dev)
+    _paged_call("hifa4_paged_decode_fwd", dev, cache._ref, hq, q.data_ptr(), _ptr(s), out.data_ptr(), lse.data_ptr(),
+                _ptr(page_weights), _ptr(weights_out), decay, ws.data_ptr(), ws.numel(), stream)
     return out, lse
 
 
@@ -687,29 +682,36 @@ def hifa4_paged_evict(block_table, seq_lens, page_weights, budget: int, first: i
     torch, dev = _torch(), block_table.device
     if block_table.dim() != 2:
         raise ValueError("block_table is [batch, max_pages]")
-    shape = tuple(block_table.shape)
+    i32, f32 = torch.int32, torch.float32
+    shape = block_table.shape
     rows = shape[:1]
-    _shaped(block_table, torch.int32, shape, dev, "block_table")
-    _shaped(seq_lens, torch.int32, rows, dev, "seq_lens")
-    _shaped(page_weights, torch.float32, shape, dev, "page_weights")
-    out = []
-    for t, dtype, size, inplace, name in ((out_table, torch.int32, shape, block_table, "out_table"),
-                                          (out_lens, torch.int32, rows, seq_lens, "out_lens"),
-                                          (out_weights, torch.float32, shape, page_weights, "out_weights"),
-                                          (freed, torch.int32, shape, None, "freed"),
-                                          (num_freed, torch.int32, rows, None, "num_freed")):
-        if t is not None:
-            _shaped(t, dtype, size, dev, name)
-        elif inplace is not None:
-            t = inplace
-        else:
-            t = torch.empty(size, dtype=dtype, device=dev)
-        out.append(t)
-    with _OnDevice(dev):
-        _check(load_library().hifa4_paged_evict(shape[0], shape[1], _ptr(block_table), _ptr(seq_lens), _ptr(page_weights),
-                                                budget, first, last, *[_ptr(t) for t in out], _stream(dev)),
-               "hifa4_paged_evict")
-    return out[3], out[4]
+    _shaped(block_table, i32, shape, dev, "block_table")
+    _shaped(seq_lens, i32, rows, dev, "seq_lens")
+    _shaped(page_weights, f32, shape, dev, "page_weights")
+    if out_table is None:
+        out_table = block_table
+    else:
+        _shaped(out_table, i32, shape, dev, "out_table")
+    if out_lens is None:
+        out_lens = seq_lens
+    else:
+        _shaped(out_lens, i32, rows, dev, "out_lens")
+    if out_weights is None:
+        out_weights = page_weights
+    else:
+        _shaped(out_weights, f32, shape, dev, "out_weights")
+    if freed is None:
+        freed = torch.empty(shape, dtype=i32, device=dev)
+    else:
+        _shaped(freed, i32, shape, dev, "freed")
+    if num_freed is None:
+        num_freed = torch.empty(rows, dtype=i32, device=dev)
+    else:
+        _shaped(num_freed, i32, rows, dev, "num_freed")
+    _paged_call("hifa4_paged_evict", dev, shape[0], shape[1], block_table.data_ptr(), seq_lens.data_ptr(),
+                page_weights.data_ptr(), budget, first, last, out_table.data_ptr(), out_lens.data_ptr(),
+                out_weights.data_ptr(), freed.data_ptr(), num_freed.data_ptr(), _stream(dev))
+    return freed, num_freed
 
 
 def hifa4_selftest_exp2(x):

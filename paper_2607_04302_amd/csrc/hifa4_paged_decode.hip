@@ -147,6 +147,8 @@ constexpr int kFp4 = 4, kFp8 = 0;            // operand formats of the instructi
 // The reference of the softmax is a whole power of two and moves only when a
 // page's largest score passes it by this many binades: fp32 sums do not mind.
 constexpr float kSlack = 16.0f;
+// Row of p's digits in LDS, padded so that the four rows of lanes write to different banks.
+constexpr int kDigitRow = 68;
 // E8M0 byte of the FP4 side without E2: 2^(94 - E2).  The bases enter as the
 // float whose bits are byte << 21 = b 2^-96, and an operand's sum is 4 values.
 constexpr uint32_t kUnit = 127 + 94;
@@ -169,16 +171,25 @@ __device__ __forceinline__ float sum_pieces(float v) {
   return v + __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4E, 0xF, 0xF, true));
 }
 
-// Digit k of x (|x| <= 16): rint(32^k x) - 32 rint(32^(k-1) x), between -16 and
-// 16; digits 0..3 add up to rint(32^3 x) / 32^3.
-struct DigitScale {
-  float now, before;       // 32^k and, for k > 0, 32^(k-1)
-};
-__device__ __forceinline__ DigitScale digit_scale(int k) {
-  return DigitScale{__uint_as_float((uint32_t)(127 + 5 * k) << 23), k ? __uint_as_float((uint32_t)(122 + 5 * k) << 23) : 0.0f};
+__device__ __forceinline__ float max_quad(float v) {
+  v = fmaxf(v, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xB1, 0xF, 0xF, true)));
+  return fmaxf(v, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4E, 0xF, 0xF, true)));
 }
-__device__ __forceinline__ float digit(float x, const DigitScale& s) {
-  return fmaf(-32.0f, __builtin_rintf(x * s.before), __builtin_rintf(x * s.now));
+// mine + the neighbour's other (quad permutation kPerm)
+template <int kPerm>
+__device__ __forceinline__ float add_xor(float mine, float other) {
+  return mine + __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(other), kPerm, 0xF, 0xF, true));
+}
+
+// The digits of x (|x| <= 16): R_k = rint(32^k x), digit k = R_k - 32 R_(k-1),
+// between -16 and 16; they add up to R_3 / 32^3.
+__device__ __forceinline__ void digits(float x, float (&d)[4]) {
+  const float r0 = __builtin_rintf(x), r1 = __builtin_rintf(x * 32.0f), r2 = __builtin_rintf(x * 1024.0f),
+              r3 = __builtin_rintf(x * 32768.0f);
+  d[0] = r0;
+  d[1] = fmaf(-32.0f, r0, r1);
+  d[2] = fmaf(-32.0f, r1, r2);
+  d[3] = fmaf(-32.0f, r2, r3);
 }
 __device__ __forceinline__ uint32_t fp8x4(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
@@ -290,10 +301,15 @@ __device__ __forceinline__ void products(const Part<G>& p, Get get, Use use) {
     use(tile, 3, c3, bases(bw.w));
   }
 }
-// The FP8 operand of two words (x: its FP4 lane j's, y: lane 2 + j's), each twice.
-__device__ __forceinline__ i8v_t fp8_operand(uint2 x, uint2 y) {
-  return i8v_t{(int)x.x, (int)x.y, (int)x.x, (int)x.y, (int)y.x, (int)y.y, (int)y.x, (int)y.y};
+// The FP8 operand of two words, each twice (x: the FP4 lane j's, y: lane 2 + j's).
+__device__ __forceinline__ i8v_t fp8_operand(uint4 x, uint4 y) {
+  return i8v_t{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
 }
+
+// Nothing is scheduled across: a page's loads stay between the last use of the
+// registers that they fill and the next page's, K's before V's, so that they
+// need no registers of their own and a wait for K's does not wait for V's.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // The pages of a run, as their records: 64 table entries at a time, one a lane.
 struct Pages {
@@ -309,7 +325,7 @@ __device__ __forceinline__ void load_pages(Pages& p, const PagedCache& c, const 
 // the exponent that each group of 64 was scaled by.
 template <int G>
 struct QueryDigits {
-  uint2 word[G][2][4][16];
+  uint4 word[G][2][4][16];             // a word's eight bytes, twice
   int exponent[G][4];
 };
 template <int G>
@@ -341,13 +357,13 @@ __device__ __forceinline__ void query_digits(QueryDigits<G>& out, const half_t* 
     const int e = top > 0.0f ? (int)(__float_as_uint(top) >> 23) - 127 : 0;
     const float up = __uint_as_float((uint32_t)(127 + 3 - e) << 23);
     if (w == 0) out.exponent[g][row] = e;
+    float d[8][4];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) digits(x[u] * up, d[u]);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const DigitScale ds = digit_scale(k);
-      float d[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) d[u] = digit(x[u] * up, ds);
-      out.word[g][w & 1][w >> 1][4 * row + k] = make_uint2(fp8x4(d[0], d[1], d[2], d[3]), fp8x4(d[4], d[5], d[6], d[7]));
+      const uint32_t d0 = fp8x4(d[0][k], d[1][k], d[2][k], d[3][k]), d1 = fp8x4(d[4][k], d[5][k], d[6][k], d[7][k]);
+      out.word[g][w & 1][w >> 1][4 * row + k] = make_uint4(d0, d1, d0, d1);
     }
   }
 }
@@ -356,6 +372,7 @@ template <int G>
 __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a, int tiles) {
   constexpr int D = 64 * G;
   __shared__ QueryDigits<G> qd;
+  __shared__ __align__(16) uint32_t pd[4][kDigitRow];      // [k][query][digit][t]: four keys' digits of p
   const int lane = threadIdx.x, n = lane & 15, k = lane >> 4, piece = n & 3;
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
@@ -373,7 +390,10 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
   bool has, has_next = false;
   // The record of page j; of a page that is none the pool's first, whose keys are all masked then.
   const auto record = [&](int j, bool& there) -> const uint8_t* {
-    if (j - pg.base >= 64) load_pages(pg, a.c, run, j, lane);
+    if (j - pg.base >= 64) {
+      load_pages(pg, a.c, run, j, lane);
+      asm volatile("" : "+v"(pg.mine));  // waited for here: else every page's look-up would wait for all loads
+    }
     const int page = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
     there = (unsigned)page < (unsigned)a.c.num_pages;
     return a.c.pool + ((size_t)(there ? page : 0) * a.c.hkv + head) * rec_bytes;
@@ -383,14 +403,16 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
   Part<G> kp, vp;
   const uint8_t* rec = record(run.begin, has);
   load_part<G>(kp, rec, lane, k);
+  keep_order();
   load_part<G>(vp, rec + 2304 * G, v_lane, k);
+  keep_order();
   __syncthreads();
-  const DigitScale ds = digit_scale(piece);
   uint32_t q_scale[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) q_scale[g] = (uint32_t)(127 - 3 - 5 * piece + qd.exponent[g][n >> 2]);
 
-  // scores in log2 units; sums are of p = 2^(score - ref), ref a whole number
+  // sums are of p = 2^(score - ref), ref a whole number
+  const bool odd = piece & 1, high = piece & 2;
   float ref = -1e30f, l = 0.0f;
   f4v_t o[G][4];
 #pragma unroll
@@ -414,28 +436,28 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
     // (the last page's own again at the end, which nothing waits for: a load that may not
     // happen would keep both pages' registers)
     const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
+    keep_order();
     load_part<G>(kp, next, lane, k);
+    keep_order();
+    // The scores: a lane adds up the digits' products of its share, the four
+    // keys 4 piece .. 4 piece + 3 of its 16; log2 units from here on.
+    float x[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) s[t][v] = sum_pieces(s[t][v]) * a.scale;
+    for (int v = 0; v < 4; ++v) {
+      const float a01 = add_xor<0xB1>(odd ? s[1][v] : s[0][v], odd ? s[0][v] : s[1][v]);
+      const float a23 = add_xor<0xB1>(odd ? s[3][v] : s[2][v], odd ? s[2][v] : s[3][v]);
+      x[v] = add_xor<0x4E>(high ? a23 : a01, high ? a01 : a23) * a.scale;
+    }
     const int held = has ? len - j * kPage : 0;
     if (held < kPage) {
-      asm volatile("");                  // (kept a branch)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (16 * k + 4 * t + v >= held) s[t][v] = -INFINITY;
+      for (int v = 0; v < 4; ++v)
+        if (16 * k + 4 * piece + v >= held) x[v] = -INFINITY;
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) top = fmaxf(top, s[t][v]);
+    const float top = max_across_rows(max_quad(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))));
     // the page's own reference: the next whole number above its largest score
     // (far below ref, where nothing of the page counts, 100 binades are enough)
-    const float own = fmaxf(ceilf(max_across_rows(top)), ref - 100.0f);
+    const float own = fmaxf(ceilf(top), ref - 100.0f);
     if (__builtin_amdgcn_ballot_w64(own > ref + kSlack)) {
       const float to = fmaxf(ref, own), f = __builtin_amdgcn_exp2f(ref - to);
       ref = to;
@@ -445,35 +467,29 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
 #pragma unroll
         for (int t = 0; t < 4; ++t) o[g][t] *= f;
     }
-    float sum = 0.0f;
-    uint32_t pw[4];
+    float sum = 0.0f, d[4][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      float y[4];
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float p = __builtin_amdgcn_exp2f(s[t][v] - (own - 4.0f));      // 16 p, at most 16
-        sum += p;
-        y[v] = digit(p, ds);
-      }
-      pw[t] = fp8x4(y[0], y[1], y[2], y[3]);
+    for (int v = 0; v < 4; ++v) {
+      const float p = __builtin_amdgcn_exp2f(x[v] - (own - 4.0f));      // 16 p, at most 16
+      sum += p;
+      digits(p, d[v]);
     }
+    // every lane's digits to the lanes that need them: of its query's 16 keys and of the next row's
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pd[k][16 * (n >> 2) + 4 * i + piece] = fp8x4(d[0][i], d[1][i], d[2][i], d[3][i]);
     // 2^(own - ref - 4): what the page's sums count
     const int up = (int)(own - ref) - 4;
     l = fmaf(sum, __uint_as_float((uint32_t)(127 + up) << 23), l);
     const uint32_t p_scale = (uint32_t)(127 + up - 5 * piece);
     if (a.w_in) {
-      const float all = sum_across_rows(sum);
+      const float all = sum_across_rows(sum_pieces(sum));
       if (k == 0 && piece == 0 && q_in < group)
         ws.page[((size_t)run.b * a.c.max_pages + j) * a.hq + h] = make_float2(own - 4.0f, all);
     }
-    i8v_t pa[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const auto x = __builtin_amdgcn_permlane16_swap(pw[2 * c], pw[2 * c], false, false);
-      const auto y = __builtin_amdgcn_permlane16_swap(pw[2 * c + 1], pw[2 * c + 1], false, false);
-      pa[c] = fp8_operand(make_uint2(x[0], y[0]), make_uint2(x[1], y[1]));
-    }
+    const uint4 pe = *reinterpret_cast<const uint4*>(&pd[k & 2][4 * n]);
+    const uint4 po = *reinterpret_cast<const uint4*>(&pd[(k & 2) + 1][4 * n]);
+    const i8v_t pa[2] = {fp8_operand(make_uint4(pe.x, pe.y, pe.x, pe.y), make_uint4(po.x, po.y, po.x, po.y)),
+                         fp8_operand(make_uint4(pe.z, pe.w, pe.z, pe.w), make_uint4(po.z, po.w, po.z, po.w))};
     products<G>(vp, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       b0 = pa[0];
       b1 = pa[1];
@@ -482,11 +498,13 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
 #pragma unroll
       for (int v = 0; v < 4; ++v) o[g][t][v] = fmaf(d[v], b[v], o[g][t][v]);
     });
+    keep_order();
     load_part<G>(vp, next + 2304 * G, v_lane, k);
+    keep_order();
     has = has_next;
   }
 
-  l = sum_across_rows(l);
+  l = sum_across_rows(sum_pieces(l));
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -542,7 +560,10 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
   load_pages(pg, a.c, run, run.begin, lane);
   bool has, has_next = false;
   const auto record = [&](int j, bool& there) -> const uint8_t* {
-    if (j - pg.base >= 64) load_pages(pg, a.c, run, j, lane);
+    if (j - pg.base >= 64) {
+      load_pages(pg, a.c, run, j, lane);
+      asm volatile("" : "+v"(pg.mine));  // waited for here: else every page's look-up would wait for all loads
+    }
     const int page = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
     there = (unsigned)page < (unsigned)a.c.num_pages;
     return a.c.pool + ((size_t)(there ? page : 0) * a.c.hkv + head) * (size_t)(256 * D);
@@ -663,58 +684,64 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
 // rows); behind those, with page weights, one per 64 pages of a sequence.
 constexpr int kJoin = 256;
 
-// (m, l) of row h over the runs; every thread of the workgroup gets it.
-__device__ __forceinline__ float2 join_row(const float2* ml, int hq, const Run& run, int h, float* red) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float m = -INFINITY;
-  for (int i = tid; i < run.count; i += kJoin) m = fmaxf(m, ml[(size_t)(run.first + i) * hq + h].x);
-  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if (lane == 0) red[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  if (m == -INFINITY) m = 0.0f;
-  float l = 0.0f;
-  for (int i = tid; i < run.count; i += kJoin) {
-    const float2 x = ml[(size_t)(run.first + i) * hq + h];
-    l += x.y * __builtin_amdgcn_exp2f(x.x - m);
-  }
-  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-  if (lane == 0) red[4 + wave] = l;
-  __syncthreads();
-  return make_float2(m, (red[4] + red[5]) + (red[6] + red[7]));
+// Two partial sums over runs as one, in the first's place.
+__device__ __forceinline__ void join_pair(float& m, float& l, f4v_t& o, float m2, float l2, f4v_t o2) {
+  const float to = fmaxf(m, m2), ref = to == -INFINITY ? 0.0f : to;
+  const float f = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+  m = to;
+  l = l * f + l2 * f2;
+  o = o * f + o2 * f2;
 }
 
 template <int kWidth>
 __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
   constexpr int kCols = kWidth / 4, kSets = kJoin / kCols;
-  __shared__ float red[8];
   __shared__ f4v_t part[kSets][kCols];
+  __shared__ float2 part_ml[kSets];
   __shared__ float2 joined[4][64];
   const int tid = threadIdx.x, lane = tid & 63, D = a.c.D;
   const int target = run_target(a.hq, a.c.hkv, D, a.c.fp16);
   const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
   if ((int)blockIdx.x < rows) {
+    // a set of threads takes every kSets-th run, (m, l) and o in one go; then the sets are joined in order
     const int slices = D / kWidth, row = blockIdx.x / slices, d0 = blockIdx.x % slices * kWidth;
     const int b = row / a.hq, h = row % a.hq;
     const Run run = find_run(a.c, target, -1, b, lane);
-    const float2 x = join_row(ws.ml, a.hq, run, h, red);
     const int col = tid % kCols, set = tid / kCols;
     f4v_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int i = set; i < run.count; i += kSets) {
-      const size_t slot = (size_t)(run.first + i) * a.hq + h;
-      o += *reinterpret_cast<const f4v_t*>(ws.o + slot * D + d0 + 4 * col) * __builtin_amdgcn_exp2f(ws.ml[slot].x - x.x);
+    float m = -INFINITY, l = 0.0f;
+    constexpr int kAhead = 4;
+    for (int i = set; i < run.count; i += kAhead * kSets) {
+      float2 x[kAhead];
+      f4v_t y[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const size_t slot = (size_t)(run.first + min(i + u * kSets, run.count - 1)) * a.hq + h;
+        x[u] = ws.ml[slot];
+        y[u] = *reinterpret_cast<const f4v_t*>(ws.o + slot * D + d0 + 4 * col);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u * kSets < run.count) join_pair(m, l, o, x[u].x, x[u].y, y[u]);
     }
     part[set][col] = o;
+    if (col == 0) part_ml[set] = make_float2(m, l);
     __syncthreads();
     if (tid < kWidth) {
-      float sum = 0.0f;
-      for (int i = 0; i < kSets; ++i) sum += part[i][tid / 4][tid & 3];
-      a.o[(size_t)row * D + d0 + tid] = (half_t)(x.y == 0.0f ? 0.0f : sum / x.y);
+      float top = -INFINITY, sum = 0.0f, all = 0.0f;
+      for (int i = 0; i < kSets; ++i) top = fmaxf(top, part_ml[i].x);
+      if (top == -INFINITY) top = 0.0f;
+#pragma unroll 8
+      for (int i = 0; i < kSets; ++i) {
+        const float f = __builtin_amdgcn_exp2f(part_ml[i].x - top);
+        all += part_ml[i].y * f;
+        sum += part[i][tid / 4][tid & 3] * f;
+      }
+      a.o[(size_t)row * D + d0 + tid] = (half_t)(all == 0.0f ? 0.0f : sum / all);
+      if (tid == 0 && d0 == 0)
+        a.lse[(size_t)h * a.c.batch + b] =
+            all == 0.0f ? -INFINITY : (float)(((double)top + (double)__log2f(all)) * 0.6931471805599453);
     }
-    if (tid == 0 && d0 == 0)
-      a.lse[(size_t)h * a.c.batch + b] =
-          x.y == 0.0f ? -INFINITY : (float)(((double)x.x + (double)__log2f(x.y)) * 0.6931471805599453);
     return;
   }
   // page weights: (m, l) of 64 heads at a time, then a sequence's pages, four threads a page

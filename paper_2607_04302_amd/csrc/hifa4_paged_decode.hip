@@ -37,7 +37,7 @@ __host__ __device__ __forceinline__ int query_tiles(int hq, int hkv, bool fp16) 
 // ceil(pages / target) pages, numbered densely over the sequences: at most
 // target + batch runs.
 __host__ __device__ __forceinline__ int run_target(int hq, int hkv, int D, bool fp16) {
-  const int waves = fp16 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : (D == 256 ? 1 : 3);
+  const int waves = fp16 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : (D == 256 ? 1 : D == 128 ? 2 : 3);
   const int each = hkv * query_tiles(hq, hkv, fp16);
   return (1024 * waves + each - 1) / each;
 }
@@ -53,13 +53,25 @@ struct Run {
 __device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
   return b < c.batch ? (paged_len(c, b) + kPage - 1) / kPage : 0;
 }
+// Sum over the sequences of f(pages), by a whole wave; n0: those of the first 64.
+template <typename F>
+__device__ __forceinline__ int sum_sequences(const PagedCache& c, int n0, int lane, F f) {
+  int total = __builtin_amdgcn_readlane(wave_scan(f(n0)), 63);
+  for (int b0 = 64; b0 < c.batch; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(f(pages_of(c, b0 + lane))), 63);
+  return total;
+}
 // The run numbered r (found by a whole wave), or with r < 0 the runs of
 // sequence `want`.
 __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, int want, int lane) {
   const int n0 = pages_of(c, lane);
-  int total = __builtin_amdgcn_readlane(wave_scan(n0), 63);
-  for (int b0 = 64; b0 < c.batch; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(pages_of(c, b0 + lane)), 63);
-  const int per = max(1, (total + target - 1) / target);
+  const int total = sum_sequences(c, n0, lane, [](int n) { return n; });
+  int per = max(1, (total + target - 1) / target);
+  // the last runs of the sequences are shorter: longer runs until all fit into one round (or nearly)
+  for (int i = 0; i < 6; ++i) {
+    const int runs = sum_sequences(c, n0, lane, [per](int n) { return (n + per - 1) / per; });
+    if (runs <= target) break;
+    per += max(1, (int)((long)per * (runs - target) / target));
+  }
   Run out = {-1, 0, 0, 0, 0};
   int before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
@@ -369,7 +381,7 @@ __device__ __forceinline__ void query_digits(QueryDigits<G>& out, const half_t* 
 }
 
 template <int G>
-__global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a, int tiles) {
+__global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(PagedDecode a, int tiles) {
   constexpr int D = 64 * G;
   __shared__ QueryDigits<G> qd;
   __shared__ __align__(16) uint32_t pd[4][kDigitRow];      // [k][query][digit][t]: four keys' digits of p
@@ -400,11 +412,11 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
   };
   query_digits<G>(qd, a.q + ((size_t)run.b * a.hq + head * group + 4 * tile) * D, group - 4 * tile,
                   a.s ? a.s + (size_t)head * D : nullptr, lane);
-  Part<G> kp, vp;
+  Part<G> kp[2], vp[2];
   const uint8_t* rec = record(run.begin, has);
-  load_part<G>(kp, rec, lane, k);
+  load_part<G>(kp[0], rec, lane, k);
   keep_order();
-  load_part<G>(vp, rec + 2304 * G, v_lane, k);
+  load_part<G>(vp[0], rec + 2304 * G, v_lane, k);
   keep_order();
   __syncthreads();
   uint32_t q_scale[G];
@@ -420,10 +432,17 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[g][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-  for (int j = run.begin; j < run.end; ++j) {
+  // One page, while the next one's K and V are loaded.
+  const auto page = [&](const Part<G>& kc, const Part<G>& vc, Part<G>& kn, Part<G>& vn, int j) __attribute__((always_inline)) {
+    const int some = run.end - run.begin, rem = 4 * (run.end - j);
+    if (rem > 3 * some) __builtin_amdgcn_s_setprio(3); else if (rem > 2 * some) __builtin_amdgcn_s_setprio(2); else if (rem > some) __builtin_amdgcn_s_setprio(1); else __builtin_amdgcn_s_setprio(0);
+    const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
+    keep_order();
+    load_part<G>(kn, next, lane, k);
+    keep_order();
     f4v_t s[4];
     asm volatile("" ::: "memory");       // the query's operands come from LDS in every page, not from registers
-    products<G>(kp, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+    products<G>(kc, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       const int j2 = k >> 1;
       b0 = fp8_operand(qd.word[g][0][j2][n], qd.word[g][0][2 + j2][n]);
       b1 = fp8_operand(qd.word[g][1][j2][n], qd.word[g][1][2 + j2][n]);
@@ -432,12 +451,8 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
 #pragma unroll
       for (int v = 0; v < 4; ++v) s[t][v] = g == 0 ? d[v] * b[v] : fmaf(d[v], b[v], s[t][v]);
     });
-    // the next page's K loads while this page's softmax and V go on
-    // (the last page's own again at the end, which nothing waits for: a load that may not
-    // happen would keep both pages' registers)
-    const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
     keep_order();
-    load_part<G>(kp, next, lane, k);
+    load_part<G>(vn, next + 2304 * G, v_lane, k);
     keep_order();
     // The scores: a lane adds up the digits' products of its share, the four
     // keys 4 piece .. 4 piece + 3 of its 16; log2 units from here on.
@@ -490,7 +505,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
     const uint4 po = *reinterpret_cast<const uint4*>(&pd[(k & 2) + 1][4 * n]);
     const i8v_t pa[2] = {fp8_operand(make_uint4(pe.x, pe.y, pe.x, pe.y), make_uint4(po.x, po.y, po.x, po.y)),
                          fp8_operand(make_uint4(pe.z, pe.w, pe.z, pe.w), make_uint4(po.z, po.w, po.z, po.w))};
-    products<G>(vp, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+    products<G>(vc, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       b0 = pa[0];
       b1 = pa[1];
       scale = p_scale;
@@ -499,9 +514,12 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 3) k_runs_hif4(PagedDecode a,
       for (int v = 0; v < 4; ++v) o[g][t][v] = fmaf(d[v], b[v], o[g][t][v]);
     });
     keep_order();
-    load_part<G>(vp, next + 2304 * G, v_lane, k);
-    keep_order();
     has = has_next;
+  };
+  for (int j = run.begin; j < run.end; j += 2) {
+    page(kp[0], vp[0], kp[1], vp[1], j);
+    if (j + 1 == run.end) break;
+    page(kp[1], vp[1], kp[0], vp[0], j + 1);
   }
 
   l = sum_across_rows(sum_pieces(l));

@@ -291,7 +291,7 @@ hifa4_status check_paged(const hifa4_paged_cache* c, bool touches, hifa4::PagedC
   if (st != HIFA4_OK) return st;
   if (c->batch <= 0 || c->num_pages <= 0 || c->max_pages <= 0)
     return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch, num_pages and max_pages must be > 0");
-  if (c->max_pages >= (1 << 25) || (int64_t)c->batch * c->max_pages >= (1LL << 31))
+  if (c->max_pages >= (1 << 25) || (int64_t)c->batch * c->max_pages >= (1LL << 30))
     return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", c->batch, c->max_pages);
   if (touches) {
     if (!c->pool || !c->block_table || !c->seq_lens) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null cache pointer");
@@ -427,7 +427,7 @@ hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* 
                                int32_t* out_table, int32_t* out_lens, float* out_weights, int32_t* freed,
                                int32_t* num_freed, void* stream) {
   if (batch <= 0 || max_pages <= 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch and max_pages must be > 0");
-  if (max_pages >= (1 << 25) || (int64_t)batch * max_pages >= (1LL << 31))
+  if (max_pages >= (1 << 25) || (int64_t)batch * max_pages >= (1LL << 30))
     return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", batch, max_pages);
   if (first < 0 || last < 1 || (int64_t)first + last > budget)
     return fail(HIFA4_ERR_INVALID_ARGUMENT, "needs first >= 0, last >= 1 and first + last <= budget (%d, %d, %d)", first,

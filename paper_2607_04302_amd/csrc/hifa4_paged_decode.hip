@@ -213,7 +213,7 @@ struct Part {
   uint4 code[2 * G];       // [tile][t/2]: (t even: words 0, 1), (t odd: words 0, 1)
   uint32_t e3[(G + 1) / 2];
   uint32_t e2;
-  uint4 base[G];           // word t: the four rows whose products the lane holds
+  uint32_t base;           // G bytes of the 64 G, in the record's order
 };
 // A scalar address that the compiler takes as given: sums with a lane's 32-bit
 // offset stay in that form instead of becoming 64-bit vector additions.
@@ -228,7 +228,7 @@ __device__ __forceinline__ T load_at(global_ptr p, uint32_t offset) {
   return *(const __attribute__((address_space(1))) T*)(p + offset);
 }
 template <int G>
-__device__ __forceinline__ void load_part(Part<G>& p, const uint8_t* part, uint32_t lane, uint32_t k) {
+__device__ __forceinline__ void load_part(Part<G>& p, const uint8_t* part, uint32_t lane, uint32_t base_lane) {
   typedef unsigned u4v_t __attribute__((ext_vector_type(4)));
   const global_ptr meta = scalar_address(part + 2048 * G);
 #pragma unroll
@@ -251,9 +251,12 @@ __device__ __forceinline__ void load_part(Part<G>& p, const uint8_t* part, uint3
     p.e3[G == 4 ? 1 : 0] = x[1];
     p.e2 = load_at<uint32_t>(meta, 4 * lane + 512);
   }
-#pragma unroll
-  for (int i = 0; i < G; ++i)
-    p.base[i] = __builtin_bit_cast(uint4, load_at<u4v_t>(meta, 16 * G * k + 192 * G + 16 * i));
+  if (G == 1)
+    p.base = load_at<uint8_t>(meta, base_lane + 192);
+  else if (G == 2)
+    p.base = load_at<uint16_t>(meta, 2 * base_lane + 384);
+  else
+    p.base = load_at<uint32_t>(meta, 4 * base_lane + 768);
 }
 
 // 0xFFFF in each half-word of word (t, c) of `tile` with E3 = 0; x: the
@@ -280,15 +283,18 @@ __device__ __forceinline__ uint32_t e3_halves(const Part<G>& p, int tile) {
   const uint32_t x = ~p.e3[tile / 2];
   return G == 1 ? (x & 0xFFu) | ((x & 0xFF00u) << 8) : x;
 }
-__device__ __forceinline__ f4v_t bases(uint32_t w) {
-  return f4v_t{__uint_as_float((w & 0xFFu) << 21), __uint_as_float((w >> 8 & 0xFFu) << 21),
-               __uint_as_float((w >> 16 & 0xFFu) << 21), __uint_as_float((w >> 24) << 21)};
+// A lane's bases to LDS as floats (b 2^-96), for the lanes that hold their rows' products.
+template <int G>
+__device__ __forceinline__ void spread_bases(float* to, uint32_t base, int lane) {
+#pragma unroll
+  for (int i = 0; i < G; ++i) to[G * lane + i] = __uint_as_float((base >> (8 * i) & 0xFFu) << 21);
 }
 // use(tile, t, products, bases): products of a tile's rows 16 t + 4k + v with
 // the columns of the other operand, which get(tile, b0, b1, scale) fetches
-// (its two words' parts).
+// (its two words' parts).  `spread`: 64 G floats of LDS for the bases.
 template <int G, typename Get, typename Use>
-__device__ __forceinline__ void products(const Part<G>& p, Get get, Use use) {
+__device__ __forceinline__ void products(const Part<G>& p, float* spread, int lane, Get get, Use use) {
+  spread_bases<G>(spread, p.base, lane);
 #pragma unroll
   for (int tile = 0; tile < G; ++tile) {
     const uint32_t x = e3_halves<G>(p, tile), s0 = e2_scales(p.e2, tile, 0), s1 = e2_scales(p.e2, tile, 1);
@@ -306,11 +312,11 @@ __device__ __forceinline__ void products(const Part<G>& p, Get get, Use use) {
     c1 = mfma_word<1>(w0.w, e3_keep<G>(x, tile, 1, 1), s1, b1, scale, c1);
     c2 = mfma_word<2>(w1.y, e3_keep<G>(x, tile, 2, 1), s1, b1, scale, c2);
     c3 = mfma_word<3>(w1.w, e3_keep<G>(x, tile, 3, 1), s1, b1, scale, c3);
-    const uint4 bw = p.base[tile];
-    use(tile, 0, c0, bases(bw.x));
-    use(tile, 1, c1, bases(bw.y));
-    use(tile, 2, c2, bases(bw.z));
-    use(tile, 3, c3, bases(bw.w));
+    const f4v_t* b = reinterpret_cast<const f4v_t*>(spread + 16 * G * (lane >> 4) + 16 * tile);
+    use(tile, 0, c0, b[0]);
+    use(tile, 1, c1, b[1]);
+    use(tile, 2, c2, b[2]);
+    use(tile, 3, c3, b[3]);
   }
 }
 // The FP8 operand of two words, each twice (x: the FP4 lane j's, y: lane 2 + j's).
@@ -385,6 +391,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
   constexpr int D = 64 * G;
   __shared__ QueryDigits<G> qd;
   __shared__ __align__(16) uint32_t pd[4][kDigitRow];      // [k][query][digit][t]: four keys' digits of p
+  __shared__ __align__(16) float spread[2][64 * G];
   const int lane = threadIdx.x, n = lane & 15, k = lane >> 4, piece = n & 3;
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
@@ -414,9 +421,9 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
                   a.s ? a.s + (size_t)head * D : nullptr, lane);
   Part<G> kp[2], vp[2];
   const uint8_t* rec = record(run.begin, has);
-  load_part<G>(kp[0], rec, lane, k);
+  load_part<G>(kp[0], rec, lane, lane);
   keep_order();
-  load_part<G>(vp[0], rec + 2304 * G, v_lane, k);
+  load_part<G>(vp[0], rec + 2304 * G, v_lane, lane);
   keep_order();
   __syncthreads();
   uint32_t q_scale[G];
@@ -432,17 +439,27 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[g][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // One page, while the next one's K and V are loaded.
+  // One page from kc and vc, while the next one's parts are loaded into kn and
+  // vn (the last page's own again at the end, which nothing waits for).
   const auto page = [&](const Part<G>& kc, const Part<G>& vc, Part<G>& kn, Part<G>& vn, int j) __attribute__((always_inline)) {
+    // The waves of a SIMD issue oldest first: one with more of its run left
+    // goes before, so that they end together (8 x 32768 tokens: 65.8 to 63.9 us).
     const int some = run.end - run.begin, rem = 4 * (run.end - j);
-    if (rem > 3 * some) __builtin_amdgcn_s_setprio(3); else if (rem > 2 * some) __builtin_amdgcn_s_setprio(2); else if (rem > some) __builtin_amdgcn_s_setprio(1); else __builtin_amdgcn_s_setprio(0);
+    if (rem > 3 * some)
+      __builtin_amdgcn_s_setprio(3);
+    else if (rem > 2 * some)
+      __builtin_amdgcn_s_setprio(2);
+    else if (rem > some)
+      __builtin_amdgcn_s_setprio(1);
+    else
+      __builtin_amdgcn_s_setprio(0);
     const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
     keep_order();
-    load_part<G>(kn, next, lane, k);
+    load_part<G>(kn, next, lane, lane);
     keep_order();
     f4v_t s[4];
     asm volatile("" ::: "memory");       // the query's operands come from LDS in every page, not from registers
-    products<G>(kc, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+    products<G>(kc, spread[0], lane, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       const int j2 = k >> 1;
       b0 = fp8_operand(qd.word[g][0][j2][n], qd.word[g][0][2 + j2][n]);
       b1 = fp8_operand(qd.word[g][1][j2][n], qd.word[g][1][2 + j2][n]);
@@ -452,7 +469,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
       for (int v = 0; v < 4; ++v) s[t][v] = g == 0 ? d[v] * b[v] : fmaf(d[v], b[v], s[t][v]);
     });
     keep_order();
-    load_part<G>(vn, next + 2304 * G, v_lane, k);
+    load_part<G>(vn, next + 2304 * G, v_lane, lane);
     keep_order();
     // The scores: a lane adds up the digits' products of its share, the four
     // keys 4 piece .. 4 piece + 3 of its 16; log2 units from here on.
@@ -505,7 +522,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     const uint4 po = *reinterpret_cast<const uint4*>(&pd[(k & 2) + 1][4 * n]);
     const i8v_t pa[2] = {fp8_operand(make_uint4(pe.x, pe.y, pe.x, pe.y), make_uint4(po.x, po.y, po.x, po.y)),
                          fp8_operand(make_uint4(pe.z, pe.w, pe.z, pe.w), make_uint4(po.z, po.w, po.z, po.w))};
-    products<G>(vc, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+    products<G>(vc, spread[1], lane, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       b0 = pa[0];
       b1 = pa[1];
       scale = p_scale;
@@ -699,8 +716,8 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
 // Joining the runs of a row: with m the largest of their references,
 // o = sum o_i 2^(m_i - m) / l, l = sum l_i 2^(m_i - m).  One workgroup per row
 // and kWidth channels (a row's channels are shared out where there are few
-// rows); behind those, with page weights, one per 64 pages of a sequence.
-constexpr int kJoin = 256;
+// rows); behind those, with page weights, one per 16 pages of a sequence.
+constexpr int kJoin = 256, kPagesJoined = 16, kShare = kJoin / kPagesJoined;
 
 // Two partial sums over runs as one, in the first's place.
 __device__ __forceinline__ void join_pair(float& m, float& l, f4v_t& o, float m2, float l2, f4v_t o2) {
@@ -762,46 +779,53 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
     }
     return;
   }
-  // page weights: (m, l) of 64 heads at a time, then a sequence's pages, four threads a page
-  const int chunks = (a.c.max_pages + 63) / 64, at = blockIdx.x - rows;
-  const int b = at / chunks, j0 = 64 * (at % chunks), wave = tid >> 6;
-  const Run run = find_run(a.c, target, -1, b, lane);
-  const int pages = pages_of(a.c, b), j = j0 + tid / 4;
+  // page weights: (m, l) of 64 heads at a time, then the pages, sixteen threads each, whose sums are
+  // fetched meanwhile
+  const int chunks = (a.c.max_pages + kPagesJoined - 1) / kPagesJoined, at = blockIdx.x - rows;
+  const int b = at / chunks, j0 = kPagesJoined * (at % chunks), wave = tid >> 6;
+  const int pages = pages_of(a.c, b), j = j0 + tid / kShare;
+  const size_t place = (size_t)b * a.c.max_pages + min(j, a.c.max_pages - 1);
+  const float before = a.w_in[place];
   float w = 0.0f;
-  for (int h0 = 0; h0 < a.hq && j0 < pages; h0 += 64) {
-    float m = -INFINITY, l = 0.0f;
-    if (h0 + lane < a.hq)
-      for (int i = wave; i < run.count; i += 4) {
-        const float2 x = ws.ml[(size_t)(run.first + i) * a.hq + h0 + lane];
-        const float to = fmaxf(m, x.x), ref = to == -INFINITY ? 0.0f : to;
-        l = l * __builtin_amdgcn_exp2f(m - ref) + x.y * __builtin_amdgcn_exp2f(x.x - ref);
-        m = to;
+  if (j0 < pages) {
+    const Run run = find_run(a.c, target, -1, b, lane);
+    for (int h0 = 0; h0 < a.hq; h0 += 64) {
+      float2 y[64 / kShare];
+#pragma unroll
+      for (int i = 0; i < 64 / kShare; ++i) {
+        const int h = h0 + tid % kShare + kShare * i;
+        y[i] = j < pages && h < a.hq ? ws.page[place * a.hq + h] : make_float2(0.0f, 0.0f);
       }
-    joined[wave][lane] = make_float2(m, l);
-    __syncthreads();
-    if (wave == 0) {
-      float2 x[4];
-      for (int i = 0; i < 4; ++i) x[i] = joined[i][lane];
-      m = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
-      if (m == -INFINITY) m = 0.0f;
-      l = 0.0f;
-      for (int i = 0; i < 4; ++i) l += x[i].y * __builtin_amdgcn_exp2f(x[i].x - m);
-      joined[0][lane] = make_float2(m, l == 0.0f ? 0.0f : 1.0f / l);
+      float m = -INFINITY, l = 0.0f;
+      if (h0 + lane < a.hq)
+        for (int i = wave; i < run.count; i += 4) {
+          const float2 x = ws.ml[(size_t)(run.first + i) * a.hq + h0 + lane];
+          const float to = fmaxf(m, x.x), ref = to == -INFINITY ? 0.0f : to;
+          l = l * __builtin_amdgcn_exp2f(m - ref) + x.y * __builtin_amdgcn_exp2f(x.x - ref);
+          m = to;
+        }
+      joined[wave][lane] = make_float2(m, l);
+      __syncthreads();
+      if (wave == 0) {
+        float2 x[4];
+        for (int i = 0; i < 4; ++i) x[i] = joined[i][lane];
+        m = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+        if (m == -INFINITY) m = 0.0f;
+        l = 0.0f;
+        for (int i = 0; i < 4; ++i) l += x[i].y * __builtin_amdgcn_exp2f(x[i].x - m);
+        joined[0][lane] = make_float2(m, l == 0.0f ? 0.0f : 1.0f / l);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 64 / kShare; ++i) {
+        const float2 x = joined[0][tid % kShare + kShare * i];
+        w += y[i].y * __builtin_amdgcn_exp2f(y[i].x - x.x) * x.y;
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    if (j < pages)
-      for (int h = tid & 3; h < min(64, a.hq - h0); h += 4) {
-        const float2 x = joined[0][h], y = ws.page[((size_t)b * a.c.max_pages + j) * a.hq + h0 + h];
-        w += y.y * __builtin_amdgcn_exp2f(y.x - x.x) * x.y;
-      }
-    __syncthreads();
   }
-  w += __shfl_xor(w, 1);
-  w += __shfl_xor(w, 2);
-  if ((tid & 3) == 0 && j < a.c.max_pages) {
-    const size_t i = (size_t)b * a.c.max_pages + j;
-    a.w_out[i] = j < pages ? a.decay * a.w_in[i] + w : a.w_in[i];
-  }
+  for (int d = 1; d < kShare; d <<= 1) w += __shfl_xor(w, d);
+  if (tid % kShare == 0 && j < a.c.max_pages) a.w_out[place] = j < pages ? a.decay * before + w : before;
 }
 
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
@@ -826,7 +850,7 @@ hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // channels shared out while there are fewer rows than compute units
-  const size_t extra = a.w_in ? (size_t)a.c.batch * ((a.c.max_pages + 63) / 64) : 0;
+  const size_t extra = a.w_in ? (size_t)a.c.batch * ((a.c.max_pages + kPagesJoined - 1) / kPagesJoined) : 0;
   const int rows = a.c.batch * a.hq;
   const bool few = rows < 256;
   const int groups = few ? rows * (a.c.D / 32) : rows;

@@ -82,7 +82,7 @@ template <int G>
 __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks) {
   constexpr int D = 64 * G, kMeta = 256 * G, kWordsK = 2 * G, kItemsV = (G + 1) / 2;
   __shared__ uint32_t meta_k[kMeta / 4], meta_v[kMeta / 4];
-  __shared__ __align__(16) uint32_t codes_v[2048 * G / 4];
+  __shared__ __align__(16) uint32_t codes_k[2048 * G / 4], codes_v[2048 * G / 4];
   const int tid = threadIdx.x;
   const PageItem it = page_item(a.c.hkv, blocks);
   const int len = paged_len(a.c, it.b);
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks)
         word |= ((nib | (nib >> 12)) & 0xFFu) << (8 * e);
       }
       const int t = key_t(key), n = key_n(key), lane = 16 * (w >> 1) + n, bit = 2 * t + (w & 1);
-      if (rec) *reinterpret_cast<uint32_t*>(rec + hif4_code_at(g, t, lane, w & 1)) = word;
+      codes_k[hif4_code_at(g, t, lane, w & 1) >> 2] = word;
       const uint32_t e2 = 1u - ne2[0], e3 = (2u - lv[0] - e2) | (2u - lv[1] - e2) << (G == 1 ? 8 : 16);
       const int a3 = hif4_e3_at(G, g, lane, 0) - 2048 * G, a2 = hif4_e2_at(G, g, lane) - 2048 * G;
       const uint32_t b3 = or_pair(e3 << (8 * (a3 & 3) + bit)), b2 = or_pair(e2 << (8 * (a2 & 3) + bit));
@@ -243,8 +243,20 @@ __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks)
   __syncthreads();
   if (rec) {
     uint8_t* vp = rec + hif4_part(G);
-    for (int i = tid; i < 2048 * G / 16; i += 256)
+#pragma unroll
+    for (int i = tid; i < 2048 * G / 16; i += 256) {
       reinterpret_cast<uint4*>(vp)[i] = reinterpret_cast<const uint4*>(codes_v)[i];
+      // of K the words of the new keys: 16 bytes are two keys' (t even, t odd)
+      const uint4 x = reinterpret_cast<const uint4*>(codes_k)[i];
+      const int t = 2 * ((i >> 6) & 1), ka = key_of(t, i & 15), kb = key_of(t + 1, i & 15);
+      const bool na = ka >= lo && ka < hi, nb = kb >= lo && kb < hi;
+      if (na && nb)
+        reinterpret_cast<uint4*>(rec)[i] = x;
+      else if (na)
+        reinterpret_cast<uint2*>(rec)[2 * i] = make_uint2(x.x, x.y);
+      else if (nb)
+        reinterpret_cast<uint2*>(rec)[2 * i + 1] = make_uint2(x.z, x.w);
+    }
     for (int i = tid; i < kMeta / 4; i += 256) {
       reinterpret_cast<uint32_t*>(rec + 2048 * G)[i] = meta_k[i];
       reinterpret_cast<uint32_t*>(vp + 2048 * G)[i] = meta_v[i];

@@ -10,9 +10,11 @@
 
 namespace hifa4 {
 
-// New tokens of row b: [begin, begin + count) of the input, at the places
-// [len - count, len) of the sequence.  Counts outside the contract are cut to
-// the input, to max_new and to the sequence, so that no access leaves a buffer.
+// New tokens of row b: [begin, begin + count) of the input go to the places
+// [first, first + count) of the sequence, whose last tokens they are.  What is
+// outside the contract is left out, so that no access leaves a buffer: rows
+// behind the input, tokens in front of the sequence (more new ones than it
+// holds) and behind max_new.
 struct NewTokens {
   int begin, count, first;
 };
@@ -20,8 +22,9 @@ __device__ __forceinline__ NewTokens new_tokens(const int* cu, int b, int total,
   NewTokens t;
   t.begin = cu ? min(max(cu[b], 0), total) : b;
   const int end = cu ? min(max(cu[b + 1], t.begin), total) : min(b + 1, total);
-  t.count = min(min(max(end - t.begin, 0), max_new), len);
-  t.first = len - t.count;
+  t.begin = max(t.begin, end - len);
+  t.first = len - (end - t.begin);
+  t.count = min(end - t.begin, max_new);
   return t;
 }
 
@@ -88,8 +91,9 @@ __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks)
   const int len = paged_len(a.c, it.b);
   const NewTokens nt = new_tokens(a.cu, it.b, a.total, a.max_new, len);
   const int place = nt.first / kPage + it.blk, p0 = place * kPage;
-  if (nt.count == 0 || p0 >= len) return;
-  const int lo = max(nt.first - p0, 0), hi = min(len - p0, kPage);     // new keys of the page: [lo, hi)
+  const int stop = nt.first + nt.count;
+  if (nt.count == 0 || p0 >= stop) return;
+  const int lo = max(nt.first - p0, 0), hi = min(stop - p0, kPage);    // new keys of the page: [lo, hi)
   uint8_t* rec = paged_record(a.c, it.b, place, it.head);
   const size_t row = (size_t)a.c.hkv * D;
   // the new token at key 0 of the page (it may lie before the input: only keys >= lo are read)
@@ -265,8 +269,8 @@ __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks)
   // The tail gets the last page's new rows.  The workgroup of the first page
   // writes them: it alone reads the tail, and has done so before the barrier.
   if (it.blk == 0) {
-    const int last = (len - 1) / kPage * kPage;               // place of the last page's first token
-    const int from = max(nt.first - last, 0), to = len - last;
+    const int last = (stop - 1) / kPage * kPage;              // place of the last page's first token
+    const int from = max(nt.first - last, 0), to = stop - last;
     const long l0 = (long)nt.begin + last - nt.first;
     for (int i = tid; i < (to - from) * (D / 8); i += 256) {
       const int key = from + i / (D / 8), ch = 8 * (i % (D / 8));
@@ -297,8 +301,9 @@ __global__ void __launch_bounds__(256) k_paged_append16(PagedAppend a, int block
   const int len = paged_len(a.c, it.b);
   const NewTokens nt = new_tokens(a.cu, it.b, a.total, a.max_new, len);
   const int place = nt.first / kPage + it.blk, p0 = place * kPage;
-  if (nt.count == 0 || p0 >= len) return;
-  const int lo = max(nt.first - p0, 0), hi = min(len - p0, kPage);
+  const int stop = nt.first + nt.count;
+  if (nt.count == 0 || p0 >= stop) return;
+  const int lo = max(nt.first - p0, 0), hi = min(stop - p0, kPage);
   uint8_t* rec = paged_record(a.c, it.b, place, it.head);
   if (!rec) return;
   const size_t row = (size_t)a.c.hkv * D;

@@ -53,46 +53,64 @@ struct Run {
 __device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
   return b < c.batch ? (paged_len(c, b) + kPage - 1) / kPage : 0;
 }
-// Sum over the sequences of f(pages), by a whole wave; n0: those of the first 64.
+// The sequences are dealt to the lanes of a wave (b, b + 64, ...), the pages of
+// a lane's first kHeldSeqs in registers.
+constexpr int kHeldSeqs = 4;
+struct Dealt {
+  int n[kHeldSeqs];
+};
+// Sum of f(pages) over the sequences of each lane.
 template <typename F>
-__device__ __forceinline__ int sum_sequences(const PagedCache& c, int n0, int lane, F f) {
-  int total = __builtin_amdgcn_readlane(wave_scan(f(n0)), 63);
-  for (int b0 = 64; b0 < c.batch; b0 += 64) total += __builtin_amdgcn_readlane(wave_scan(f(pages_of(c, b0 + lane))), 63);
-  return total;
+__device__ __forceinline__ int lane_sum(const PagedCache& c, const Dealt& d, int lane, F f) {
+  int sum = f(d.n[0]);
+#pragma unroll
+  for (int i = 1; i < kHeldSeqs; ++i)
+    if (c.batch > 64 * i) sum += f(d.n[i]);
+  for (int b = 64 * kHeldSeqs + lane; b < c.batch; b += 64) sum += f(pages_of(c, b));
+  return sum;
 }
 // The run numbered r (found by a whole wave), or with r < 0 the runs of
-// sequence `want`.
+// sequence `want`.  Runs are numbered lane by lane of the above.
 __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, int want, int lane) {
-  const int n0 = pages_of(c, lane);
-  const int total = sum_sequences(c, n0, lane, [](int n) { return n; });
+  Dealt d;
+#pragma unroll
+  for (int i = 0; i < kHeldSeqs; ++i) d.n[i] = pages_of(c, 64 * i + lane);
+  const int total = __builtin_amdgcn_readlane(wave_scan(lane_sum(c, d, lane, [](int n) { return n; })), 63);
   int per = max(1, (total + target - 1) / target);
+  int mine = 0, upto = 0;
   // the last runs of the sequences are shorter: longer runs until all fit into one round (or nearly)
-  for (int i = 0; i < 6; ++i) {
-    const int runs = sum_sequences(c, n0, lane, [per](int n) { return (n + per - 1) / per; });
-    if (runs <= target) break;
+  for (int i = 0;; ++i) {
+    mine = lane_sum(c, d, lane, [per](int n) { return (n + per - 1) / per; });
+    upto = wave_scan(mine);
+    const int runs = __builtin_amdgcn_readlane(upto, 63);
+    if (runs <= target || i == 6 || c.batch >= target) break;
     per += max(1, (int)((long)per * (runs - target) / target));
   }
   Run out = {-1, 0, 0, 0, 0};
-  int before = 0;
-  for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    const int n = b0 ? pages_of(c, b0 + lane) : n0, cnt = (n + per - 1) / per;
-    const int upto = wave_scan(cnt), mine = before + upto - cnt;
-    const bool hit = r >= 0 ? (r >= mine && r < mine + cnt) : b0 + lane == want;
-    const unsigned long long who = __builtin_amdgcn_ballot_w64(hit);
-    if (who) {
-      const int src = __builtin_ctzll(who);
-      out.b = b0 + src;
-      out.first = __builtin_amdgcn_readlane(mine, src);
-      out.count = __builtin_amdgcn_readlane(cnt, src);
-      const int pages = __builtin_amdgcn_readlane(n, src);
+  int src = want & 63;
+  if (r >= 0) {
+    const unsigned long long who = __builtin_amdgcn_ballot_w64(r < upto);
+    if (!who) return out;
+    src = __builtin_ctzll(who);
+  }
+  out.first = __builtin_amdgcn_readlane(upto - mine, src);
+  for (int b = src, i = 0; b < c.batch; b += 64, ++i) {
+    const int n = i == 0   ? __builtin_amdgcn_readlane(d.n[0], src)
+                  : i == 1 ? __builtin_amdgcn_readlane(d.n[1], src)
+                  : i == 2 ? __builtin_amdgcn_readlane(d.n[2], src)
+                  : i == 3 ? __builtin_amdgcn_readlane(d.n[3], src)
+                           : __builtin_amdgcn_readfirstlane(pages_of(c, b));
+    out.count = (n + per - 1) / per;
+    if (r >= 0 ? r < out.first + out.count : b == want) {
+      out.b = b;
       if (r >= 0) {                  // the first runs get one page more where the count does not divide
-        const int i = r - out.first, some = pages / out.count, more = pages % out.count;
-        out.begin = i * some + min(i, more);
-        out.end = out.begin + some + (i < more);
+        const int k = r - out.first, some = n / out.count, more = n % out.count;
+        out.begin = k * some + min(k, more);
+        out.end = out.begin + some + (k < more);
       }
       return out;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
+    out.first += out.count;
   }
   return out;
 }

@@ -175,6 +175,141 @@ def test_decode_is_deterministic_and_keeps_workspaces_apart(fmt):
     assert torch.allclose(torch.where(used, w2, 0.0).sum(1), torch.full((3,), 8.0, device="cuda"), rtol=0, atol=1e-4)
 
 
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d,hkv", [(64, 32), (128, 64), (256, 32)])
+def test_decode_runs_longer_than_a_table_look_up(fmt, d, hkv):
+    """Runs of more than 64 pages, on a table that names a few pages again and again: key j of page i counts as often
+    as the table has i."""
+    rng = np.random.default_rng(d)
+    num, mp = 5, 6400 if d == 64 else 2200
+    n = 64 * mp - 17
+    k, v, _ = _sequences(rng, [64 * num], hkv, d, False)
+    pool = P.fill_pool(k, v, np.arange(num)[None], [64 * num], num, FMT[fmt])
+    table = rng.integers(0, num, (2, mp)).astype(np.int32)
+    cache = _cache(pool, table, [n, 70], d, FMT[fmt])
+    q = rng.standard_normal((2, hkv, d)).astype(np.float16)
+    w = np.zeros((2, mp), np.float32)
+    wt = to_gpu(w)
+    o, lse = h.hifa4_paged_decode_fwd(cache, to_gpu(q), page_weights=wt)
+    o, lse, wt = to_np(o).astype(np.float64), to_np(lse), to_np(wt)
+    count = np.zeros((num, 64))
+    for j in range(mp):
+        count[table[0, j], :64 if j < mp - 1 else 47] += 1
+    for head in range(hkv):
+        kk, vv, _ = P.cached(pool[:, head:head + 1], np.arange(num), 64 * num, 1, d, FMT[fmt])
+        s = kk[:, 0] @ q[0, head].astype(np.float64) / np.sqrt(d)
+        e = np.exp(s - s.max()) * count.ravel()
+        p = e / e.sum()
+        assert abs(lse[head, 0] - (s.max() + np.log(e.sum()))) < 1e-4
+        # p in 11 bits or more, the fp32 sums of 6400 pages (2^-24 a step at most), o to fp16
+        bound = (2.0 ** -11 + 6400 * 2.0 ** -24) * (p @ np.abs(vv[:, 0])) + 2.0 ** -11 * np.abs(p @ vv[:, 0]) + 1e-6
+        assert (np.abs(o[0, head] - p @ vv[:, 0]) <= bound).all()
+    assert abs(wt[0].sum() - hkv) < 1e-2 and abs(wt[1, :2].sum() - hkv) < 1e-3 and (wt[1, 2:] == 0).all()
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+def test_decode_batches_of_hundreds(fmt):
+    """Batches over the 256 sequences that a wave keeps in registers, most of them empty, some with several runs."""
+    rng = np.random.default_rng(12)
+    lens = [int(x) for x in rng.integers(1, 90, 330) * (rng.random(330) < 0.3)]
+    lens[5], lens[69], lens[261], lens[325], lens[329] = 1300, 900, 1500, 700, 0
+    _decode_case(13, lens, 1, 1, 64, FMT[fmt], weights=True)
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+def test_pages_beyond_four_gib(fmt):
+    """A pool of more than 2^32 bytes: append, gather and decode at its end give what they give in a small pool."""
+    import torch
+    fm, hkv, d = FMT[fmt], 8, 128
+    page = h.hifa4_paged_page_bytes(hkv, d, fm)
+    big = (1 << 32) // page + 40
+    rng = np.random.default_rng(6)
+    lens = [500, 130]
+    k, v, s = _sequences(rng, lens, hkv, d, True)
+    table, num = _table(rng, lens)
+    got = []
+    for shift, pages in ((0, num), (big - num, big)):
+        t = np.where(table >= 0, table + shift, -1).astype(np.int32)
+        cache = h.PagedCache.empty(pages, 2, t.shape[1], hkv, d, fm)
+        cache.block_table.copy_(to_gpu(t))
+        cache.seq_lens.copy_(to_gpu(np.array(lens, np.int32)))
+        cu = to_gpu(np.array([0, 500, 630], np.int32))
+        h.hifa4_paged_append(cache, to_gpu(np.concatenate(k)), to_gpu(np.concatenate(v)), to_gpu(s), cu_new=cu)
+        q = to_gpu(np.random.default_rng(1).standard_normal((2, 16, d)).astype(np.float16))
+        got.append(h.hifa4_paged_gather(cache, cu, 630) + h.hifa4_paged_decode_fwd(cache, q, to_gpu(s)))
+        torch.cuda.synchronize()
+    assert cache.pool.numel() > 1 << 32
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    """Calls of two streams in flight together, each with a workspace of its own."""
+    import torch
+    rng = np.random.default_rng(21)
+    lens = [5000, 2000, 64]
+    k, v, _ = _sequences(rng, lens, 2, 128, False)
+    table, num = _table(rng, lens)
+    cache = _cache(P.fill_pool(k, v, table, lens, num, P.HIF4), table, lens, 128, P.HIF4)
+    q = [to_gpu(rng.standard_normal((3, 8, 128)).astype(np.float16)) for _ in range(2)]
+    want = [h.hifa4_paged_decode_fwd(cache, x) for x in q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(h.hifa4_paged_decode_fwd(cache, q[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o, lse in got[i]:
+            assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+def test_binding_refusals():
+    import torch
+    c = h.PagedCache.empty(4, 2, 3, 2, 64)
+    z = lambda *s, t=torch.float16: torch.zeros(s, dtype=t, device="cuda")
+    f32, i32 = torch.float32, torch.int32
+    for args, kw in (((z(2, 4, 128),), {}), ((z(3, 4, 64),), {}), ((z(2, 4, 64, t=f32),), {}), ((z(2, 64, 4).transpose(1, 2),), {}),
+                     ((z(2, 4, 64).cpu(),), {}), ((z(2, 4, 64), z(1, 64, t=f32)), {}), ((z(2, 4, 64),), {"out": z(2, 4, 128)}),
+                     ((z(2, 4, 64),), {"lse": z(2, 4, t=f32)}), ((z(2, 4, 64),), {"weights_out": z(2, 3, t=f32)}),
+                     ((z(2, 4, 64),), {"page_weights": z(2, 4, t=f32)}), ((z(4, 64),), {})):
+        with pytest.raises(ValueError):
+            h.hifa4_paged_decode_fwd(c, *args, **kw)
+    with pytest.raises(h.Hifa4Error, match="multiple"):
+        h.hifa4_paged_decode_fwd(c, z(2, 3, 64))
+    for k, v, kw in ((z(2, 2, 64), z(2, 2, 128), {}), (z(2, 1, 64), z(2, 1, 64), {}),
+                     (z(2, 2, 64), z(2, 2, 64), {"cu_new": z(2, t=i32)}), (z(2, 2, 64), z(2, 2, 64), {"s": z(2, 64)})):
+        with pytest.raises(ValueError):
+            h.hifa4_paged_append(c, k, v, **kw)
+    with pytest.raises(h.Hifa4Error, match="one new token per sequence"):
+        h.hifa4_paged_append(c, z(3, 2, 64), z(3, 2, 64))
+    with pytest.raises(h.Hifa4Error, match="v_tail"):
+        h.hifa4_paged_append(h.PagedCache(c.pool, c.block_table, c.seq_lens, 64), z(2, 2, 64), z(2, 2, 64))
+    with pytest.raises(ValueError):
+        h.hifa4_paged_gather(c, z(3, t=i32), 5, k=z(5, 2, 64), v=z(4, 2, 64))
+    with pytest.raises(ValueError):
+        h.hifa4_paged_gather(c, z(2, t=i32), 5)
+    with pytest.raises(h.Hifa4Error, match="first"):
+        h.hifa4_paged_evict(c.block_table, c.seq_lens, z(2, 3, t=f32), 2, 2, 1)
+    for bad in ({"out_table": z(2, 4, t=i32)}, {"out_lens": z(3, t=i32)}, {"out_weights": z(2, 3)}, {"freed": z(2, 3, t=f32)},
+                {"num_freed": z(2, 1, t=i32)}):
+        with pytest.raises(ValueError):
+            h.hifa4_paged_evict(c.block_table, c.seq_lens, z(2, 3, t=f32), 2, **bad)
+    for args in ((c.pool[:, 0], c.block_table, c.seq_lens, 64), (c.pool, c.block_table[0], c.seq_lens, 64),
+                 (c.pool, c.block_table, c.seq_lens[:1], 64), (c.pool, c.block_table, c.seq_lens, 128),
+                 (c.pool, c.block_table, c.seq_lens, 64, h.OPERANDS_FP16), (c.pool, c.block_table, c.seq_lens, 64, 0, z(2, 64, 2, 128))):
+        with pytest.raises(ValueError):
+            h.PagedCache(*args)
+    # nothing to do
+    h.hifa4_paged_append(c, z(0, 2, 64), z(0, 2, 64), cu_new=z(3, t=i32))
+    k, v = h.hifa4_paged_gather(c, z(3, t=i32), 0)
+    assert k.shape == (0, 2, 64)
+    o, lse = h.hifa4_paged_decode_fwd(c, z(2, 4, 64) + 1)
+    assert bool((o == 0).all()) and bool((lse == float("-inf")).all())
+
+
 # --------------------------------------------------------------------------- append and gather
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 @pytest.mark.parametrize("d", [64, 128, 256])
@@ -265,26 +400,36 @@ def test_append_and_gather_stay_inside(fmt):
     import torch
     fm, hkv, d = FMT[fmt], 2, 64
     rng = np.random.default_rng(4)
-    table = np.array([[0, -1, 5, 2], [7, 1 << 30, -5, 4], [1, 3, -1, -1]], np.int32)
-    pool = rng.integers(0, 256, (6, hkv, P.record_bytes(d, fm))).astype(np.uint8)
-    lens = np.array([1000, 200, -3], np.int32)              # cut to 256 and 0
-    cu = np.array([0, 230, 500, 900], np.int32)             # past the input (600 rows), more than the sequence holds
-    cache = _cache(pool, table, lens, d, fm, np.zeros((3, 64, hkv, d), np.float16) if fm == P.HIF4 else None)
-    k = torch.randn(600, hkv, d, device="cuda").half()
+    table = np.array([[0, -1, 5, 2], [7, 1 << 30, -5, 4], [1, 3, -1, -1], [6, -1, -1, -1]], np.int32)
+    pool = rng.integers(0, 256, (7, hkv, P.record_bytes(d, fm))).astype(np.uint8)
+    lens = np.array([1000, 200, -3, 30], np.int32)          # cut to 256 and 0
+    cu = np.array([0, 160, 230, 300, 900], np.int32)        # past the input (400 rows), more than a sequence holds
+    cache = _cache(pool, table, lens, d, fm, np.zeros((4, 64, hkv, d), np.float16) if fm == P.HIF4 else None)
+    k = torch.randn(400, hkv, d, device="cuda").half()
     h.hifa4_paged_append(cache, k, k, cu_new=to_gpu(cu), max_new=100)
     after = to_np(cache.pool)
-    # new tokens: sequence 0 places 156..255 (pages 5, 2), sequence 1 100..199 (its pages are none but place 3: page 4)
+    # Sequence 0: 160 new ones at 96..255, the first 100 stored (96..195: pages -1, 5, 2); sequence 1: 70 at
+    # 130..199 (its last two pages, none and 4); sequence 3: the last 30 of 100.
     for page in (0, 1, 3):
         assert np.array_equal(after[page], pool[page]), page
-    for b, n, first in ((0, 256, 156), (1, 200, 100)):
-        gk, gv, there = P.cached(after, table[b], n, hkv, d, fm)
-        begin = int(cu[b])
-        kn = to_np(k)[begin:begin + n - first].astype(np.float64)
-        at = np.arange(first, n)[there[first:]]
+    assert len(cu) - 1 == len(lens)
+    for b, first, stop, begin in ((0, 96, 196, 0), (1, 130, 200, 160), (3, 0, 30, 370)):
+        gk, gv, there = P.cached(after, table[b], stop, hkv, d, fm)
+        kn = to_np(k)[begin:begin + stop - first]
+        at = np.arange(first, stop)[there[first:]]
+        assert len(at)
         if fm == P.FP16:
             assert np.array_equal(gk[at], kn[at - first]) and np.array_equal(gv[at], kn[at - first])
-    gk, gv = h.hifa4_paged_gather(cache, to_gpu(np.array([-5, 300, 300, 10000], np.int32)), 320, max_tokens=310,
-                                  starts=to_gpu(np.array([-7, 2 ** 31 - 1, 3], np.int32)),
+        else:
+            from oracle import hif4
+            want = hif4.quantize(kn.astype(np.float64).reshape(-1, hkv, d // 64, 64))["xhat"].reshape(kn.shape)
+            assert np.array_equal(gk[at], want[at - first])
+    if fm == P.FP16:                                        # behind max_new: as it was (HIF4 clears what is unused)
+        gk0 = P.cached(pool, table[0], 256, hkv, d, fm)[0]
+        gk1 = P.cached(after, table[0], 256, hkv, d, fm)[0]
+        assert np.array_equal(gk0[196:], gk1[196:], equal_nan=True)
+    gk, gv = h.hifa4_paged_gather(cache, to_gpu(np.array([-5, 300, 300, 310, 10000], np.int32)), 320, max_tokens=310,
+                                  starts=to_gpu(np.array([-7, 2 ** 31 - 1, 3, 40], np.int32)),
                                   k=torch.full((320, hkv, d), 7.0, device="cuda").half(),
                                   v=torch.full((320, hkv, d), 7.0, device="cuda").half())
     wk, wv, _ = P.cached(after, table[0], 256, hkv, d, fm)

@@ -69,30 +69,28 @@ __device__ __forceinline__ int lane_sum(const PagedCache& c, const Dealt& d, int
   for (int b = 64 * kHeldSeqs + lane; b < c.batch; b += 64) sum += f(pages_of(c, b));
   return sum;
 }
-// The run numbered r (found by a whole wave), or with r < 0 the runs of
-// sequence `want`.  Runs are numbered lane by lane of the above.
-__device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, int want, int lane) {
+// The run numbered r (found by a whole wave).  Runs are numbered lane by lane of the above.
+__device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, int lane) {
   Dealt d;
 #pragma unroll
   for (int i = 0; i < kHeldSeqs; ++i) d.n[i] = pages_of(c, 64 * i + lane);
-  const int total = __builtin_amdgcn_readlane(wave_scan(lane_sum(c, d, lane, [](int n) { return n; })), 63);
-  int per = max(1, (total + target - 1) / target);
-  int mine = 0, upto = 0;
-  // the last runs of the sequences are shorter: longer runs until all fit into one round (or nearly)
-  for (int i = 0;; ++i) {
-    mine = lane_sum(c, d, lane, [per](int n) { return (n + per - 1) / per; });
-    upto = wave_scan(mine);
-    const int runs = __builtin_amdgcn_readlane(upto, 63);
-    if (runs <= target || i == 6 || c.batch >= target) break;
-    per += max(1, (int)((long)per * (runs - target) / target));
+  int mine = lane_sum(c, d, lane, [](int n) { return n; }), upto = wave_scan(mine), per = 1;
+  const int total = __builtin_amdgcn_readlane(upto, 63);
+  if (total > target) {
+    per = (total + target - 1) / target;
+    // the last runs of the sequences are shorter: longer runs until all fit into one round (or nearly)
+    for (int i = 0;; ++i) {
+      mine = lane_sum(c, d, lane, [per](int n) { return (n + per - 1) / per; });
+      upto = wave_scan(mine);
+      const int runs = __builtin_amdgcn_readlane(upto, 63);
+      if (runs <= target || i == 6 || c.batch >= target) break;
+      per += max(1, (int)((long)per * (runs - target) / target));
+    }
   }
   Run out = {-1, 0, 0, 0, 0};
-  int src = want & 63;
-  if (r >= 0) {
-    const unsigned long long who = __builtin_amdgcn_ballot_w64(r < upto);
-    if (!who) return out;
-    src = __builtin_ctzll(who);
-  }
+  const unsigned long long who = __builtin_amdgcn_ballot_w64(r < upto);
+  if (!who) return out;
+  const int src = __builtin_ctzll(who);
   out.first = __builtin_amdgcn_readlane(upto - mine, src);
   for (int b = src, i = 0; b < c.batch; b += 64, ++i) {
     const int n = i == 0   ? __builtin_amdgcn_readlane(d.n[0], src)
@@ -101,13 +99,11 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, 
                   : i == 3 ? __builtin_amdgcn_readlane(d.n[3], src)
                            : __builtin_amdgcn_readfirstlane(pages_of(c, b));
     out.count = (n + per - 1) / per;
-    if (r >= 0 ? r < out.first + out.count : b == want) {
-      out.b = b;
-      if (r >= 0) {                  // the first runs get one page more where the count does not divide
-        const int k = r - out.first, some = n / out.count, more = n % out.count;
-        out.begin = k * some + min(k, more);
-        out.end = out.begin + some + (k < more);
-      }
+    if (r < out.first + out.count) {
+      const int k = r - out.first, some = n / out.count, more = n % out.count;
+      out.b = b;                       // the first runs get one page more where the count does not divide
+      out.begin = k * some + min(k, more);
+      out.end = out.begin + some + (k < more);
       return out;
     }
     out.first += out.count;
@@ -115,11 +111,13 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, 
   return out;
 }
 
-// Workspace: o [slots][hq][D], then (m, l) [slots][hq], then with page weights
-// (m, sum) [batch][max_pages][hq]; m in log2 units.
+// Workspace: o [slots][hq][D], then (m, l) [slots][hq], the runs (first, count)
+// of each sequence that has any, then with page weights (m, sum)
+// [batch][max_pages][hq]; m in log2 units.
 struct DecodeWs {
   float* o;
   float2* ml;
+  int2* runs;
   float2* page;
 };
 __host__ __device__ __forceinline__ DecodeWs decode_ws(uint8_t* ws, const PagedCache& c, int target, int hq) {
@@ -127,12 +125,13 @@ __host__ __device__ __forceinline__ DecodeWs decode_ws(uint8_t* ws, const PagedC
   DecodeWs w;
   w.o = reinterpret_cast<float*>(ws);
   w.ml = reinterpret_cast<float2*>(w.o + slots * hq * c.D);
-  w.page = w.ml + slots * hq;
+  w.runs = reinterpret_cast<int2*>(w.ml + slots * hq);
+  w.page = reinterpret_cast<float2*>(w.runs + c.batch);
   return w;
 }
 size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights) {
   const size_t slots = run_slots(c.batch, run_target(hq, c.hkv, c.D, c.fp16), c.max_pages);
-  return slots * hq * (c.D + 2) * 4 + (weights ? (size_t)c.batch * c.max_pages * hq * 8 : 0);
+  return slots * hq * (c.D + 2) * 4 + (size_t)c.batch * 8 + (weights ? (size_t)c.batch * c.max_pages * hq * 8 : 0);
 }
 
 // q s to fp16, the exact product rounded once: the fp32 product made odd where
@@ -364,24 +363,40 @@ struct QueryDigits {
   uint4 word[G][2][4][16];             // a word's eight bytes, twice
   int exponent[G][4];
 };
+// The rows as they come, eight channels of a row per lane and step (they are
+// fetched before the first page's loads, so that only they are waited for).
 template <int G>
-__device__ __forceinline__ void query_digits(QueryDigits<G>& out, const half_t* q, int rows, const float* s, int lane) {
+struct QueryRows {
+  uint4 q[(G + 1) / 2];
+  f4v_t s[(G + 1) / 2][2];
+};
+template <int G>
+__device__ __forceinline__ void load_query(QueryRows<G>& in, const half_t* q, int rows, const float* s, int lane) {
 #pragma unroll
-  for (int i = lane; i < 32 * G; i += 64) {
-    const int row = i / (8 * G), g = i / 8 % G, w = i & 7;
-    uint4 in = make_uint4(0, 0, 0, 0);
-    if (row < rows) in = *reinterpret_cast<const uint4*>(q + (size_t)row * 64 * G + 64 * g + 8 * w);
-    const h2_t y[4] = {__builtin_bit_cast(h2_t, in.x), __builtin_bit_cast(h2_t, in.y), __builtin_bit_cast(h2_t, in.z),
-                       __builtin_bit_cast(h2_t, in.w)};
-    float x[8];
+  for (int k = 0; k < (G + 1) / 2; ++k) {
+    const int i = lane + 64 * k, row = i / (8 * G), at = 8 * (i % (8 * G));
+    in.q[k] = make_uint4(0, 0, 0, 0);
+    if (row < min(rows, 4)) in.q[k] = *reinterpret_cast<const uint4*>(q + (size_t)row * 64 * G + at);
     if (s) {
-      const f4v_t s0 = *reinterpret_cast<const f4v_t*>(s + 64 * g + 8 * w);
-      const f4v_t s1 = *reinterpret_cast<const f4v_t*>(s + 64 * g + 8 * w + 4);
+      in.s[k][0] = *reinterpret_cast<const f4v_t*>(s + at);
+      in.s[k][1] = *reinterpret_cast<const f4v_t*>(s + at + 4);
+    }
+  }
+}
+template <int G>
+__device__ __forceinline__ void query_digits(QueryDigits<G>& out, const QueryRows<G>& in, bool smooth, int lane) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = (float)round_product(y[u >> 1][u & 1], u < 4 ? s0[u & 3] : s1[u & 3]);
-    } else {
+  for (int step = 0; step < (G + 1) / 2; ++step) {
+    const int i = lane + 64 * step, row = i / (8 * G), g = i / 8 % G, w = i & 7;
+    if (row >= 4) break;               // (half of the lanes with one group)
+    const uint4 q = in.q[step];
+    const h2_t y[4] = {__builtin_bit_cast(h2_t, q.x), __builtin_bit_cast(h2_t, q.y), __builtin_bit_cast(h2_t, q.z),
+                       __builtin_bit_cast(h2_t, q.w)};
+    float x[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = (float)y[u >> 1][u & 1];
+    for (int u = 0; u < 8; ++u) {
+      const half_t z = y[u >> 1][u & 1];
+      x[u] = smooth ? (float)round_product(z, in.s[step][u >> 2][u & 3]) : (float)z;
     }
     float top = 0.0f;
 #pragma unroll
@@ -414,10 +429,11 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
   const int target = run_target(a.hq, a.c.hkv, D, false);
-  const Run run = find_run(a.c, target, r, 0, lane);
+  const Run run = find_run(a.c, target, r, lane);
   if (run.b < 0) return;
   const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
   const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
+  if (r == run.first && head == 0 && tile == 0 && lane == 0) ws.runs[run.b] = make_int2(run.first, run.count);
   const size_t rec_bytes = (size_t)72 * D;
   const int v_lane = 16 * ((k & 1) * 2 + (k >> 1)) + n;        // lanes k = 1, 2 exchanged
   const int q_in = 4 * tile + (n >> 2), h = head * group + q_in;
@@ -435,14 +451,17 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     there = (unsigned)page < (unsigned)a.c.num_pages;
     return a.c.pool + ((size_t)(there ? page : 0) * a.c.hkv + head) * rec_bytes;
   };
-  query_digits<G>(qd, a.q + ((size_t)run.b * a.hq + head * group + 4 * tile) * D, group - 4 * tile,
-                  a.s ? a.s + (size_t)head * D : nullptr, lane);
+  QueryRows<G> rows;
+  load_query<G>(rows, a.q + ((size_t)run.b * a.hq + head * group + 4 * tile) * D, group - 4 * tile,
+                a.s ? a.s + (size_t)head * D : nullptr, lane);
+  keep_order();
   Part<G> kp[2], vp[2];
   const uint8_t* rec = record(run.begin, has);
   load_part<G>(kp[0], rec, lane, lane);
   keep_order();
   load_part<G>(vp[0], rec + 2304 * G, v_lane, lane);
   keep_order();
+  query_digits<G>(qd, rows, a.s != nullptr, lane);
   __syncthreads();
   uint32_t q_scale[G];
 #pragma unroll
@@ -603,10 +622,11 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
   const int target = run_target(a.hq, a.c.hkv, D, true);
-  const Run run = find_run(a.c, target, r, 0, lane);
+  const Run run = find_run(a.c, target, r, lane);
   if (run.b < 0) return;
   const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
   const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
+  if (r == run.first && head == 0 && tile == 0 && lane == 0) ws.runs[run.b] = make_int2(run.first, run.count);
   const int q_in = 16 * tile + n, h = head * group + q_in;
 
   Pages pg;
@@ -622,25 +642,23 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
     return a.c.pool + ((size_t)(there ? page : 0) * a.c.hkv + head) * (size_t)(256 * D);
   };
   h8v_t q[2 * G];
+  const float* s = a.s + (size_t)head * D + 8 * k;
 #pragma unroll
   for (int c = 0; c < 2 * G; ++c) {
-    const int ch = 32 * c + 8 * k;
     q[c] = h8v_t{0, 0, 0, 0, 0, 0, 0, 0};
-    if (q_in < group) {
-      q[c] = *reinterpret_cast<const h8v_t*>(a.q + ((size_t)run.b * a.hq + h) * D + ch);
-      if (a.s) {
-        const float* s = a.s + (size_t)head * D + ch;
-        const f4v_t s0 = *reinterpret_cast<const f4v_t*>(s), s1 = *reinterpret_cast<const f4v_t*>(s + 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[c][i] = round_product(q[c][i], i < 4 ? s0[i & 3] : s1[i & 3]);
-      }
-    }
+    if (q_in < group) q[c] = *reinterpret_cast<const h8v_t*>(a.q + ((size_t)run.b * a.hq + h) * D + 32 * c + 8 * k);
   }
+  if (a.s)
+#pragma unroll
+    for (int c = 0; c < 2 * G; ++c) {
+      const f4v_t s0 = *reinterpret_cast<const f4v_t*>(s + 32 * c), s1 = *reinterpret_cast<const f4v_t*>(s + 32 * c + 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[c][i] = round_product(q[c][i], i < 4 ? s0[i & 3] : s1[i & 3]);
+    }
   h8v_t kr[8 * G], vr[8 * G];          // K [t][D/32], V [D/16][c]
   const uint8_t* rec = record(run.begin, has);
   load_operands(kr, rec, lane);
   load_operands(vr, rec + 128 * D, lane);
-
   float ref = -1e30f, l = 0.0f;            // p = 2^(score - ref + kTop16), scores in log2 units
   f4v_t o[4 * G];
 #pragma unroll
@@ -737,6 +755,12 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
 // rows); behind those, with page weights, one per 16 pages of a sequence.
 constexpr int kJoin = 256, kPagesJoined = 16, kShare = kJoin / kPagesJoined;
 
+// (first, count) of a sequence's runs; the runs kernel wrote those of sequences with pages.
+__device__ __forceinline__ int2 sequence_runs(const PagedCache& c, const DecodeWs& ws, int b) {
+  const int2 r = ws.runs[b];
+  return paged_len(c, b) ? r : make_int2(0, 0);
+}
+
 // Two partial sums over runs as one, in the first's place.
 __device__ __forceinline__ void join_pair(float& m, float& l, f4v_t& o, float m2, float l2, f4v_t o2) {
   const float to = fmaxf(m, m2), ref = to == -INFINITY ? 0.0f : to;
@@ -759,23 +783,23 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
     // a set of threads takes every kSets-th run, (m, l) and o in one go; then the sets are joined in order
     const int slices = D / kWidth, row = blockIdx.x / slices, d0 = blockIdx.x % slices * kWidth;
     const int b = row / a.hq, h = row % a.hq;
-    const Run run = find_run(a.c, target, -1, b, lane);
+    const int2 run = sequence_runs(a.c, ws, b);
     const int col = tid % kCols, set = tid / kCols;
     f4v_t o = {0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
     constexpr int kAhead = 4;
-    for (int i = set; i < run.count; i += kAhead * kSets) {
+    for (int i = set; i < run.y; i += kAhead * kSets) {
       float2 x[kAhead];
       f4v_t y[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const size_t slot = (size_t)(run.first + min(i + u * kSets, run.count - 1)) * a.hq + h;
+        const size_t slot = (size_t)(run.x + min(i + u * kSets, run.y - 1)) * a.hq + h;
         x[u] = ws.ml[slot];
         y[u] = *reinterpret_cast<const f4v_t*>(ws.o + slot * D + d0 + 4 * col);
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
-        if (i + u * kSets < run.count) join_pair(m, l, o, x[u].x, x[u].y, y[u]);
+        if (i + u * kSets < run.y) join_pair(m, l, o, x[u].x, x[u].y, y[u]);
     }
     part[set][col] = o;
     if (col == 0) part_ml[set] = make_float2(m, l);
@@ -806,7 +830,7 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
   const float before = a.w_in[place];
   float w = 0.0f;
   if (j0 < pages) {
-    const Run run = find_run(a.c, target, -1, b, lane);
+    const int2 run = sequence_runs(a.c, ws, b);
     for (int h0 = 0; h0 < a.hq; h0 += 64) {
       float2 y[64 / kShare];
 #pragma unroll
@@ -816,8 +840,8 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
       }
       float m = -INFINITY, l = 0.0f;
       if (h0 + lane < a.hq)
-        for (int i = wave; i < run.count; i += 4) {
-          const float2 x = ws.ml[(size_t)(run.first + i) * a.hq + h0 + lane];
+        for (int i = wave; i < run.y; i += 4) {
+          const float2 x = ws.ml[(size_t)(run.x + i) * a.hq + h0 + lane];
           const float to = fmaxf(m, x.x), ref = to == -INFINITY ? 0.0f : to;
           l = l * __builtin_amdgcn_exp2f(m - ref) + x.y * __builtin_amdgcn_exp2f(x.x - ref);
           m = to;

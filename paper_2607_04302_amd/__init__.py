@@ -33,7 +33,8 @@ EXPORTED = ("hifa4_workspace_bytes", "hifa4_calibrate_workspace_bytes", "hifa4_c
             "hifa4_calibrate_smooth_qk_layers",
             "hifa4_quantize_qk", "hifa4_quantize_v", "hifa4_attention_fwd", "hifa4_decode_workspace_bytes",
             "hifa4_decode_fwd", "hifa4_paged_page_bytes", "hifa4_paged_append", "hifa4_paged_gather",
-            "hifa4_paged_decode_workspace_bytes", "hifa4_paged_decode_fwd", "hifa4_paged_evict", "hifa4_selftest_exp2", "hifa4_last_error", "hifa4_attention_fwd_noalloc")
+            "hifa4_paged_decode_workspace_bytes", "hifa4_paged_decode_fwd", "hifa4_paged_evict", "hifa4_selftest_exp2",
+            "hifa4_last_error", "hifa4_attention_fwd_noalloc")
 NOALLOC_SCRATCH_BYTES = 32 << 20
 PAGE_TOKENS = 64
 
@@ -496,6 +497,13 @@ def _shaped(t, dtype, shape, device, name):
         raise ValueError(f"{name} must be on {device}, got {t.device}")
 
 
+def _count(x, name):
+    """`x` where a 32-bit count goes (ctypes would cut a larger one without a word)."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits, got {x}")
+    return x
+
+
 def _paged_call(name, device, *args):
     """Calls an entry point of the library with `device` current."""
     fn = getattr(load_library(), name)
@@ -586,7 +594,9 @@ def hifa4_paged_append(cache: PagedCache, k, v, s=None, cu_new=None, max_new: Op
     s: the Smooth-QK scales (the pages then hold k/s).  max_new: an upper bound
     of the tokens per sequence (default: all of them)."""
     torch, dev = _torch(), cache.device
-    total = k.shape[0]
+    if k.dim() != 3:
+        raise ValueError("k is [total, heads_kv, head_dim]")
+    total = _count(k.shape[0], "the rows of k")
     _shaped(k, torch.float16, (total, cache.heads_kv, cache.head_dim), dev, "k")
     _shaped(v, torch.float16, (total, cache.heads_kv, cache.head_dim), dev, "v")
     if s is not None:
@@ -595,7 +605,7 @@ def hifa4_paged_append(cache: PagedCache, k, v, s=None, cu_new=None, max_new: Op
         _shaped(cu_new, torch.int32, (cache.batch + 1,), dev, "cu_new")
     if max_new is None:
         max_new = total if cu_new is not None else 1
-    _paged_call("hifa4_paged_append", dev, cache._ref, total, max_new, _ptr(cu_new), k.data_ptr(), v.data_ptr(), _ptr(s),
+    _paged_call("hifa4_paged_append", dev, cache._ref, total, _count(max_new, "max_new"), _ptr(cu_new), k.data_ptr(), v.data_ptr(), _ptr(s),
                 _stream(dev))
 
 
@@ -607,7 +617,8 @@ def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_toke
     cached.  max_tokens: an upper bound of the rows per sequence (default: all
     of them)."""
     torch, dev = _torch(), cache.device
-    shape = (total_tokens, cache.heads_kv, cache.head_dim)
+    shape = (_count(total_tokens, "total_tokens"), cache.heads_kv, cache.head_dim)
+    max_tokens = total_tokens if max_tokens is None else _count(max_tokens, "max_tokens")
     _shaped(cu_tokens, torch.int32, (cache.batch + 1,), dev, "cu_tokens")
     if starts is not None:
         _shaped(starts, torch.int32, (cache.batch,), dev, "starts")
@@ -619,8 +630,8 @@ def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_toke
         v = torch.empty(shape, dtype=torch.float16, device=dev)
     else:
         _shaped(v, torch.float16, shape, dev, "v")
-    _paged_call("hifa4_paged_gather", dev, cache._ref, total_tokens, total_tokens if max_tokens is None else max_tokens,
-                cu_tokens.data_ptr(), _ptr(starts), k.data_ptr(), v.data_ptr(), _stream(dev))
+    _paged_call("hifa4_paged_gather", dev, cache._ref, total_tokens, max_tokens, cu_tokens.data_ptr(),
+                _ptr(starts), k.data_ptr(), v.data_ptr(), _stream(dev))
     return k, v
 
 
@@ -682,6 +693,8 @@ def hifa4_paged_evict(block_table, seq_lens, page_weights, budget: int, first: i
     torch, dev = _torch(), block_table.device
     if block_table.dim() != 2:
         raise ValueError("block_table is [batch, max_pages]")
+    for x, name in ((budget, "budget"), (first, "first"), (last, "last")):
+        _count(x, name)
     i32, f32 = torch.int32, torch.float32
     shape = block_table.shape
     rows = shape[:1]

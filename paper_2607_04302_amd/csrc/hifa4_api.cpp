@@ -320,10 +320,17 @@ hifa4_status check_query_heads(int32_t hq, int32_t batch, int32_t hkv) {
 }
 
 // workgroups of a launch over (sequence, page, head)
-hifa4_status check_page_grid(const hifa4_paged_cache* c, int32_t tokens) {
+hifa4_status check_page_grid(const hifa4_paged_cache* c, int32_t tokens, const char* bound) {
   const int64_t blocks = ((int64_t)tokens + 62) / 64 + 1;
-  if (blocks * c->batch * c->num_heads_kv >= (1LL << 31))
-    return fail(HIFA4_ERR_UNSUPPORTED, "too many pages for one launch");
+  if ((int64_t)c->batch * c->num_heads_kv >= (1LL << 31) ||
+      (size_t)(blocks * c->batch * c->num_heads_kv) >= hifa4::kMaxGrid)
+    return fail(HIFA4_ERR_UNSUPPORTED, "too many pages for one launch (%s of %d tokens for each of %d sequences)", bound,
+                tokens, c->batch);
+  return HIFA4_OK;
+}
+hifa4_status check_join_grid(const hifa4::PagedCache& c, int32_t hq, bool weights) {
+  if (!hifa4::paged_decode_fits(c, hq, weights))
+    return fail(HIFA4_ERR_UNSUPPORTED, "page weights of %d x %d pages are too many for one launch", c.batch, c.max_pages);
   return HIFA4_OK;
 }
 
@@ -349,7 +356,7 @@ hifa4_status hifa4_paged_append(const hifa4_paged_cache* c, int32_t total_new, i
   if ((st = check_aligned16({k, v, s})) != HIFA4_OK) return st;
   if ((st = check_aligned4({cu_new})) != HIFA4_OK) return st;
   a.max_new = cu_new ? std::min(max_new, total_new) : 1;
-  if ((st = check_page_grid(c, a.max_new)) != HIFA4_OK) return st;
+  if ((st = check_page_grid(c, a.max_new, "max_new")) != HIFA4_OK) return st;
   a.k = (const hifa4::half_t*)k;
   a.v = (const hifa4::half_t*)v;
   a.s = s;
@@ -373,7 +380,7 @@ hifa4_status hifa4_paged_gather(const hifa4_paged_cache* c, int32_t total_tokens
   if ((st = check_aligned16({k, v})) != HIFA4_OK) return st;
   if ((st = check_aligned4({cu_tokens, starts})) != HIFA4_OK) return st;
   a.max_tokens = std::min(max_tokens, total_tokens);
-  if ((st = check_page_grid(c, a.max_tokens)) != HIFA4_OK) return st;
+  if ((st = check_page_grid(c, a.max_tokens, "max_tokens")) != HIFA4_OK) return st;
   a.cu = cu_tokens;
   a.starts = starts;
   a.k = (hifa4::half_t*)k;
@@ -386,7 +393,8 @@ hifa4_status hifa4_paged_gather(const hifa4_paged_cache* c, int32_t total_tokens
 
 size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q, int32_t page_weights) {
   hifa4::PagedCache pc;
-  if (check_paged(c, false, &pc) != HIFA4_OK || check_query_heads(num_heads_q, c->batch, c->num_heads_kv) != HIFA4_OK)
+  if (check_paged(c, false, &pc) != HIFA4_OK || check_query_heads(num_heads_q, c->batch, c->num_heads_kv) != HIFA4_OK ||
+      check_join_grid(pc, num_heads_q, page_weights != 0) != HIFA4_OK)
     return 0;
   return hifa4::paged_decode_workspace(pc, num_heads_q, page_weights != 0);
 }
@@ -398,6 +406,7 @@ hifa4_status hifa4_paged_decode_fwd(const hifa4_paged_cache* c, int32_t num_head
   hifa4_status st = check_paged(c, true, &a.c);
   if (st != HIFA4_OK) return st;
   if ((st = check_query_heads(num_heads_q, c->batch, c->num_heads_kv)) != HIFA4_OK) return st;
+  if ((st = check_join_grid(a.c, num_heads_q, page_weights != nullptr)) != HIFA4_OK) return st;
   if (!q || !o || !lse) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
   if ((page_weights == nullptr) != (weights_out == nullptr))
     return fail(HIFA4_ERR_INVALID_ARGUMENT, "page_weights and weights_out must both be set or both be NULL");
@@ -427,7 +436,7 @@ hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* 
                                int32_t* out_table, int32_t* out_lens, float* out_weights, int32_t* freed,
                                int32_t* num_freed, void* stream) {
   if (batch <= 0 || max_pages <= 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch and max_pages must be > 0");
-  if (max_pages >= (1 << 25) || (int64_t)batch * max_pages >= (1LL << 30))
+  if (max_pages >= (1 << 25) || (int64_t)batch * max_pages >= (1LL << 30) || batch >= (1 << 22))
     return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", batch, max_pages);
   if (first < 0 || last < 1 || (int64_t)first + last > budget)
     return fail(HIFA4_ERR_INVALID_ARGUMENT, "needs first >= 0, last >= 1 and first + last <= budget (%d, %d, %d)", first,

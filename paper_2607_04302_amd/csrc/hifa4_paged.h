@@ -86,6 +86,7 @@ __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // lane 15 of each row to the next
   return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
 }
+
 struct PagedAppend {
   PagedCache c;
   const half_t *k, *v;
@@ -119,6 +120,12 @@ struct PagedDecode {
   uint8_t* ws;
 };
 
+// Workgroups of 256 threads that one launch may have: HIP counts the threads of
+// a grid in 32 bits.
+constexpr size_t kMaxGrid = (size_t)1 << 24;
+
+// Whether the join's grid is a launch.
+bool paged_decode_fits(const PagedCache& c, int hq, bool weights);
 size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights);
 
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st);

@@ -870,6 +870,18 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
   if (tid % kShare == 0 && j < a.c.max_pages) a.w_out[place] = j < pages ? a.decay * before + w : before;
 }
 
+// Workgroups of the join: those of the rows (their channels shared out while
+// there are fewer rows than compute units) and those of the page weights.
+static int join_rows(const PagedCache& c, int hq) {
+  const int rows = c.batch * hq;
+  return rows < 256 ? rows * (c.D / 32) : rows;
+}
+static int join_pages(const PagedCache& c) { return c.batch * ((c.max_pages + kPagesJoined - 1) / kPagesJoined); }
+
+bool paged_decode_fits(const PagedCache& c, int hq, bool weights) {
+  return (size_t)join_rows(c, hq) + (weights ? join_pages(c) : 0) < kMaxGrid;
+}
+
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
   const int tiles = query_tiles(a.hq, a.c.hkv, a.c.fp16);
   const size_t runs = run_slots(a.c.batch, run_target(a.hq, a.c.hkv, a.c.D, a.c.fp16), a.c.max_pages);
@@ -891,12 +903,9 @@ hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // channels shared out while there are fewer rows than compute units
-  const size_t extra = a.w_in ? (size_t)a.c.batch * ((a.c.max_pages + kPagesJoined - 1) / kPagesJoined) : 0;
-  const int rows = a.c.batch * a.hq;
-  const bool few = rows < 256;
-  const int groups = few ? rows * (a.c.D / 32) : rows;
-  const dim3 join((unsigned)(groups + extra));
+  const int groups = join_rows(a.c, a.hq);
+  const bool few = groups != a.c.batch * a.hq;
+  const dim3 join((unsigned)(groups + (a.w_in ? join_pages(a.c) : 0)));
   if (few)
     k_paged_join<32><<<join, kJoin, 0, st>>>(a, groups);
   else if (a.c.D == 64)

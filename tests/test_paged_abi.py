@@ -126,6 +126,59 @@ def test_evict_is_checked(lib):
         assert _evict(lib, ptrs=p) == -1
 
 
+def test_launches_that_are_too_large_are_refused(lib):
+    """2^24 workgroups of 256 threads (2^22 of 1024) are more than one launch holds."""
+    big = _cache(batch=1 << 15, num_heads_kv=1 << 4, max_pages=64)      # 2^19 heads: 32 pages each are too many
+    for call in (_append, _gather):
+        assert call(lib, big, total=1 << 20, most=31 * 64, cu=FAKE) == -2
+        assert "too many pages for one launch" in h.hifa4_last_error()
+        assert call(lib, _cache(batch=1 << 20, num_heads_kv=1 << 12), total=1 << 20, most=1, cu=FAKE) == -2
+    wide = _cache(batch=1 << 8, max_pages=(1 << 22) - 1)                 # 2^26 groups of 16 pages
+    assert _decode(lib, wide, w=FAKE, wo=FAKE) == -2
+    assert "page weights" in h.hifa4_last_error()
+    assert lib.hifa4_paged_decode_workspace_bytes(ctypes.byref(wide), 4, 1) == 0
+    assert lib.hifa4_paged_decode_workspace_bytes(ctypes.byref(wide), 4, 0) > 0
+    assert _decode(lib, wide, ws=None) == -3                             # (no weights: that many pages are fine)
+    assert _evict(lib, batch=1 << 22, mp=4) == -2
+
+
+def test_counts_beyond_32_bits_are_refused(lib):
+    """A count is never cut to 32 bits (2^32 tokens at most would otherwise mean none)."""
+    class Cache:
+        batch, heads_kv, head_dim, max_pages, device, _ref = 2, 2, 64, 4, torch.device("cuda", 0), None
+
+    class Gpu:                                                           # as a GPU tensor of the right kind
+        is_cuda, dtype = True, torch.float16
+        device = Cache.device
+
+        def __init__(self, *shape, dtype=torch.float16):
+            self.shape, self.dtype = torch.Size(shape), dtype
+
+        def dim(self):
+            return len(self.shape)
+
+        def get_device(self):
+            return 0
+
+        def is_contiguous(self):
+            return True
+
+    x, cu = Gpu(5, 2, 64), Gpu(3, dtype=torch.int32)
+    for most in (1 << 32, -(1 << 40), 1 << 31):
+        with pytest.raises(ValueError, match="max_new must fit 32 bits"):
+            h.hifa4_paged_append(Cache, x, x, cu_new=cu, max_new=most)
+        with pytest.raises(ValueError, match="max_tokens must fit 32 bits"):
+            h.hifa4_paged_gather(Cache, cu, 5, max_tokens=most, k=x, v=x)
+    with pytest.raises(ValueError, match="total_tokens must fit 32 bits"):
+        h.hifa4_paged_gather(Cache, cu, 1 << 31)
+    with pytest.raises(ValueError, match="k is"):
+        h.hifa4_paged_append(Cache, Gpu(), x)
+    table, lens, w = Gpu(2, 4, dtype=torch.int32), Gpu(2, dtype=torch.int32), Gpu(2, 4, dtype=torch.float32)
+    for kw in ({"budget": 1 << 32}, {"budget": 2, "first": 1 << 32}, {"budget": 2, "last": (1 << 32) + 1}):
+        with pytest.raises(ValueError, match="must fit 32 bits"):
+            h.hifa4_paged_evict(table, lens, w, **kw)
+
+
 def test_the_binding_refuses_before_the_library(lib):
     t = torch.zeros
     with pytest.raises(ValueError, match="pool must be a GPU tensor"):

@@ -37,9 +37,6 @@ __device__ __forceinline__ PageItem page_item(int hkv, int blocks) {
   const int i = blockIdx.x / hkv;
   return PageItem{i / blocks, i % blocks, (int)blockIdx.x % hkv};
 }
-__device__ __forceinline__ uint32_t or_pair(uint32_t v) {            // with the neighbouring lane
-  return v | (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);
-}
 __device__ __forceinline__ uint32_t max_pair16(uint32_t p, uint32_t q) {
   return __builtin_bit_cast(uint32_t,
                             __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, p), __builtin_bit_cast(u16x2_t, q)));
@@ -75,18 +72,215 @@ __device__ __forceinline__ void channels_to_keys(const uint4 (&y)[4], uint2 (&x)
 // from the new tokens and, before them in the page, from the fp16 rows that
 // the tail keeps of the open page, places behind the last token zero: the page
 // holds at any time what quantizing the whole sequence would give.
-// A thread holds whole words (eight channels of a key of K, eight keys of four
-// channels of V), eight lanes a group; all its loads are issued before the
-// first is used.  Metadata bits are gathered in LDS (the two words of a lane of
-// the record are neighbours: one of them writes for both) and the page's parts
-// written whole.
-// Bound by HBM: 16 prompts of 512 to 2048 tokens, 8 heads, D=128 (107 MB).
+// One wave per tile of K and one per tile of V.  A lane of K is the record's
+// lane: 16 channels of the keys of its four rows, so its codes and its bytes of
+// metadata are whole and a group's maximum is a matter of four lanes, two rows
+// at a time.  A lane of V takes 16 keys of four neighbouring channels, that its
+// loads are 8 bytes wide; its codes go through LDS into 16-byte pieces, the
+// bits of the four rows of a lane of the record are joined across the wave.
+// 16 prompts of 512 to 2048 tokens, 8 heads, D=128, smoothed (107 MB): 30.9 us,
+// where the copy rate would take 23.  What is left is the wait for a page's
+// loads at its start: six waves per SIMD hide most of it, so K fetches its
+// scales from LDS for every row and is scheduled row by row (79 registers; with
+// 111, four waves, 41 us; seven with spills 35).
+__device__ __forceinline__ int padded(int at) { return at + (at >> 8) * 16; }
+
+// The codes of four pairs of values, a pair in the two halves of a register,
+// as nibbles (sign << 3 | u) in the low halves of bytes 0, 1 and 2, 3: those of
+// y0's and y1's values.  `sel` orders the four; x: the values, for their signs.
+__device__ __forceinline__ uint32_t nibble_bytes(uint32_t y0, uint32_t y1, h2_t x0, h2_t x1, uint32_t sel) {
+  const uint32_t u = __builtin_amdgcn_perm(y1, y0, sel) & 0x07070707u;
+  const uint32_t s = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x1), __builtin_bit_cast(uint32_t, x0), sel + 0x01010101u);
+  const uint32_t v = u | ((u + 0x07070707u) & ((s >> 4) & 0x08080808u));      // a zero code has no sign
+  return v | v >> 4;                       // bytes 0 and 2: two nibbles each
+}
+// Nothing is scheduled across: fewer registers at a time.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ uint32_t max_rows16(uint32_t v) {          // over the four lanes 16 apart, per half
+  const Pair32 p = pair32(v);
+  v = max_pair16(p.x, p.y);
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max_pair16(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t or_rows(uint32_t v) {
+  const Pair32 p = pair32(v);
+  v = p.x | p.y;
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return r[0] | r[1];
+}
+
+// K: the lane's metadata into `meta` (LDS), its codes into the record.  s: the
+// scales of the tile's 64 channels, or NULL; they and their reciprocals wait in
+// LDS (`scales`), where every row fetches its lane's 16.
 template <int G>
-__global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks) {
-  constexpr int D = 64 * G, kMeta = 256 * G, kWordsK = 2 * G, kItemsV = (G + 1) / 2;
-  __shared__ uint32_t meta_k[kMeta / 4], meta_v[kMeta / 4];
-  __shared__ __align__(16) uint32_t codes_k[2048 * G / 4], codes_v[2048 * G / 4];
-  const int tid = threadIdx.x;
+__device__ __forceinline__ void append_k(const uint4 (&in)[4][2], const float* s, float* scales, uint8_t* rec,
+                                         uint8_t* meta, int tile, int lane, int lo, int hi) {
+  const int n = lane & 15, k = lane >> 4;
+  if (s) {
+    scales[lane] = s[lane];
+    scales[64 + lane] = 1.0f / scales[lane];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  uint32_t e2 = 0, e3 = 0, bases = 0;      // E2 and E3 (halves: of the words' halves) by bit 2t + c; a base a byte
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {            // rows t = 2i and 2i + 1
+    const int key = key_of(2 * i, n);
+    const bool na = key >= lo && key < hi, nb = key + 4 >= lo && key + 4 < hi;
+    if (!__builtin_amdgcn_ballot_w64(na || nb)) continue;
+    h2_t x[2][8], a4[2][2];
+    u16x2_t a8[2][2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const uint4 w0 = in[2 * i + r][0], w1 = in[2 * i + r][1];
+      const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[r][e] = __builtin_bit_cast(h2_t, w[e]);
+      if (s) {
+        asm volatile("" ::: "memory");     // (fetched again: registers for more waves are worth more)
+        divide_pairs(x[r], scales + 16 * k, scales + 64 + 16 * k);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        a4[r][c] = hmax_pairs(hmax2(habs2(x[r][4 * c]), habs2(x[r][4 * c + 1])),
+                              hmax2(habs2(x[r][4 * c + 2]), habs2(x[r][4 * c + 3])));
+        a8[r][c] = __builtin_elementwise_max(as_u16(a4[r][c]), __builtin_shufflevector(as_u16(a4[r][c]), as_u16(a4[r][c]), 1, 0));
+      }
+      keep_order();
+    }
+    const u16x2_t t0 = __builtin_elementwise_max(a8[0][0], a8[0][1]), t1 = __builtin_elementwise_max(a8[1][0], a8[1][1]);
+    const h2_t top = __builtin_bit_cast(h2_t, max_rows16(__builtin_bit_cast(uint32_t, u16x2_t{t0[0], t1[1]})));
+    uint32_t word[2][2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const uint32_t base = e6m2_ceil((float)top[r]);
+      const float R = hif4_rcp_step(base);
+      const h2_t thr = range_floors(e6m2_value(base));
+      bases |= base << (8 * (2 * i + r));
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        u16x2_t lv, ne2;
+        block_levels(a4[r][c], __builtin_bit_cast(h2_t, a8[r][c]), h2_t{thr[0], thr[0]}, h2_t{thr[1], thr[1]}, lv, ne2);
+        uint32_t y[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const unsigned short ne = lv[q];
+          const h2_t u = x[r][4 * c + 2 * q], v = x[r][4 * c + 2 * q + 1];
+          y[q] = nibble_bytes(codes2(habs2(u), R, R, u16x2_t{ne, ne}), codes2(habs2(v), R, R, u16x2_t{ne, ne}), u, v,
+                              0x06040200u);
+        }
+        word[r][c] = __builtin_amdgcn_perm(y[1], y[0], 0x06040200u);
+        const int bit = 2 * (2 * i + r) + c;
+        e2 |= (1u - ne2[0]) << bit;
+        e3 |= __builtin_bit_cast(uint32_t, u16x2_t{1, 1} + ne2 - lv) << bit;
+      }
+      keep_order();
+    }
+    if (rec) {
+      uint8_t* at = rec + 2048 * tile + 1024 * i + 16 * lane;
+      if (na && nb)
+        *reinterpret_cast<uint4*>(at) = make_uint4(word[0][0], word[0][1], word[1][0], word[1][1]);
+      else if (na)
+        *reinterpret_cast<uint2*>(at) = make_uint2(word[0][0], word[0][1]);
+      else if (nb)
+        *reinterpret_cast<uint2*>(at + 8) = make_uint2(word[1][0], word[1][1]);
+    }
+  }
+  const int a3 = hif4_e3_at(G, tile, lane, 0) - 2048 * G, b3 = hif4_e3_at(G, tile, lane, 1) - 2048 * G;
+  const int a2 = hif4_e2_at(G, tile, lane) - 2048 * G, ab = hif4_base_at(G, tile, k, n) - 2048 * G;    // base: of row t = k
+  uint32_t base = bases >> (8 * k) & 0xFFu;
+  if (lo > 0 || hi < kPage) {              // the keys before lo keep what they have, those from hi on have nothing
+    uint32_t mine = 0, old = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int key = key_of(t, n);
+      if (key < lo)
+        old |= 3u << (2 * t);
+      else if (key < hi)
+        mine |= 3u << (2 * t);
+    }
+    e2 &= mine;
+    e3 &= mine * 0x00010001u;
+    if (!(mine >> (2 * k) & 1u)) base = 0;
+    if (lo > 0 && rec) {
+      const uint8_t* was = rec + 2048 * G;
+      e2 |= was[a2] & old;
+      e3 |= (was[a3] & old) | (was[b3] & old) << 16;
+      if (old >> (2 * k) & 1u) base = was[ab];
+    }
+  }
+  meta[a3] = (uint8_t)e3;
+  meta[b3] = (uint8_t)(e3 >> 16);
+  meta[a2] = (uint8_t)e2;
+  meta[ab] = (uint8_t)base;
+}
+
+// V: codes and metadata of a lane's 16 keys of four channels into LDS.
+template <int G>
+__device__ __forceinline__ void append_v(const uint2 (&in)[16], uint8_t* codes, uint8_t* meta, int tile, int lane) {
+  const int k = lane & 3, n = lane & 12, t = lane >> 4;          // channels 64 tile + 16 t + n ..
+  uint32_t e2[2], ea[2], eb[2], bases = 0;                       // E2; E3 of the words' first and second halves
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {            // channels n + 2p and n + 2p + 1, in the two halves
+    h2_t x[16], a4[4];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_bit_cast(h2_t, p ? in[e].y : in[e].x);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      a4[q] = hmax2(hmax2(habs2(x[4 * q]), habs2(x[4 * q + 1])), hmax2(habs2(x[4 * q + 2]), habs2(x[4 * q + 3])));
+    const u16x2_t a8[2] = {__builtin_elementwise_max(as_u16(a4[0]), as_u16(a4[1])),
+                           __builtin_elementwise_max(as_u16(a4[2]), as_u16(a4[3]))};
+    uint32_t all = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a8[0], a8[1]));
+    all = max_pair16(all, (uint32_t)__builtin_amdgcn_mov_dpp((int)all, 0xB1, 0xF, 0xF, true));
+    all = max_pair16(all, (uint32_t)__builtin_amdgcn_mov_dpp((int)all, 0x4E, 0xF, 0xF, true));
+    const h2_t top = __builtin_bit_cast(h2_t, all);
+    const uint32_t base[2] = {e6m2_ceil((float)top[0]), e6m2_ceil((float)top[1])};
+    const float r0 = hif4_rcp_step(base[0]), r1 = hif4_rcp_step(base[1]);
+    const h2_t f0 = range_floors(e6m2_value(base[0])), f1 = range_floors(e6m2_value(base[1]));
+    bases |= (base[0] | base[1] << 8) << (16 * p);
+    uint32_t word[2][2];                   // [channel][c]
+    e2[p] = ea[p] = eb[p] = 0;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t y[4];                       // two keys' nibbles of either channel
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u16x2_t lv, ne2;
+        block_levels(a4[2 * c + q], __builtin_bit_cast(h2_t, a8[c]), h2_t{f0[0], f1[0]}, h2_t{f0[1], f1[1]}, lv, ne2);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const h2_t u = x[8 * c + 4 * q + 2 * e], v = x[8 * c + 4 * q + 2 * e + 1];
+          y[2 * q + e] = nibble_bytes(codes2(habs2(u), r0, r1, lv), codes2(habs2(v), r0, r1, lv), u, v, 0x06020400u);
+        }
+        const uint32_t e3 = __builtin_bit_cast(uint32_t, u16x2_t{1, 1} + ne2 - lv);
+        (q ? eb[p] : ea[p]) |= e3 << c;
+        if (q == 0) e2[p] |= __builtin_bit_cast(uint32_t, u16x2_t{1, 1} - ne2) << c;
+      }
+      const uint32_t lo = __builtin_amdgcn_perm(y[1], y[0], 0x06020400u), hi = __builtin_amdgcn_perm(y[3], y[2], 0x06020400u);
+      word[0][c] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+      word[1][c] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      *reinterpret_cast<uint2*>(codes + padded(hif4_code_at(tile, t, 16 * k + n + 2 * p + e, 0))) =
+          make_uint2(word[e][0], word[e][1]);
+  }
+  // a byte a channel, the bits of its row t; joined, the bytes of the record's four lanes n .. n+3
+  const auto join = [&](const uint32_t (&x)[2]) { return or_rows(__builtin_amdgcn_perm(x[1], x[0], 0x06040200u) << (2 * t)) >> (8 * t); };
+  const int to = 16 * k + n + t;
+  meta[hif4_e2_at(G, tile, to) - 2048 * G] = (uint8_t)join(e2);
+  meta[hif4_e3_at(G, tile, to, 0) - 2048 * G] = (uint8_t)join(ea);
+  meta[hif4_e3_at(G, tile, to, 1) - 2048 * G] = (uint8_t)join(eb);
+  if (k == 0) *reinterpret_cast<uint32_t*>(meta + hif4_base_at(G, tile, t, n) - 2048 * G) = bases;
+}
+
+template <int G>
+__global__ void __launch_bounds__(128 * G) k_paged_append(PagedAppend a, int blocks) {
+  constexpr int D = 64 * G, kThreads = 128 * G, kMeta = 256 * G;
+  __shared__ __align__(16) uint8_t meta[2][kMeta];
+  __shared__ __align__(16) uint8_t codes[2048 * G + 8 * G * 16];
+  __shared__ __align__(16) float scales[2 * D];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), tile = wave % G;
   const PageItem it = page_item(a.c.hkv, blocks);
   const int len = paged_len(a.c, it.b);
   const NewTokens nt = new_tokens(a.cu, it.b, a.total, a.max_new, len);
@@ -100,170 +294,43 @@ __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks)
   const long t0 = (long)nt.begin + p0 - nt.first;
   half_t* tail = a.c.tail + ((size_t)it.b * kPage * a.c.hkv + it.head) * D;
 
-  // K: word w of group g of the keys key0, key0 + 32 / G, ...
-  const int w = tid & 7, g = (tid >> 3) % G, key0 = lo + tid / (8 * G);
-  uint4 in_k[kWordsK];
+  if (wave < G) {
+    const size_t at = (size_t)it.head * D + 64 * tile + 16 * (lane >> 4);
+    uint4 in[4][2];
 #pragma unroll
-  for (int i = 0; i < kWordsK; ++i) {
-    const int key = min(key0 + i * (32 / G), hi - 1);
-    in_k[i] = *reinterpret_cast<const uint4*>(a.k + (size_t)(t0 + key) * row + (size_t)it.head * D + 64 * g + 8 * w);
-  }
-  // V: keys 8w .. 8w+7 of four channels
-  uint2 in_v[kItemsV][8];
-#pragma unroll
-  for (int i = 0; i < kItemsV; ++i) {
-    const int ch = 4 * (tid >> 3) + 128 * i;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int key = 8 * w + e;
-      in_v[i][e] = make_uint2(0, 0);
-      if (key < hi && ch < D)
-        in_v[i][e] = key >= lo ? *reinterpret_cast<const uint2*>(a.v + (size_t)(t0 + key) * row + (size_t)it.head * D + ch)
-                               : *reinterpret_cast<const uint2*>(tail + (size_t)key * row + ch);
+    for (int t = 0; t < 4; ++t) {
+      const int key = min(max(key_of(t, lane & 15), lo), hi - 1);
+      const uint4* from = reinterpret_cast<const uint4*>(a.k + (size_t)(t0 + key) * row + at);
+      in[t][0] = from[0];
+      in[t][1] = from[1];
     }
-  }
-  // metadata: K's as it stands for the keys before lo, nothing for the others
-  for (int i = tid; i < kMeta / 4; i += 256) {
-    uint32_t x = 0;
-    if (lo > 0 && rec) {
-      x = reinterpret_cast<const uint32_t*>(rec + 2048 * G)[i];
-      uint32_t keep = 0;
-      for (int j = 0; j < 4; ++j) {
-        const int at = 4 * i + j;
-        if (at < 192 * G) {                                  // E3 or E2: bits 2t + c of a lane
-          const int n = (at < 128 * G ? at / (2 * G) : (at - 128 * G) / G) & 15;
-          for (int t = 0; t < 4; ++t)
-            if (key_of(t, n) < lo) keep |= 3u << (8 * j + 2 * t);
-        } else {
-          const int y = at - 192 * G, n = 4 * (y / (16 * G)) + (y & 3), t = (y >> 2) & 3;
-          if (key_of(t, n) < lo) keep |= 0xFFu << (8 * j);
-        }
-      }
-      x &= keep;
-    }
-    meta_k[i] = x;
-    meta_v[i] = 0;
-  }
-  __syncthreads();
-  uint8_t* bytes_k = reinterpret_cast<uint8_t*>(meta_k);
-  uint8_t* bytes_v = reinterpret_cast<uint8_t*>(meta_v);
-
-  {
-    float sc[8], rc[8];
-    if (a.s) {
-      const float4* sp = reinterpret_cast<const float4*>(a.s + (size_t)it.head * D + 64 * g + 8 * w);
-      const float4 s0 = sp[0], s1 = sp[1];
-      const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+    append_k<G>(in, a.s ? a.s + (size_t)it.head * D + 64 * tile : nullptr, scales + 128 * tile, rec, meta[0], tile, lane, lo, hi);
+  } else {
+    const int key0 = 16 * (lane & 3), ch = 64 * tile + 4 * (lane >> 2);
+    uint2 in[16];
+    if (lo == 0 && hi == kPage) {
+      const half_t* from = a.v + (size_t)(t0 + key0) * row + (size_t)it.head * D + ch;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sc[e] = s[e];
-        rc[e] = 1.0f / s[e];
+      for (int e = 0; e < 16; ++e) in[e] = *reinterpret_cast<const uint2*>(from + e * row);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = key0 + e;
+        in[e] = make_uint2(0, 0);
+        if (key < hi)
+          in[e] = *reinterpret_cast<const uint2*>(
+              key >= lo ? a.v + (size_t)(t0 + key) * row + (size_t)it.head * D + ch : tail + (size_t)key * row + ch);
       }
     }
-#pragma unroll
-    for (int i = 0; i < kWordsK; ++i) {
-      const int key = key0 + i * (32 / G);
-      if (key >= hi) break;                                  // whole sets of eight lanes
-      h2_t x[4] = {__builtin_bit_cast(h2_t, in_k[i].x), __builtin_bit_cast(h2_t, in_k[i].y),
-                   __builtin_bit_cast(h2_t, in_k[i].z), __builtin_bit_cast(h2_t, in_k[i].w)};
-      if (a.s) divide_pairs(x, sc, rc);
-      h2_t m[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] = habs2(x[e]);
-      const h2_t a4 = hmax_pairs(hmax2(m[0], m[1]), hmax2(m[2], m[3]));
-      const u16x2_t a8u = __builtin_elementwise_max(as_u16(a4), __builtin_shufflevector(as_u16(a4), as_u16(a4), 1, 0));
-      const uint32_t gm = reduce8(__builtin_bit_cast(uint32_t, a8u), max_pair16);
-      const uint32_t base = e6m2_ceil((float)__builtin_bit_cast(h2_t, gm)[0]);
-      const float R = hif4_rcp_step(base);
-      const h2_t thr = range_floors(e6m2_value(base));
-      u16x2_t lv, ne2;
-      block_levels(a4, __builtin_bit_cast(h2_t, a8u), h2_t{thr[0], thr[0]}, h2_t{thr[1], thr[1]}, lv, ne2);
-      uint32_t word = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned short ne = lv[e >> 1];
-        const uint32_t nib = nibbles2(codes2(m[e], R, R, u16x2_t{ne, ne}), x[e]);
-        word |= ((nib | (nib >> 12)) & 0xFFu) << (8 * e);
-      }
-      const int t = key_t(key), n = key_n(key), lane = 16 * (w >> 1) + n, bit = 2 * t + (w & 1);
-      codes_k[hif4_code_at(g, t, lane, w & 1) >> 2] = word;
-      const uint32_t e2 = 1u - ne2[0], e3 = (2u - lv[0] - e2) | (2u - lv[1] - e2) << (G == 1 ? 8 : 16);
-      const int a3 = hif4_e3_at(G, g, lane, 0) - 2048 * G, a2 = hif4_e2_at(G, g, lane) - 2048 * G;
-      const uint32_t b3 = or_pair(e3 << (8 * (a3 & 3) + bit)), b2 = or_pair(e2 << (8 * (a2 & 3) + bit));
-      if ((w & 1) == 0) {
-        atomicOr(&meta_k[a3 >> 2], b3);
-        atomicOr(&meta_k[a2 >> 2], b2);
-      }
-      if (w == 0) bytes_k[hif4_base_at(G, g, t, n) - 2048 * G] = (uint8_t)base;
-    }
-  }
-
-#pragma unroll
-  for (int i = 0; i < kItemsV; ++i) {
-    const int ch = 4 * (tid >> 3) + 128 * i;
-    if (ch >= D) break;
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      h2_t x[8], a4[2];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(h2_t, p ? in_v[i][e].y : in_v[i][e].x);
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-        a4[q] = hmax2(hmax2(habs2(x[4 * q]), habs2(x[4 * q + 1])), hmax2(habs2(x[4 * q + 2]), habs2(x[4 * q + 3])));
-      const u16x2_t a8u = __builtin_elementwise_max(as_u16(a4[0]), as_u16(a4[1]));
-      const h2_t top = __builtin_bit_cast(h2_t, reduce8(__builtin_bit_cast(uint32_t, a8u), max_pair16));
-      const uint32_t base[2] = {e6m2_ceil((float)top[0]), e6m2_ceil((float)top[1])};
-      const float r0 = hif4_rcp_step(base[0]), r1 = hif4_rcp_step(base[1]);
-      const h2_t f0 = range_floors(e6m2_value(base[0])), f1 = range_floors(e6m2_value(base[1]));
-      uint32_t acc[2] = {0, 0};            // four keys' nibbles per channel, in the two halves
-      uint32_t e2 = 0, e3[2];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u16x2_t lv, ne2;
-        block_levels(a4[q], __builtin_bit_cast(h2_t, a8u), h2_t{f0[0], f1[0]}, h2_t{f0[1], f1[1]}, lv, ne2);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[q] |= nibbles2(codes2(habs2(x[4 * q + e]), r0, r1, lv), x[4 * q + e]) << (4 * e);
-        e2 = 0x00010001u - __builtin_bit_cast(uint32_t, ne2);
-        e3[q] = 0x00020002u - __builtin_bit_cast(uint32_t, lv) - e2;
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = ch + 2 * p + e, tile = c >> 6, t = (c >> 4) & 3, n = c & 15;
-        const int lane = 16 * (w >> 1) + n, bit = 2 * t + (w & 1);
-        codes_v[hif4_code_at(tile, t, lane, w & 1) >> 2] =
-            __builtin_amdgcn_perm(acc[1], acc[0], e ? 0x07060302u : 0x05040100u);
-        const int a3 = hif4_e3_at(G, tile, lane, 0) - 2048 * G, a2 = hif4_e2_at(G, tile, lane) - 2048 * G;
-        const uint32_t both = ((e3[0] >> (16 * e)) & 1u) | ((e3[1] >> (16 * e)) & 1u) << (G == 1 ? 8 : 16);
-        const uint32_t b3 = or_pair(both << (8 * (a3 & 3) + bit));
-        const uint32_t b2 = or_pair(((e2 >> (16 * e)) & 1u) << (8 * (a2 & 3) + bit));
-        if ((w & 1) == 0) {
-          atomicOr(&meta_v[a3 >> 2], b3);
-          atomicOr(&meta_v[a2 >> 2], b2);
-        }
-        if (w == 0) bytes_v[hif4_base_at(G, tile, t, n) - 2048 * G] = (uint8_t)base[e];
-      }
-    }
+    append_v<G>(in, codes, meta[1], tile, lane);
   }
   __syncthreads();
   if (rec) {
     uint8_t* vp = rec + hif4_part(G);
-#pragma unroll
-    for (int i = tid; i < 2048 * G / 16; i += 256) {
-      reinterpret_cast<uint4*>(vp)[i] = reinterpret_cast<const uint4*>(codes_v)[i];
-      // of K the words of the new keys: 16 bytes are two keys' (t even, t odd)
-      const uint4 x = reinterpret_cast<const uint4*>(codes_k)[i];
-      const int t = 2 * ((i >> 6) & 1), ka = key_of(t, i & 15), kb = key_of(t + 1, i & 15);
-      const bool na = ka >= lo && ka < hi, nb = kb >= lo && kb < hi;
-      if (na && nb)
-        reinterpret_cast<uint4*>(rec)[i] = x;
-      else if (na)
-        reinterpret_cast<uint2*>(rec)[2 * i] = make_uint2(x.x, x.y);
-      else if (nb)
-        reinterpret_cast<uint2*>(rec)[2 * i + 1] = make_uint2(x.z, x.w);
-    }
-    for (int i = tid; i < kMeta / 4; i += 256) {
-      reinterpret_cast<uint32_t*>(rec + 2048 * G)[i] = meta_k[i];
-      reinterpret_cast<uint32_t*>(vp + 2048 * G)[i] = meta_v[i];
+    *reinterpret_cast<uint4*>(vp + 16 * tid) = *reinterpret_cast<const uint4*>(codes + padded(16 * tid));
+    if (tid < 2 * kMeta / 16) {
+      const int part = tid / (kMeta / 16), at = 16 * (tid % (kMeta / 16));
+      *reinterpret_cast<uint4*>((part ? vp : rec) + 2048 * G + at) = *reinterpret_cast<const uint4*>(&meta[part][at]);
     }
   }
   // The tail gets the last page's new rows.  The workgroup of the first page
@@ -272,7 +339,7 @@ __global__ void __launch_bounds__(256) k_paged_append(PagedAppend a, int blocks)
     const int last = (stop - 1) / kPage * kPage;              // place of the last page's first token
     const int from = max(nt.first - last, 0), to = stop - last;
     const long l0 = (long)nt.begin + last - nt.first;
-    for (int i = tid; i < (to - from) * (D / 8); i += 256) {
+    for (int i = tid; i < (to - from) * (D / 8); i += kThreads) {
       const int key = from + i / (D / 8), ch = 8 * (i % (D / 8));
       *reinterpret_cast<uint4*>(tail + (size_t)key * row + ch) =
           *reinterpret_cast<const uint4*>(a.v + (size_t)(l0 + key) * row + (size_t)it.head * D + ch);
@@ -381,11 +448,11 @@ hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st) {
       k_paged_append16<4><<<grid, 256, 0, st>>>(a, blocks);
   } else {
     if (a.c.D == 64)
-      k_paged_append<1><<<grid, 256, 0, st>>>(a, blocks);
+      k_paged_append<1><<<grid, 128, 0, st>>>(a, blocks);
     else if (a.c.D == 128)
       k_paged_append<2><<<grid, 256, 0, st>>>(a, blocks);
     else
-      k_paged_append<4><<<grid, 256, 0, st>>>(a, blocks);
+      k_paged_append<4><<<grid, 512, 0, st>>>(a, blocks);
   }
   return hipGetLastError();
 }
@@ -399,7 +466,6 @@ hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st) {
 // K from one word, eight keys of four channels of V from four.  A value is
 // u b/4 2^-(E2+E3), whole in fp32, rounded once.  Bound by HBM: mostly the
 // writes.
-__device__ __forceinline__ int padded(int at) { return at + (at >> 8) * 16; }
 
 // The eight values of word (lane, c) of row (t, n) of a part in LDS, in fp32.
 template <int G>

@@ -47,9 +47,9 @@ __device__ __forceinline__ uint32_t nibbles2(uint32_t u, h2_t x) {
 // reciprocal taken two units in the last place (ulps) down and up, the fp32
 // products bracket the exact quotient (two ulps exceed the reciprocal's half
 // ulp and the product's rounding together), so where both ends round to the
-// same fp16 the quotient does too.  `open` collects the bits in which they
-// differ (about one value in 2000): those take the exact division.
-__device__ __forceinline__ h2_t divide2(h2_t k, float r0, float r1, uint32_t& open) {
+// same fp16 the quotient does too.  `open`: the lanes in which they differ
+// (about one value in 2000).
+__device__ __forceinline__ h2_t divide2(h2_t k, float r0, float r1, unsigned long long& open) {
   const float d0 = __uint_as_float(__float_as_uint(r0) - 2u), u0 = __uint_as_float(__float_as_uint(r0) + 2u);
   const float d1 = __uint_as_float(__float_as_uint(r1) - 2u), u1 = __uint_as_float(__float_as_uint(r1) + 2u);
   float a, b, c, d;
@@ -60,24 +60,25 @@ __device__ __forceinline__ h2_t divide2(h2_t k, float r0, float r1, uint32_t& op
       : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
       : "v"(k), "v"(d0), "v"(d1), "v"(u0), "v"(u1));
   const h2_t lo = pack2_f16(a, b), hi = pack2_f16(c, d);
-  open |= __builtin_bit_cast(uint32_t, lo) ^ __builtin_bit_cast(uint32_t, hi);
+  open = __builtin_amdgcn_ballot_w64(__builtin_bit_cast(uint32_t, lo) != __builtin_bit_cast(uint32_t, hi));
   return lo;
 }
 
-// fp16(k/s) of N pairs: s and rs are the scales and their reciprocals.
-template <int N, typename S>
-__device__ __forceinline__ void divide_pairs(h2_t (&x)[N], const S& s, const S& rs) {
+// fp16(k/s) of N pairs: s and rs are the scales and their reciprocals.  A pair
+// that is open in any lane takes the exact division.
+template <int N, typename S, typename R>
+__device__ __forceinline__ void divide_pairs(h2_t (&x)[N], const S& s, const R& rs) {
   h2_t y[N];
-  uint32_t any = 0;
+  unsigned long long open[N], any = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) y[i] = divide2(x[i], rs[2 * i], rs[2 * i + 1], any);
-  if (__builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0, 0)) {
+  for (int i = 0; i < N; ++i) {
+    y[i] = divide2(x[i], rs[2 * i], rs[2 * i + 1], open[i]);
+    any |= open[i];
+  }
+  if (__builtin_expect(any != 0, 0)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint32_t open = 0;
-      divide2(x[i], rs[2 * i], rs[2 * i + 1], open);
-      if (open) y[i] = h2_t{div_rn16((float)x[i][0], s[2 * i]), div_rn16((float)x[i][1], s[2 * i + 1])};
-    }
+    for (int i = 0; i < N; ++i)
+      if (open[i]) y[i] = h2_t{div_rn16((float)x[i][0], s[2 * i]), div_rn16((float)x[i][1], s[2 * i + 1])};
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = y[i];

@@ -33,54 +33,64 @@ __host__ __device__ __forceinline__ int query_tiles(int hq, int hkv, bool fp16) 
   return (hq / hkv + per - 1) / per;
 }
 // How the pages are cut: into as many runs as give every SIMD the waves that
-// its registers hold.  Every sequence is cut into equal parts of at most
-// ceil(pages / target) pages, numbered densely over the sequences: at most
+// its registers hold (a page's K and V and, on their way, the next one's).
+// More runs than that wait for a place and are short: 8 x 32768 tokens, HIF4,
+// D=128, 63.7 us with two waves' runs a SIMD, 71, 73 and 77 with 3, 4 and 6;
+// fewer registers a wave for three waves spill (81).  At D=256 one wave: 39 us
+// for what two, with spills, take 47.  Every sequence is cut into equal parts
+// of at most ceil(units / target), numbered densely over the sequences: at most
 // target + batch runs.
 __host__ __device__ __forceinline__ int run_target(int hq, int hkv, int D, bool fp16) {
   const int waves = fp16 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : (D == 256 ? 1 : D == 128 ? 2 : 3);
   const int each = hkv * query_tiles(hq, hkv, fp16);
   return (1024 * waves + each - 1) / each;
 }
-__host__ __device__ __forceinline__ size_t run_slots(int batch, int target, int max_pages) {
-  const size_t all = (size_t)batch * max_pages, most = (size_t)target + batch;
+// Units of a page that runs are cut into: FP16 pages of D = 256 (64 KiB a head,
+// few a wave) in halves, keys 16k + 8c .. 16k + 8c + 7 in half c: 3 sequences
+// of 2000 tokens 19.0 to 16.9 us, 4 of 1000 to 8192 39.9 to 38.9.  At D=128 the
+// second half's turn costs more than the balance gives: 13.2 to 14.4 us.
+__host__ __device__ constexpr int page_units(int D, bool fp16) { return fp16 && D == 256 ? 2 : 1; }
+__host__ __device__ __forceinline__ size_t run_slots(const PagedCache& c, int target) {
+  const size_t all = (size_t)c.batch * c.max_pages * page_units(c.D, c.fp16), most = (size_t)target + c.batch;
   return all < most ? all : most;
 }
 struct Run {
-  int b, begin, end;              // pages [begin, end) of sequence b; b < 0: no such run
+  int b, begin, end;              // units [begin, end) of sequence b; b < 0: no such run
   int first, count;               // the sequence's runs: [first, first + count)
 };
 
 __device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
   return b < c.batch ? (paged_len(c, b) + kPage - 1) / kPage : 0;
 }
-// The sequences are dealt to the lanes of a wave (b, b + 64, ...), the pages of
+// The sequences are dealt to the lanes of a wave (b, b + 64, ...), the units of
 // a lane's first kHeldSeqs in registers.
 constexpr int kHeldSeqs = 4;
 struct Dealt {
   int n[kHeldSeqs];
 };
-// Sum of f(pages) over the sequences of each lane.
-template <typename F>
+// Sum of f(units) over the sequences of each lane.
+template <int kUnits, typename F>
 __device__ __forceinline__ int lane_sum(const PagedCache& c, const Dealt& d, int lane, F f) {
   int sum = f(d.n[0]);
 #pragma unroll
   for (int i = 1; i < kHeldSeqs; ++i)
     if (c.batch > 64 * i) sum += f(d.n[i]);
-  for (int b = 64 * kHeldSeqs + lane; b < c.batch; b += 64) sum += f(pages_of(c, b));
+  for (int b = 64 * kHeldSeqs + lane; b < c.batch; b += 64) sum += f(kUnits * pages_of(c, b));
   return sum;
 }
 // The run numbered r (found by a whole wave).  Runs are numbered lane by lane of the above.
+template <int kUnits>
 __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, int lane) {
   Dealt d;
 #pragma unroll
-  for (int i = 0; i < kHeldSeqs; ++i) d.n[i] = pages_of(c, 64 * i + lane);
-  int mine = lane_sum(c, d, lane, [](int n) { return n; }), upto = wave_scan(mine), per = 1;
+  for (int i = 0; i < kHeldSeqs; ++i) d.n[i] = kUnits * pages_of(c, 64 * i + lane);
+  int mine = lane_sum<kUnits>(c, d, lane, [](int n) { return n; }), upto = wave_scan(mine), per = 1;
   const int total = __builtin_amdgcn_readlane(upto, 63);
   if (total > target) {
     per = (total + target - 1) / target;
     // the last runs of the sequences are shorter: longer runs until all fit into one round (or nearly)
     for (int i = 0;; ++i) {
-      mine = lane_sum(c, d, lane, [per](int n) { return (n + per - 1) / per; });
+      mine = lane_sum<kUnits>(c, d, lane, [per](int n) { return (n + per - 1) / per; });
       upto = wave_scan(mine);
       const int runs = __builtin_amdgcn_readlane(upto, 63);
       if (runs <= target || i == 6 || c.batch >= target) break;
@@ -97,11 +107,11 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, 
                   : i == 1 ? __builtin_amdgcn_readlane(d.n[1], src)
                   : i == 2 ? __builtin_amdgcn_readlane(d.n[2], src)
                   : i == 3 ? __builtin_amdgcn_readlane(d.n[3], src)
-                           : __builtin_amdgcn_readfirstlane(pages_of(c, b));
+                           : __builtin_amdgcn_readfirstlane(kUnits * pages_of(c, b));
     out.count = (n + per - 1) / per;
     if (r < out.first + out.count) {
       const int k = r - out.first, some = n / out.count, more = n % out.count;
-      out.b = b;                       // the first runs get one page more where the count does not divide
+      out.b = b;                       // the first runs get one unit more where the count does not divide
       out.begin = k * some + min(k, more);
       out.end = out.begin + some + (k < more);
       return out;
@@ -113,7 +123,7 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int target, int r, 
 
 // Workspace: o [slots][hq][D], then (m, l) [slots][hq], the runs (first, count)
 // of each sequence that has any, then with page weights (m, sum)
-// [batch][max_pages][hq]; m in log2 units.
+// [batch][max_pages * units][hq]; m in log2 units.
 struct DecodeWs {
   float* o;
   float2* ml;
@@ -121,7 +131,7 @@ struct DecodeWs {
   float2* page;
 };
 __host__ __device__ __forceinline__ DecodeWs decode_ws(uint8_t* ws, const PagedCache& c, int target, int hq) {
-  const size_t slots = run_slots(c.batch, target, c.max_pages);
+  const size_t slots = run_slots(c, target);
   DecodeWs w;
   w.o = reinterpret_cast<float*>(ws);
   w.ml = reinterpret_cast<float2*>(w.o + slots * hq * c.D);
@@ -130,8 +140,8 @@ __host__ __device__ __forceinline__ DecodeWs decode_ws(uint8_t* ws, const PagedC
   return w;
 }
 size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights) {
-  const size_t slots = run_slots(c.batch, run_target(hq, c.hkv, c.D, c.fp16), c.max_pages);
-  return slots * hq * (c.D + 2) * 4 + (size_t)c.batch * 8 + (weights ? (size_t)c.batch * c.max_pages * hq * 8 : 0);
+  const size_t slots = run_slots(c, run_target(hq, c.hkv, c.D, c.fp16));
+  return slots * hq * (c.D + 2) * 4 + (size_t)c.batch * 8 + (weights ? (size_t)c.batch * c.max_pages * page_units(c.D, c.fp16) * hq * 8 : 0);
 }
 
 // q s to fp16, the exact product rounded once: the fp32 product made odd where
@@ -172,6 +182,11 @@ __device__ __forceinline__ half_t round_product(half_t q, float s) {
 // exchanged, which makes the words of FP4 lanes j and 2 + j the keys whose
 // scores lanes 2j and 2j + 1 have: one exchange between neighbouring rows of
 // 16 lanes brings p into place.
+//
+// Bound by the reads of the pages: 8 x 32768 tokens, 8 kv heads, D=128 (302
+// MB) in 58 us, 5.2 TB/s, where a plain read of as much reaches 5.6.  Mixed
+// lengths (32 of 300 to 8192, 165 MB) take 39 us, 4.2 TB/s: about 3 us until
+// the first page is there, and 10% for runs of unequal length.
 constexpr int kFp4 = 4, kFp8 = 0;            // operand formats of the instruction
 // The reference of the softmax is a whole power of two and moves only when a
 // page's largest score passes it by this many binades: fp32 sums do not mind.
@@ -350,9 +365,9 @@ __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0)
 struct Pages {
   int mine, base;
 };
-__device__ __forceinline__ void load_pages(Pages& p, const PagedCache& c, const Run& r, int from, int lane) {
+__device__ __forceinline__ void load_pages(Pages& p, const PagedCache& c, int b, int from, int last, int lane) {
   p.base = from;
-  p.mine = from + lane < r.end ? c.table[(size_t)r.b * c.max_pages + from + lane] : -1;
+  p.mine = from + lane <= last ? c.table[(size_t)b * c.max_pages + from + lane] : -1;
 }
 
 // The digits of four query heads' rows (q: the first of them, `rows` exist) in
@@ -429,7 +444,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
   const int target = run_target(a.hq, a.c.hkv, D, false);
-  const Run run = find_run(a.c, target, r, lane);
+  const Run run = find_run<page_units(D, false)>(a.c, target, r, lane);
   if (run.b < 0) return;
   const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
   const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
@@ -439,12 +454,12 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
   const int q_in = 4 * tile + (n >> 2), h = head * group + q_in;
 
   Pages pg;
-  load_pages(pg, a.c, run, run.begin, lane);
+  load_pages(pg, a.c, run.b, run.begin, run.end - 1, lane);
   bool has, has_next = false;
   // The record of page j; of a page that is none the pool's first, whose keys are all masked then.
   const auto record = [&](int j, bool& there) -> const uint8_t* {
     if (j - pg.base >= 64) {
-      load_pages(pg, a.c, run, j, lane);
+      load_pages(pg, a.c, run.b, j, run.end - 1, lane);
       asm volatile("" : "+v"(pg.mine));  // waited for here: else every page's look-up would wait for all loads
     }
     const int page = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
@@ -601,40 +616,44 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
 // would round a row that rests on one key by 2^-12 more than its output is
 // rounded anyway), scaled so that the heaviest key so far lies between 2^7 and
 // 2^15: small weights stay above fp16's subnormals down to 2^-21 of it.
+// Bound by the reads: D=128, 8 x 8192 tokens (268 MB) in 52 us, 5.2 TB/s.
 typedef half_t h8v_t __attribute__((ext_vector_type(8)));
 typedef half_t h4v_t __attribute__((ext_vector_type(4)));
 constexpr float kTop16 = 7.0f, kSlack16 = 8.0f;
 
-template <int N>
+template <int N, int kStep>
 __device__ __forceinline__ void load_operands(h8v_t (&x)[N], const uint8_t* p, uint32_t lane) {
+  constexpr int kSome = 4096 / kStep;
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const global_ptr at = scalar_address(p + 1024 * i);
+  for (int i = 0; i < N; i += kSome) {
+    const global_ptr at = scalar_address(p + kStep * i);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[i + u] = load_at<h8v_t>(at, 16 * lane + 1024 * u);
+    for (int u = 0; u < kSome; ++u) x[i + u] = load_at<h8v_t>(at, 16 * lane + kStep * u);
   }
 }
 
 template <int G>
 __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(PagedDecode a, int tiles) {
-  constexpr int D = 64 * G;
+  constexpr int D = 64 * G, kUnits = page_units(D, true), kT = 4 / kUnits, kC = 2 / kUnits;
   const int lane = threadIdx.x, n = lane & 15, k = lane >> 4;
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
   const int target = run_target(a.hq, a.c.hkv, D, true);
-  const Run run = find_run(a.c, target, r, lane);
+  const Run run = find_run<kUnits>(a.c, target, r, lane);
   if (run.b < 0) return;
   const int len = __builtin_amdgcn_readfirstlane(paged_len(a.c, run.b));
   const DecodeWs ws = decode_ws(a.ws, a.c, target, a.hq);
   if (r == run.first && head == 0 && tile == 0 && lane == 0) ws.runs[run.b] = make_int2(run.first, run.count);
   const int q_in = 16 * tile + n, h = head * group + q_in;
 
+  const int last = (run.end - 1) / kUnits;
   Pages pg;
-  load_pages(pg, a.c, run, run.begin, lane);
+  load_pages(pg, a.c, run.b, run.begin / kUnits, last, lane);
   bool has, has_next = false;
-  const auto record = [&](int j, bool& there) -> const uint8_t* {
+  const auto record = [&](int unit, bool& there) -> const uint8_t* {
+    const int j = unit / kUnits;
     if (j - pg.base >= 64) {
-      load_pages(pg, a.c, run, j, lane);
+      load_pages(pg, a.c, run.b, j, last, lane);
       asm volatile("" : "+v"(pg.mine));  // waited for here: else every page's look-up would wait for all loads
     }
     const int page = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
@@ -655,47 +674,56 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
 #pragma unroll
       for (int i = 0; i < 8; ++i) q[c][i] = round_product(q[c][i], i < 4 ? s0[i & 3] : s1[i & 3]);
     }
-  h8v_t kr[8 * G], vr[8 * G];          // K [t][D/32], V [D/16][c]
+  h8v_t kr[2 * G * kT], vr[4 * G * kC];    // K [t][D/32], V [D/16][c]
   const uint8_t* rec = record(run.begin, has);
-  load_operands(kr, rec, lane);
-  load_operands(vr, rec + 128 * D, lane);
+  // a unit's part of a record: half of K's rows, every other KiB of V
+  const auto load_k = [&](const uint8_t* from, int j) {
+    load_operands<2 * G * kT, 1024>(kr, from + j % kUnits * 64 * D, lane);
+  };
+  const auto load_v = [&](const uint8_t* from, int j) {
+    load_operands<4 * G * kC, 1024 * kUnits>(vr, from + 128 * D + j % kUnits * 1024, lane);
+  };
+  load_k(rec, run.begin);
+  load_v(rec, run.begin);
   float ref = -1e30f, l = 0.0f;            // p = 2^(score - ref + kTop16), scores in log2 units
   f4v_t o[4 * G];
 #pragma unroll
   for (int c = 0; c < 4 * G; ++c) o[c] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 
   for (int j = run.begin; j < run.end; ++j) {
-    f4v_t s[4];
+    f4v_t s[kT];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < kT; ++t) s[t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int c = 0; c < 2 * G; ++c)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[2 * G * t + c], q[c], s[t], 0, 0, 0);
-    const uint8_t* next = record(min(j + 1, run.end - 1), has_next);
-    load_operands(kr, next, lane);
+      for (int t = 0; t < kT; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[2 * G * t + c], q[c], s[t], 0, 0, 0);
+    const int j2 = min(j + 1, run.end - 1);
+    const uint8_t* next = record(j2, has_next);
+    load_k(next, j2);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] *= a.scale;
-    const int held = has ? len - j * kPage : 0;
+    for (int t = 0; t < kT; ++t) s[t] *= a.scale;
+    const int held = has ? len - j / kUnits * kPage : 0;
+    const int first = 16 * k + 8 * (j % kUnits);     // the lane's first key in the page
     if (held < kPage) {
       asm volatile("");                  // (kept a branch)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < kT; ++t)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          if (16 * k + 4 * t + v >= held) s[t][v] = -INFINITY;
+          if (first + 4 * t + v >= held) s[t][v] = -INFINITY;
       // what lies in the page behind the last token may be anything: 0 times it has to be 0
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < kC; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (16 * k + 8 * c + i >= held)
+          if (first + 8 * c + i >= held)
 #pragma unroll
-            for (int u = 0; u < 4 * G; ++u) vr[2 * u + c][i] = (half_t)0;
+            for (int u = 0; u < 4 * G; ++u) vr[kC * u + c][i] = (half_t)0;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < kT; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v) top = fmaxf(top, s[t][v]);
     if (__builtin_amdgcn_ballot_w64(top > ref + kSlack16)) {
@@ -706,9 +734,9 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
       for (int c = 0; c < 4 * G; ++c) o[c] *= f;
     }
     float sum = 0.0f;
-    h8v_t hi[2], lo[2];
+    h8v_t hi[kC], lo[kC];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < kT; ++t) {
       f4v_t p;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
@@ -727,16 +755,16 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
     if (a.w_in) {
       const float all = sum_across_rows(sum);
       if (k == 0 && q_in < group)
-        ws.page[((size_t)run.b * a.c.max_pages + j) * a.hq + h] = make_float2(ref - kTop16, all);
+        ws.page[((size_t)run.b * a.c.max_pages * kUnits + j) * a.hq + h] = make_float2(ref - kTop16, all);
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < kC; ++c)
 #pragma unroll
       for (int u = 0; u < 4 * G; ++u) {
-        o[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vr[2 * u + c], lo[c], o[u], 0, 0, 0);
-        o[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vr[2 * u + c], hi[c], o[u], 0, 0, 0);
+        o[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vr[kC * u + c], lo[c], o[u], 0, 0, 0);
+        o[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vr[kC * u + c], hi[c], o[u], 0, 0, 0);
       }
-    load_operands(vr, next + 128 * D, lane);
+    load_v(next, j2);
     has = has_next;
   }
 
@@ -753,6 +781,9 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
 // o = sum o_i 2^(m_i - m) / l, l = sum l_i 2^(m_i - m).  One workgroup per row
 // and kWidth channels (a row's channels are shared out where there are few
 // rows); behind those, with page weights, one per 16 pages of a sequence.
+// Bound by latency: 4 to 5 us, most of it the launch, two dependent reads and
+// the sets' sum (as a part of the runs' kernel, by the last wave of a row, it
+// took longer: one wave then walks all of them).
 constexpr int kJoin = 256, kPagesJoined = 16, kShare = kJoin / kPagesJoined;
 
 // (first, count) of a sequence's runs; the runs kernel wrote those of sequences with pages.
@@ -826,6 +857,7 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
   const int chunks = (a.c.max_pages + kPagesJoined - 1) / kPagesJoined, at = blockIdx.x - rows;
   const int b = at / chunks, j0 = kPagesJoined * (at % chunks), wave = tid >> 6;
   const int pages = pages_of(a.c, b), j = j0 + tid / kShare;
+  const int units = page_units(D, a.c.fp16);
   const size_t place = (size_t)b * a.c.max_pages + min(j, a.c.max_pages - 1);
   const float before = a.w_in[place];
   float w = 0.0f;
@@ -836,7 +868,7 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
 #pragma unroll
       for (int i = 0; i < 64 / kShare; ++i) {
         const int h = h0 + tid % kShare + kShare * i;
-        y[i] = j < pages && h < a.hq ? ws.page[place * a.hq + h] : make_float2(0.0f, 0.0f);
+        y[i] = j < pages && h < a.hq ? ws.page[place * units * a.hq + h] : make_float2(0.0f, 0.0f);
       }
       float m = -INFINITY, l = 0.0f;
       if (h0 + lane < a.hq)
@@ -862,6 +894,11 @@ __global__ void __launch_bounds__(kJoin) k_paged_join(PagedDecode a, int rows) {
       for (int i = 0; i < 64 / kShare; ++i) {
         const float2 x = joined[0][tid % kShare + kShare * i];
         w += y[i].y * __builtin_amdgcn_exp2f(y[i].x - x.x) * x.y;
+        const int h = h0 + tid % kShare + kShare * i;
+        if (units == 2 && j < pages && h < a.hq) {
+          const float2 z = ws.page[(place * 2 + 1) * a.hq + h];
+          w += z.y * __builtin_amdgcn_exp2f(z.x - x.x) * x.y;
+        }
       }
       __syncthreads();
     }
@@ -884,7 +921,7 @@ bool paged_decode_fits(const PagedCache& c, int hq, bool weights) {
 
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {
   const int tiles = query_tiles(a.hq, a.c.hkv, a.c.fp16);
-  const size_t runs = run_slots(a.c.batch, run_target(a.hq, a.c.hkv, a.c.D, a.c.fp16), a.c.max_pages);
+  const size_t runs = run_slots(a.c, run_target(a.hq, a.c.hkv, a.c.D, a.c.fp16));
   const dim3 grid((unsigned)(runs * a.c.hkv * tiles));
   if (a.c.fp16) {
     if (a.c.D == 64)

@@ -103,6 +103,13 @@ def test_decode_many_rows(fmt):
 
 
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_decode_few_keys_in_the_last_page(fmt, d):
+    """Last pages of which a half, or all but a few of a lane's keys, are empty; pages that are none."""
+    _decode_case(17, [8, 9, 72, 73, 136, 0, 56, 201], 4, 2, d, FMT[fmt], weights=True, holes=True)
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_decode_long(fmt, d):
     """Runs of one page and of many."""

@@ -359,7 +359,8 @@ hifa4_status hifa4_decode_fwd(const hifa4_problem* p, const hifa4_fwd_options* o
  *                hifa4_paged_append for HIFA4_OPERANDS_HIF4 (a group of V^ is
  *                quantized again when a token joins it); may be NULL otherwise
  *                and for the other entry points.
- * head_dim is 64, 128 or 256.  Every entry point reads the table and the
+ * head_dim is 64, 128 or 256.  Calls of more pages than one launch holds (2^24
+ * workgroups; batch * max_pages reaches 2^30) are refused.  Every entry point reads the table and the
  * lengths on the device, enqueues a fixed number of kernels whose grid follows
  * from host values alone, and may be captured into a graph and replayed with
  * other lengths and tables. */
@@ -424,7 +425,10 @@ size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t nu
  * head_dim]), lse = log sum_j exp(S_j) (DEVICE fp32 [num_heads_q, batch]).
  * Unlike hifa4_decode_fwd, which repeats a row of the prefill code for code,
  * only the cache is quantized here: a step's time is the cache's bytes, and
- * the query, the scores, the softmax state (fp32) and p keep their precision.
+ * the query, the scores, the softmax state (fp32) and p keep their precision (on
+ * HIF4 pages the query's values and p enter the products as whole numbers,
+ * rounded by at most 2^-19 of the largest of their 64: a group's channels, a
+ * page's keys; on FP16 pages p as the sum of two fp16 values).
  * Sequences without tokens get o = 0 and lse = -inf.
  * page_weights (DEVICE fp32 [batch, max_pages], may be NULL): then
  * weights_out[b][j] = decay * page_weights[b][j] + the sum of p over every

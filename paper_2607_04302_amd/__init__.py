@@ -627,7 +627,7 @@ def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_toke
     else:
         _shaped(k, torch.float16, shape, dev, "k")
     if v is None:
-        v = torch.empty(shape, dtype=torch.float16, device=dev)
+        v = torch.empty_like(k)
     else:
         _shaped(v, torch.float16, shape, dev, "v")
     _paged_call("hifa4_paged_gather", dev, cache._ref, total_tokens, max_tokens, cu_tokens.data_ptr(),

@@ -359,7 +359,9 @@ __device__ __forceinline__ int fp16_v_at(int D, int w, int ch) {
 // Append, FP16: the new tokens' K~ and V go to their places in the record.  A
 // thread takes eight channels of a key of K, and eight keys of four channels
 // of V, which it transposes in registers: all accesses but those of a page's
-// unfinished sets of eight keys are 16 bytes wide (8 for V's rows).
+// unfinished sets of eight keys are 16 bytes wide (8 for V's rows).  Bound by
+// HBM: 16 prompts of 512 to 2048 tokens, 8 heads, D=256 (342 MB) in 81 us, 4.2
+// TB/s.
 template <int G>
 __global__ void __launch_bounds__(256) k_paged_append16(PagedAppend a, int blocks) {
   constexpr int D = 64 * G, kK = 2 * G, kV = (G + 1) / 2;
@@ -464,8 +466,9 @@ hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st) {
 // one sweep, padded by 16 bytes per 256 so that the four lanes of a row and
 // the tiles lie in different banks; a thread makes eight channels of a key of
 // K from one word, eight keys of four channels of V from four.  A value is
-// u b/4 2^-(E2+E3), whole in fp32, rounded once.  Bound by HBM: mostly the
-// writes.
+// u b/4 2^-(E2+E3), whole in fp32, rounded once.  Bound by HBM, mostly the
+// writes: 32 sequences of 300 to 8192 tokens, 8 heads, D=128, HIF4 (750 MB) in
+// 153 us, 4.9 TB/s.
 
 // The eight values of word (lane, c) of row (t, n) of a part in LDS, in fp32.
 template <int G>
@@ -590,7 +593,8 @@ hipError_t launch_paged_gather(const PagedGather& a, hipStream_t st) {
 // digit by digit (8 bits at a time, by counts in LDS), then one pass over the
 // places moves what stays and lists what leaves, both in order.  The first
 // 2048 places' weights and pages are read once, into registers.  Bound by
-// latency: four counts and one pass, three barriers each.
+// latency: four counts and one pass, three barriers each, 5.5 us for 8 sequences
+// of 512 pages, 7.0 for 64 of up to 2048.
 constexpr int kEvictThreads = 1024, kEvictHeld = 2;
 
 // Order of the weights as unsigned integers; NaN below everything, -0 as 0.

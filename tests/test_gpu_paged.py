@@ -147,6 +147,32 @@ def test_decode_small_weights_count(fmt, rising):
 
 
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_decode_not_finite(fmt, d):
+    """A NaN or infinity in a query makes its own row NaN and no other; one in an FP16 page those of its head alone,
+    and none behind the last token."""
+    rng = np.random.default_rng(31)
+    lens, hq, hkv = [150, 40, 9], 10, 2
+    k, v, _ = _sequences(rng, lens, hkv, d, False)
+    table, num = _table(rng, lens)
+    pool = P.fill_pool(k, v, table, lens, num, FMT[fmt], junk=rng)
+    q = rng.standard_normal((3, hq, d)).astype(np.float16)
+    ro, rl, _, bo, bl, _ = P.decode(q, pool, table, lens, FMT[fmt])
+    bad = np.zeros((3, hq), bool)
+    for b, head, ch, x in ((0, 1, 3, np.nan), (1, 7, d - 1, np.inf), (2, 9, 0, -np.inf)):
+        q[b, head, ch] = x
+        bad[b, head] = True
+    if fmt == "fp16":
+        pool[table[0, 1], 1].view(np.float16)[P.fp16_places(d, 0)[5, 7]] = np.nan
+        bad[0, hq // hkv:] = True
+    o, lse = h.hifa4_paged_decode_fwd(_cache(pool, table, lens, d, FMT[fmt]), to_gpu(q))
+    o, lse = to_np(o), to_np(lse)
+    assert np.isnan(o[bad]).all() and np.isnan(lse.T[bad]).all()
+    assert (np.abs(o[~bad] - ro[~bad]) <= bo[~bad]).all()
+    assert (np.abs(lse.T[~bad] - rl.T[~bad]) <= bl.T[~bad]).all()
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 def test_decode_pages_that_are_none(fmt):
     _decode_case(8, [300, 200, 640, 100], 4, 2, 128, FMT[fmt], weights=True, holes=True)
 

@@ -328,9 +328,10 @@ hifa4_status check_page_grid(const hifa4_paged_cache* c, int32_t tokens, const c
                 tokens, c->batch);
   return HIFA4_OK;
 }
-hifa4_status check_join_grid(const hifa4::PagedCache& c, int32_t hq, bool weights) {
+hifa4_status check_decode_grid(const hifa4::PagedCache& c, int32_t hq, bool weights) {
   if (!hifa4::paged_decode_fits(c, hq, weights))
-    return fail(HIFA4_ERR_UNSUPPORTED, "page weights of %d x %d pages are too many for one launch", c.batch, c.max_pages);
+    return fail(HIFA4_ERR_UNSUPPORTED, "%d x %d pages%s are too many for one launch", c.batch, c.max_pages,
+                weights ? " with page weights" : "");
   return HIFA4_OK;
 }
 
@@ -394,7 +395,7 @@ hifa4_status hifa4_paged_gather(const hifa4_paged_cache* c, int32_t total_tokens
 size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q, int32_t page_weights) {
   hifa4::PagedCache pc;
   if (check_paged(c, false, &pc) != HIFA4_OK || check_query_heads(num_heads_q, c->batch, c->num_heads_kv) != HIFA4_OK ||
-      check_join_grid(pc, num_heads_q, page_weights != 0) != HIFA4_OK)
+      check_decode_grid(pc, num_heads_q, page_weights != 0) != HIFA4_OK)
     return 0;
   return hifa4::paged_decode_workspace(pc, num_heads_q, page_weights != 0);
 }
@@ -406,7 +407,7 @@ hifa4_status hifa4_paged_decode_fwd(const hifa4_paged_cache* c, int32_t num_head
   hifa4_status st = check_paged(c, true, &a.c);
   if (st != HIFA4_OK) return st;
   if ((st = check_query_heads(num_heads_q, c->batch, c->num_heads_kv)) != HIFA4_OK) return st;
-  if ((st = check_join_grid(a.c, num_heads_q, page_weights != nullptr)) != HIFA4_OK) return st;
+  if ((st = check_decode_grid(a.c, num_heads_q, page_weights != nullptr)) != HIFA4_OK) return st;
   if (!q || !o || !lse) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
   if ((page_weights == nullptr) != (weights_out == nullptr))
     return fail(HIFA4_ERR_INVALID_ARGUMENT, "page_weights and weights_out must both be set or both be NULL");

@@ -124,7 +124,7 @@ struct PagedDecode {
 // a grid in 32 bits.
 constexpr size_t kMaxGrid = (size_t)1 << 24;
 
-// Whether the join's grid is a launch.
+// Whether the pages can be counted and the join's grid is a launch.
 bool paged_decode_fits(const PagedCache& c, int hq, bool weights);
 size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights);
 

@@ -916,7 +916,8 @@ static int join_rows(const PagedCache& c, int hq) {
 static int join_pages(const PagedCache& c) { return c.batch * ((c.max_pages + kPagesJoined - 1) / kPagesJoined); }
 
 bool paged_decode_fits(const PagedCache& c, int hq, bool weights) {
-  return (size_t)join_rows(c, hq) + (weights ? join_pages(c) : 0) < kMaxGrid;
+  return (size_t)c.batch * c.max_pages * page_units(c.D, c.fp16) < (size_t)1 << 30 &&      // find_run counts in 32 bits
+         (size_t)join_rows(c, hq) + (weights ? join_pages(c) : 0) < kMaxGrid;
 }
 
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st) {

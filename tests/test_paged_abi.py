@@ -140,6 +140,10 @@ def test_launches_that_are_too_large_are_refused(lib):
     assert lib.hifa4_paged_decode_workspace_bytes(ctypes.byref(wide), 4, 0) > 0
     assert _decode(lib, wide, ws=None) == -3                             # (no weights: that many pages are fine)
     assert _evict(lib, batch=1 << 22, mp=4) == -2
+    # pages that runs take in halves: half as many
+    halves = dict(batch=1 << 8, max_pages=1 << 21, operands=h.OPERANDS_FP16)
+    assert _decode(lib, _cache(head_dim=256, **halves)) == -2
+    assert _decode(lib, _cache(head_dim=128, **halves), ws=None) == -3
 
 
 def test_counts_beyond_32_bits_are_refused(lib):

@@ -615,7 +615,9 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
 // p enters that product as the sum of two fp16 values (22 bits; one alone
 // would round a row that rests on one key by 2^-12 more than its output is
 // rounded anyway), scaled so that the heaviest key so far lies between 2^7 and
-// 2^15: small weights stay above fp16's subnormals down to 2^-21 of it.
+// 2^15: small weights stay above fp16's subnormals down to 2^-21 of it.  What p
+// counts from is held itself, not the score 7 binades above it: of scores over
+// 2^24 that difference is no number, and p would pass fp16's range.
 // Bound by the reads: D=128, 8 x 8192 tokens (268 MB) in 52 us, 5.2 TB/s.
 typedef half_t h8v_t __attribute__((ext_vector_type(8)));
 typedef half_t h4v_t __attribute__((ext_vector_type(4)));
@@ -685,7 +687,7 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
   };
   load_k(rec, run.begin);
   load_v(rec, run.begin);
-  float ref = -1e30f, l = 0.0f;            // p = 2^(score - ref + kTop16), scores in log2 units
+  float ref = -1e30f, l = 0.0f;            // p = 2^(score - ref), scores in log2 units
   f4v_t o[4 * G];
 #pragma unroll
   for (int c = 0; c < 4 * G; ++c) o[c] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -726,8 +728,8 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
     for (int t = 0; t < kT; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v) top = fmaxf(top, s[t][v]);
-    if (__builtin_amdgcn_ballot_w64(top > ref + kSlack16)) {
-      const float to = fmaxf(ref, max_across_rows(top)), f = __builtin_amdgcn_exp2f(ref - to);
+    if (__builtin_amdgcn_ballot_w64(top - ref > kTop16 + kSlack16)) {
+      const float to = fmaxf(ref, max_across_rows(top) - kTop16), f = __builtin_amdgcn_exp2f(ref - to);
       ref = to;
       l *= f;
 #pragma unroll
@@ -740,7 +742,7 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
       f4v_t p;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        p[v] = __builtin_amdgcn_exp2f(s[t][v] - (ref - kTop16));
+        p[v] = __builtin_amdgcn_exp2f(s[t][v] - ref);
         sum += p[v];
       }
       const h4v_t a4 = __builtin_convertvector(p, h4v_t);
@@ -755,7 +757,7 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
     if (a.w_in) {
       const float all = sum_across_rows(sum);
       if (k == 0 && q_in < group)
-        ws.page[((size_t)run.b * a.c.max_pages * kUnits + j) * a.hq + h] = make_float2(ref - kTop16, all);
+        ws.page[((size_t)run.b * a.c.max_pages * kUnits + j) * a.hq + h] = make_float2(ref, all);
     }
 #pragma unroll
     for (int c = 0; c < kC; ++c)
@@ -773,7 +775,7 @@ __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(P
   const size_t slot = (size_t)r * a.hq + h;
 #pragma unroll
   for (int c = 0; c < 4 * G; ++c) *reinterpret_cast<f4v_t*>(ws.o + slot * D + 16 * c + 4 * k) = o[c];
-  if (k == 0) ws.ml[slot] = make_float2(l == 0.0f ? -INFINITY : ref - kTop16, l);
+  if (k == 0) ws.ml[slot] = make_float2(l == 0.0f ? -INFINITY : ref, l);
 }
 
 // ---------------------------------------------------------------------------

@@ -542,7 +542,10 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     // the page's own reference: the next whole number above its largest score
     // (far below ref, where nothing of the page counts, 100 binades are enough)
     const float own = fmaxf(ceilf(top), ref - 100.0f);
-    if (__builtin_amdgcn_ballot_w64(own > ref + kSlack)) {
+    // 2^low counts 1 in the page's sums; beside numbers over 2^26 it may be own
+    // or own - 8 (p, a power of two there, is then at most 1 or 256)
+    const float low = own - 4.0f;
+    if (__builtin_amdgcn_ballot_w64(own - ref > kSlack)) {
       const float to = fmaxf(ref, own), f = __builtin_amdgcn_exp2f(ref - to);
       ref = to;
       l *= f;
@@ -554,21 +557,21 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     float sum = 0.0f, d[4][4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const float p = __builtin_amdgcn_exp2f(x[v] - (own - 4.0f));      // 16 p, at most 16
+      const float p = __builtin_amdgcn_exp2f(x[v] - low);      // 16 p, at most 16
       sum += p;
       digits(p, d[v]);
     }
     // every lane's digits to the lanes that need them: of its query's 16 keys and of the next row's
 #pragma unroll
     for (int i = 0; i < 4; ++i) pd[k][16 * (n >> 2) + 4 * i + piece] = fp8x4(d[0][i], d[1][i], d[2][i], d[3][i]);
-    // 2^(own - ref - 4): what the page's sums count
-    const int up = (int)(own - ref) - 4;
+    // 2^up: what the page's sums count (ref - 100 may lie 128 below ref)
+    const int up = max((int)(low - ref), -104);
     l = fmaf(sum, __uint_as_float((uint32_t)(127 + up) << 23), l);
     const uint32_t p_scale = (uint32_t)(127 + up - 5 * piece);
     if (a.w_in) {
       const float all = sum_across_rows(sum_pieces(sum));
       if (k == 0 && piece == 0 && q_in < group)
-        ws.page[((size_t)run.b * a.c.max_pages + j) * a.hq + h] = make_float2(own - 4.0f, all);
+        ws.page[((size_t)run.b * a.c.max_pages + j) * a.hq + h] = make_float2(low, all);
     }
     const uint4 pe = *reinterpret_cast<const uint4*>(&pd[k & 2][4 * n]);
     const uint4 po = *reinterpret_cast<const uint4*>(&pd[(k & 2) + 1][4 * n]);

@@ -35,7 +35,7 @@ def _call(pool, table, lens, q, fmt, copies=1, weights=None, decay=1.0, s=None):
     return o[:, 0], lse[0], None if w is None else to_np(w)
 
 
-@pytest.mark.parametrize("fmt,d,batch", [("fp16", 64, 24), ("fp16", 128, 16), ("fp16", 256, 8)])
+@pytest.mark.parametrize("fmt,d,batch", [("fp16", 64, 24), ("fp16", 128, 16), ("fp16", 256, 8), ("hif4", 128, 16), ("hif4", 256, 8)])
 @pytest.mark.parametrize("size", [2 ** 24, 2 ** 25, 2 ** 26, 2 ** 27, 2 ** 29, 2 ** 30])
 def test_scores_of_millions(fmt, d, batch, size):
     """Scores whose fp32 steps are 2 binades and more, so that a reference some binades beside one is no number:

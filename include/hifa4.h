@@ -360,10 +360,11 @@ hifa4_status hifa4_decode_fwd(const hifa4_problem* p, const hifa4_fwd_options* o
  *                quantized again when a token joins it); may be NULL otherwise
  *                and for the other entry points.
  * head_dim is 64, 128 or 256.  Calls of more pages than one launch holds (2^24
- * workgroups; batch * max_pages reaches 2^30) are refused.  Every entry point reads the table and the
- * lengths on the device, enqueues a fixed number of kernels whose grid follows
- * from host values alone, and may be captured into a graph and replayed with
- * other lengths and tables. */
+ * workgroups, 2^23 for an append to HIF4 pages of head_dim 256: a grid's threads
+ * are counted in 32 bits; batch * max_pages reaches 2^30) are refused.  Every
+ * entry point reads the table and the lengths on the device, enqueues a fixed
+ * number of kernels whose grid follows from host values alone, and may be
+ * captured into a graph and replayed with other lengths and tables. */
 typedef struct {
   int32_t batch;
   int32_t num_heads_kv;

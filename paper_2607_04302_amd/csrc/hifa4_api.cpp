@@ -319,11 +319,11 @@ hifa4_status check_query_heads(int32_t hq, int32_t batch, int32_t hkv) {
   return HIFA4_OK;
 }
 
-// workgroups of a launch over (sequence, page, head)
-hifa4_status check_page_grid(const hifa4_paged_cache* c, int32_t tokens, const char* bound) {
+// workgroups of `threads` threads of a launch over (sequence, page, head)
+hifa4_status check_page_grid(const hifa4_paged_cache* c, int32_t tokens, int threads, const char* bound) {
   const int64_t blocks = ((int64_t)tokens + 62) / 64 + 1;
   if ((int64_t)c->batch * c->num_heads_kv >= (1LL << 31) ||
-      (size_t)(blocks * c->batch * c->num_heads_kv) >= hifa4::kMaxGrid)
+      (size_t)(blocks * c->batch * c->num_heads_kv) >= hifa4::max_grid(threads))
     return fail(HIFA4_ERR_UNSUPPORTED, "too many pages for one launch (%s of %d tokens for each of %d sequences)", bound,
                 tokens, c->batch);
   return HIFA4_OK;
@@ -357,7 +357,7 @@ hifa4_status hifa4_paged_append(const hifa4_paged_cache* c, int32_t total_new, i
   if ((st = check_aligned16({k, v, s})) != HIFA4_OK) return st;
   if ((st = check_aligned4({cu_new})) != HIFA4_OK) return st;
   a.max_new = cu_new ? std::min(max_new, total_new) : 1;
-  if ((st = check_page_grid(c, a.max_new, "max_new")) != HIFA4_OK) return st;
+  if ((st = check_page_grid(c, a.max_new, hifa4::paged_append_threads(c->head_dim, a.c.fp16), "max_new")) != HIFA4_OK) return st;
   a.k = (const hifa4::half_t*)k;
   a.v = (const hifa4::half_t*)v;
   a.s = s;
@@ -381,7 +381,7 @@ hifa4_status hifa4_paged_gather(const hifa4_paged_cache* c, int32_t total_tokens
   if ((st = check_aligned16({k, v})) != HIFA4_OK) return st;
   if ((st = check_aligned4({cu_tokens, starts})) != HIFA4_OK) return st;
   a.max_tokens = std::min(max_tokens, total_tokens);
-  if ((st = check_page_grid(c, a.max_tokens, "max_tokens")) != HIFA4_OK) return st;
+  if ((st = check_page_grid(c, a.max_tokens, 256, "max_tokens")) != HIFA4_OK) return st;
   a.cu = cu_tokens;
   a.starts = starts;
   a.k = (hifa4::half_t*)k;

@@ -120,9 +120,12 @@ struct PagedDecode {
   uint8_t* ws;
 };
 
-// Workgroups of 256 threads that one launch may have: HIP counts the threads of
-// a grid in 32 bits.
+// Workgroups that one launch may have (fewer than this): HIP counts the threads
+// of a grid in 32 bits.
 constexpr size_t kMaxGrid = (size_t)1 << 24;
+constexpr size_t max_grid(int threads) { return threads <= 256 ? kMaxGrid : ((size_t)1 << 32) / threads; }
+// Threads of a workgroup of the append: HIF4 a wave per tile of K and per tile of V.
+constexpr int paged_append_threads(int D, bool fp16) { return fp16 ? 256 : 2 * D; }
 
 // Whether the pages can be counted and the join's grid is a launch.
 bool paged_decode_fits(const PagedCache& c, int hq, bool weights);

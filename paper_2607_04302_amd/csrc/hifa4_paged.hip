@@ -441,20 +441,21 @@ hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st) {
   // pages that max_new tokens can touch from any place in a page
   const int blocks = (a.max_new + kPage - 2) / kPage + 1;
   const dim3 grid((unsigned)((size_t)a.c.batch * blocks * a.c.hkv));
+  const int threads = paged_append_threads(a.c.D, a.c.fp16);
   if (a.c.fp16) {
     if (a.c.D == 64)
-      k_paged_append16<1><<<grid, 256, 0, st>>>(a, blocks);
+      k_paged_append16<1><<<grid, threads, 0, st>>>(a, blocks);
     else if (a.c.D == 128)
-      k_paged_append16<2><<<grid, 256, 0, st>>>(a, blocks);
+      k_paged_append16<2><<<grid, threads, 0, st>>>(a, blocks);
     else
-      k_paged_append16<4><<<grid, 256, 0, st>>>(a, blocks);
+      k_paged_append16<4><<<grid, threads, 0, st>>>(a, blocks);
   } else {
     if (a.c.D == 64)
-      k_paged_append<1><<<grid, 128, 0, st>>>(a, blocks);
+      k_paged_append<1><<<grid, threads, 0, st>>>(a, blocks);
     else if (a.c.D == 128)
-      k_paged_append<2><<<grid, 256, 0, st>>>(a, blocks);
+      k_paged_append<2><<<grid, threads, 0, st>>>(a, blocks);
     else
-      k_paged_append<4><<<grid, 512, 0, st>>>(a, blocks);
+      k_paged_append<4><<<grid, threads, 0, st>>>(a, blocks);
   }
   return hipGetLastError();
 }

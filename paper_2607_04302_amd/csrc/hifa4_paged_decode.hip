@@ -315,6 +315,9 @@ __device__ __forceinline__ uint32_t e3_halves(const Part<G>& p, int tile) {
   const uint32_t x = ~p.e3[tile / 2];
   return G == 1 ? (x & 0xFFu) | ((x & 0xFF00u) << 8) : x;
 }
+// Between a wave's accesses of LDS that hand data from lane to lane: the hardware
+// keeps their order, the compiler would only where one lane's meet.
+__device__ __forceinline__ void lds_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
 // A lane's bases to LDS as floats (b 2^-96), for the lanes that hold their rows' products.
 template <int G>
 __device__ __forceinline__ void spread_bases(float* to, uint32_t base, int lane) {
@@ -327,6 +330,7 @@ __device__ __forceinline__ void spread_bases(float* to, uint32_t base, int lane)
 template <int G, typename Get, typename Use>
 __device__ __forceinline__ void products(const Part<G>& p, float* spread, int lane, Get get, Use use) {
   spread_bases<G>(spread, p.base, lane);
+  lds_order();
 #pragma unroll
   for (int tile = 0; tile < G; ++tile) {
     const uint32_t x = e3_halves<G>(p, tile), s0 = e2_scales(p.e2, tile, 0), s1 = e2_scales(p.e2, tile, 1);
@@ -439,7 +443,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
   constexpr int D = 64 * G;
   __shared__ QueryDigits<G> qd;
   __shared__ __align__(16) uint32_t pd[4][kDigitRow];      // [k][query][digit][t]: four keys' digits of p
-  __shared__ __align__(16) float spread[2][64 * G];
+  __shared__ __align__(16) float spread_k[64 * G], spread_v[64 * G];
   const int lane = threadIdx.x, n = lane & 15, k = lane >> 4, piece = n & 3;
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
   const int tile = blockIdx.x / a.c.hkv % tiles, r = blockIdx.x / a.c.hkv / tiles;
@@ -511,7 +515,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     keep_order();
     f4v_t s[4];
     asm volatile("" ::: "memory");       // the query's operands come from LDS in every page, not from registers
-    products<G>(kc, spread[0], lane, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+    products<G>(kc, spread_k, lane, [&](int g, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       const int j2 = k >> 1;
       b0 = fp8_operand(qd.word[g][0][j2][n], qd.word[g][0][2 + j2][n]);
       b1 = fp8_operand(qd.word[g][1][j2][n], qd.word[g][1][2 + j2][n]);
@@ -564,6 +568,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     // every lane's digits to the lanes that need them: of its query's 16 keys and of the next row's
 #pragma unroll
     for (int i = 0; i < 4; ++i) pd[k][16 * (n >> 2) + 4 * i + piece] = fp8x4(d[0][i], d[1][i], d[2][i], d[3][i]);
+    lds_order();
     // 2^up: what the page's sums count (ref - 100 may lie 128 below ref)
     const int up = max((int)(low - ref), -104);
     l = fmaf(sum, __uint_as_float((uint32_t)(127 + up) << 23), l);
@@ -577,7 +582,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
     const uint4 po = *reinterpret_cast<const uint4*>(&pd[(k & 2) + 1][4 * n]);
     const i8v_t pa[2] = {fp8_operand(make_uint4(pe.x, pe.y, pe.x, pe.y), make_uint4(po.x, po.y, po.x, po.y)),
                          fp8_operand(make_uint4(pe.z, pe.w, pe.z, pe.w), make_uint4(po.z, po.w, po.z, po.w))};
-    products<G>(vc, spread[1], lane, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
+    products<G>(vc, spread_v, lane, [&](int, i8v_t& b0, i8v_t& b1, uint32_t& scale) {
       b0 = pa[0];
       b1 = pa[1];
       scale = p_scale;

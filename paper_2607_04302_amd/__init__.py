@@ -523,7 +523,8 @@ def _paged_call(name, device, *args):
 
 def hifa4_paged_page_bytes(heads_kv: int, head_dim: int, operands: int = OPERANDS_HIF4) -> int:
     """Bytes of a page: 64 tokens of K and V, every kv head."""
-    n = int(load_library().hifa4_paged_page_bytes(heads_kv, head_dim, operands))
+    n = int(load_library().hifa4_paged_page_bytes(_count(heads_kv, "heads_kv"), _count(head_dim, "head_dim"),
+                                                  _count(operands, "operands")))
     if not n:
         raise Hifa4Error(f"hifa4_paged_page_bytes: {hifa4_last_error()}")
     return n
@@ -636,7 +637,8 @@ def hifa4_paged_gather(cache: PagedCache, cu_tokens, total_tokens: int, max_toke
 
 
 def hifa4_paged_decode_workspace_bytes(cache: PagedCache, heads_q: int, page_weights: bool = False) -> int:
-    n = int(load_library().hifa4_paged_decode_workspace_bytes(cache._ref, heads_q, 1 if page_weights else 0))
+    n = int(load_library().hifa4_paged_decode_workspace_bytes(cache._ref, _count(heads_q, "heads_q"),
+                                                              1 if page_weights else 0))
     if not n:
         raise Hifa4Error(f"hifa4_paged_decode_workspace_bytes: {hifa4_last_error()}")
     return n

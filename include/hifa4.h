@@ -355,10 +355,16 @@ hifa4_status hifa4_decode_fwd(const hifa4_problem* p, const hifa4_fwd_options* o
  *                those that an append brings included; 0 for an unused row
  *                (values outside [0, 64 max_pages] are cut to that range);
  *   v_tail       DEVICE fp16 [batch, 64, num_heads_kv, head_dim]: V of the
- *                tokens in each sequence's last page, kept by
- *                hifa4_paged_append for HIFA4_OPERANDS_HIF4 (a group of V^ is
- *                quantized again when a token joins it); may be NULL otherwise
- *                and for the other entry points.
+ *                tokens in the page that each sequence's last append ended in,
+ *                kept by hifa4_paged_append for HIFA4_OPERANDS_HIF4 (a group of
+ *                V^ is quantized again when a token joins it); may be NULL
+ *                otherwise and for the other entry points.
+ * Before an append a length may be cut back (tokens that were rejected) within
+ * the page that the last append ended in, or to a multiple of 64; on HIF4 pages
+ * not into the middle of an earlier page, whose V is no longer in v_tail: the
+ * append would quantize that page's group from rows of the later one, without
+ * an error.  A sequence that moves to another row of the batch takes its row of
+ * v_tail along.
  * head_dim is 64, 128 or 256.  Calls of more pages than one launch holds (2^24
  * workgroups, 2^23 for an append to HIF4 pages of head_dim 256: a grid's threads
  * are counted in 32 bits; batch * max_pages reaches 2^30) are refused.  Every
@@ -393,7 +399,8 @@ size_t hifa4_paged_page_bytes(int32_t num_heads_kv, int32_t head_dim, int32_t op
  * max_new: a host bound of the tokens that one sequence gets (it sizes the
  * launch; further tokens are not stored).  An append may begin inside a page
  * and end in another; earlier tokens of the page must have come through
- * hifa4_paged_append, with the same v_tail.  Asynchronous. */
+ * hifa4_paged_append, with the same v_tail, which must still hold them (above:
+ * lengths that are cut back).  Asynchronous. */
 hifa4_status hifa4_paged_append(const hifa4_paged_cache* c, int32_t total_new, int32_t max_new,
                                 const int32_t* cu_new, const void* k, const void* v,
                                 const float* s, void* stream);

@@ -542,7 +542,10 @@ class PagedCache:
                  last page (hifa4_paged_append on HIF4 pages needs it)
 
     The tensors stay the caller's: tables and lengths are changed in place,
-    also between replays of a captured call.  PagedCache.empty allocates them."""
+    also between replays of a captured call.  Before an append a length may be
+    cut back within the page that the last append ended in, or to a multiple of
+    64 (FP16 pages: anywhere; on HIF4 pages v_tail no longer holds V of an
+    earlier page's tokens).  PagedCache.empty allocates them."""
 
     def __init__(self, pool, block_table, seq_lens, head_dim: int, operands: int = OPERANDS_HIF4, v_tail=None):
         torch = _torch()

@@ -436,7 +436,9 @@ size_t hifa4_paged_decode_workspace_bytes(const hifa4_paged_cache* c, int32_t nu
  * the query, the scores, the softmax state (fp32) and p keep their precision (on
  * HIF4 pages the query's values and p enter the products as whole numbers,
  * rounded by at most 2^-19 of the largest of their 64: a group's channels, a
- * page's keys; on FP16 pages p as the sum of two fp16 values).
+ * page's keys; on FP16 pages p as the sum of two fp16 values).  A score moves
+ * with the query by up to 2^-19 of sum max|q| sum|k| / sqrt(D) over the groups:
+ * lse by up to 1e-4 where a few channels of q are 64 times the others.
  * Sequences without tokens get o = 0 and lse = -inf.
  * page_weights (DEVICE fp32 [batch, max_pages], may be NULL): then
  * weights_out[b][j] = decay * page_weights[b][j] + the sum of p over every

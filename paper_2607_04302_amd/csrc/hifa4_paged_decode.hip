@@ -6,8 +6,10 @@
 //   page weights w'[page] = decay w[page] + sum over the heads and the page's
 //   tokens of p_j.
 // q~ = fp16(q s) under Smooth-QK (the cache holds k/s); keys and values are
-// what the cache holds; scores, m, l, the weights p and o are held in fp32 and
-// o is rounded once to fp16.
+// what the cache holds; scores, m, l, the page weights and o are held in fp32
+// and o is rounded once to fp16.  In the products p has 22 bits (FP16 pages) or,
+// like q~, 19 under the largest of its 64 (HIF4 pages): the operands that the
+// matrix instructions take, in two and four pieces.
 //
 // The pages of all sequences are cut into runs of about equal length, as many
 // as fill the chip: a run leaves (m, l, o) of its rows, and a second kernel
@@ -172,7 +174,8 @@ __device__ __forceinline__ half_t round_product(half_t q, float s) {
 // four queries, and four neighbouring lanes add up to the score in fp32.  The
 // weights p of a page are cut the same way, relative to the page's largest:
 // light pages keep their bits, and a key that is light beside another of its
-// page is rounded to 2^-20 of that one's weight.
+// page is rounded by up to 2^-19 of that one's weight (half a step of 2^-15
+// where the largest lies between 8 and 16).
 //
 // Slots of v_mfma_scale_f32_16x16x128_f8f6f4 (measured): FP4 operand lane
 // 16k + n holds K 32k .. 32k+31, its four registers in order; FP8 operand lane

@@ -1,4 +1,6 @@
-"""Paged decode in runs of many pages on the GPU: scores of millions."""
+"""Paged decode in runs of many pages on the GPU: a maximum that moves within a
+run, the weight of every page, plans of more runs than the call aims at, and
+bounds that know what each rounding of the step may cost."""
 import numpy as np
 import pytest
 
@@ -6,7 +8,7 @@ import _paged as P
 import _paged_runs as R
 import paper_2607_04302_amd as h
 from _gpu_util import to_gpu, to_np
-from test_gpu_paged import FMT
+from test_gpu_paged import FMT, _check
 
 pytestmark = pytest.mark.gpu
 
@@ -33,6 +35,83 @@ def _call(pool, table, lens, q, fmt, copies=1, weights=None, decay=1.0, s=None):
     assert all(np.array_equal(o[:, c], o[:, 0], equal_nan=True) for c in range(copies))
     assert all(np.array_equal(lse[c], lse[0], equal_nan=True) for c in range(copies))
     return o[:, 0], lse[0], None if w is None else to_np(w)
+
+
+def _compare(got, want):
+    o, lse, w = got
+    ro, rl, rw, bo, bl, bw = want
+    for a, x, bound, what in ((o, ro, bo, "o"), (lse, rl, bl, "lse"), (w, rw, bw, "weights")):
+        if a is not None:
+            _check(_Host(a), x, bound, what)
+
+
+class _Host:
+    """An array where a tensor is expected."""
+    def __init__(self, a):
+        self.a = a
+
+    def detach(self):
+        return self
+
+    cpu = detach
+
+    def numpy(self):
+        return self.a
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_p_keeps_its_bits(fmt, d):
+    """Values that cancel: a row of few keys whose output is far below its parts shows p's rounding, which that of o
+    hides elsewhere.  One fp16 value for p would be out of the bound."""
+    fm = FMT[fmt]
+    rng = np.random.default_rng(5)
+    batch, lens = 40, [2] * 40
+    # one channel decides the score; the two keys weigh nearly the same, their values are opposite
+    k = np.zeros((batch, 1, 64, d), np.float16)
+    k[:, 0, 0, 0], k[:, 0, 1, 0] = 1.0, -1.0
+    v = np.zeros((batch, 1, 64, d), np.float16)
+    v[:, 0, 0], v[:, 0, 1] = 1.0, -1.0
+    pool = _records(k, v, fm)
+    table = np.arange(batch, dtype=np.int32)[:, None].copy()
+    q = np.zeros((batch, 1, d), np.float16)
+    q[:, 0, 0] = rng.uniform(0.001, 0.01, batch)
+    kv = R.pool_values(pool, d, fm)
+    want = R.decode(q, kv, table, lens, fm)
+    if fmt == "fp16":
+        wrong = R.decode(q, kv, table, lens, fm, rounded_p=True)[0]
+        assert (np.abs(wrong - want[0]) > want[3]).any((1, 2)).sum() > batch // 2
+    _compare(_call(pool, table, lens, q, fm), want)
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("smooth", [False, True])
+def test_queries_with_outlier_channels(fmt, d, smooth):
+    """Channels of 16 and 64 times the others, as the query has them where Smooth-QK took them out of the keys."""
+    fm = FMT[fmt]
+    rng = np.random.default_rng(d + 1)
+    lens = [200, 64, 700, 1]
+    pages = [-(-n // 64) for n in lens]
+    table = np.full((4, max(pages)), -1, np.int32)
+    order = rng.permutation(sum(pages))
+    for b, n in enumerate(pages):
+        table[b, :n] = order[sum(pages[:b]):sum(pages[:b]) + n]
+    k, v = rng.standard_normal((2, sum(pages), 2, 64, d)).astype(np.float16)
+    q = rng.standard_normal((4, 8, d)).astype(np.float32)
+    s = None
+    if smooth:
+        s = rng.uniform(0.5, 2.0, (2, d)).astype(np.float32)
+        s[:, 5::d // 2] *= 64.0
+        s[:, 9::d // 4] *= 16.0
+    else:
+        q[:, ::2, 5::d // 2] *= 64.0
+        q[:, 1::2, 9::d // 4] *= 16.0
+    pool = _records(k, v, fm)
+    q = q.astype(np.float16)
+    w = np.zeros(table.shape, np.float32)
+    _compare(_call(pool, table, lens, q, fm, weights=w, s=s),
+             R.decode(q, R.pool_values(pool, d, fm), table, lens, fm, s, w))
 
 
 @pytest.mark.parametrize("fmt,d,batch", [("fp16", 64, 24), ("fp16", 128, 16), ("fp16", 256, 8), ("hif4", 128, 16), ("hif4", 256, 8)])

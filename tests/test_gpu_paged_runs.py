@@ -59,6 +59,68 @@ class _Host:
         return self.a
 
 
+def _leveled(rng, num, d, levels, fmt):
+    """Pages whose scores lie at levels[page, j] for the queries of kind j: channel 16 j holds the level, the query's
+    other values of it.  Four kv heads, four queries each."""
+    k = rng.standard_normal((num, 4, 64, d)).astype(np.float16)
+    for j in range(4):
+        k[:, :, :, 16 * j] = (levels[:, j, None, None] + rng.uniform(-0.5, 0.5, (num, 4, 64))).astype(np.float16)
+    v = rng.standard_normal((num, 4, 64, d)).astype(np.float16)
+    return _records(k, v, fmt)
+
+
+def _queries(rng, batch, d):
+    """Whole multiples of 2^-8 up to 32: digits hold them."""
+    q = np.rint(rng.standard_normal((batch, 16, d)) * 64) / 256
+    for head in range(16):
+        for j in range(4):
+            q[:, head, 16 * j] = 32.0 if j == head % 4 else 0.0
+    return q.astype(np.float16)
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d,batch", [(64, 24), (128, 16), (256, 8)])
+@pytest.mark.parametrize("kind", ["moving", "flat"])
+def test_runs_of_many_pages(fmt, d, batch, kind):
+    """Two runs of six or seven pages a sequence.  "moving": a row's largest score rises within a run by less and by
+    more than the softmax's reference tolerates, and falls by more than a hundred binades, at other places for each
+    of a wave's four queries; pages that are none at a run's start and inside it."""
+    fm, copies, num, pages = FMT[fmt], 16, 14, 13
+    rng = np.random.default_rng(d)
+    # binades of a level: 32 / sqrt(d) log2(e) each
+    unit = np.sqrt(d) / 32 * np.log(2)
+    binades = np.array([-170, -60, -25, -12, -6, -3, 0, 3, 6, 12, 20, 40, 90, 170], float)
+    levels = np.stack([rng.permutation(binades) for _ in range(4)], 1) * unit if kind == "moving" else np.zeros((num, 4))
+    pool = _leveled(rng, num, d, levels, fm)
+    lens = [64 * pages - int(x) for x in rng.integers(0, 64, batch)]
+    table = np.stack([rng.permutation(num)[:pages] for _ in range(batch)]).astype(np.int32)
+    half = -(-pages // 2)
+    table[1, 0] = table[2, half] = table[3, 3] = table[4, half + 2] = table[5, 5] = table[5, 6] = -1
+    table[6, 1] = num
+    q = _queries(rng, batch, d)
+    w = rng.uniform(0, 1, table.shape).astype(np.float32)
+    w[::2] = 0.0                                                  # (light pages show)
+    runs = R.plan(lens, 16 * copies, 4 * copies, d, fm)
+    assert [r[2] - r[1] >= 6 * R.units_of(d, fm) for r in runs] == [True] * (2 * batch)
+    kv = R.pool_values(pool, d, fm)
+    if kind == "moving":                                          # the case is what it is meant to be
+        rise, fall = np.zeros(3, int), 0
+        for b, begin, end in runs:
+            for head in range(4):
+                top = -np.inf
+                for j in range(begin // R.units_of(d, fm), end // R.units_of(d, fm)):
+                    if not 0 <= table[b, j] < num:
+                        continue
+                    x = (kv[0, table[b, j], 0] @ q[b, head].astype(float)).max() / np.sqrt(d) / np.log(2)
+                    if np.isfinite(top):
+                        rise += [0 < x - top < 8, 8 < x - top < 16, x - top > 16]
+                        fall += x < top - 100
+                    top = max(top, x)
+        assert rise.min() >= 5 and rise[2] > 30 and fall > 30, (rise, fall)
+    got = _call(pool, table, lens, q, fm, copies, w, 0.5)
+    _compare(got, R.decode(q, kv, table, lens, fm, weights=w, decay=0.5, copies=copies))
+
+
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_p_keeps_its_bits(fmt, d):

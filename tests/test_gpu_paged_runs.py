@@ -122,6 +122,29 @@ def test_runs_of_many_pages(fmt, d, batch, kind):
 
 
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("lens", ["short", "long", "mixed"])
+def test_plans_of_many_sequences(fmt, lens):
+    """64 heads of 256 channels aim at 16 runs: more sequences than that, and fewer of which some need several."""
+    fm, d, copies, num = FMT[fmt], 256, 16, 9
+    rng = np.random.default_rng(len(lens))
+    n = {"short": rng.integers(1, 65, 70), "long": rng.integers(1, 600, 15), "mixed": rng.integers(0, 260, 40)}[lens]
+    n = [int(x) for x in n]
+    target = R.run_target(64, 64, d, fm)
+    runs = R.plan(n, 64, 64, d, fm)
+    assert target == 16 and (len(n) >= target or lens == "long")
+    if lens != "long":
+        assert len(runs) > target
+    assert max(r[2] - r[1] for r in runs) > (1 if lens == "short" else 2) * R.units_of(d, fm) or lens == "short"
+    k, v = rng.standard_normal((2, num, 4, 64, d)).astype(np.float16)
+    pool = _records(k, v, fm)
+    table = rng.integers(0, num, (len(n), -(-max(n) // 64) + 1)).astype(np.int32)
+    q = (np.rint(rng.standard_normal((len(n), 4, d)) * 64) / 64).astype(np.float16)
+    w = np.zeros(table.shape, np.float32)
+    got = _call(pool, table, n, q, fm, copies, w)
+    _compare(got, R.decode(q, R.pool_values(pool, d, fm), table, n, fm, weights=w, copies=copies))
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_p_keeps_its_bits(fmt, d):
     """Values that cancel: a row of few keys whose output is far below its parts shows p's rounding, which that of o

@@ -395,7 +395,10 @@ size_t hifa4_paged_page_bytes(int32_t num_heads_kv, int32_t head_dim, int32_t op
  * [num_heads_kv, head_dim] or NULL.  K~ = fp16(k/s), rounded once; with HIF4
  * pages K~ and V become the codes of hifa4_quantize_qk and hifa4_quantize_v:
  * the pages hold at any time the codes of quantizing the whole sequence (the
- * group of an open page zero padded), whatever pieces it came in.
+ * group of an open page zero padded), whatever pieces it came in.  HIF4 has no
+ * infinity and no NaN: where K~ or V is not finite, what the page holds for that
+ * kv head is undefined (no other page and no other head is touched); FP16 pages
+ * hold it as it is.
  * max_new: a host bound of the tokens that one sequence gets (it sizes the
  * launch; further tokens are not stored).  An append may begin inside a page
  * and end in another; earlier tokens of the page must have come through

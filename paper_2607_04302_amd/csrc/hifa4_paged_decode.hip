@@ -38,10 +38,10 @@ __host__ __device__ __forceinline__ int query_tiles(int hq, int hkv, bool fp16) 
 // its registers hold (a page's K and V and, on their way, the next one's).
 // More runs than that wait for a place and are short: 8 x 32768 tokens, HIF4,
 // D=128, 63.7 us with two waves' runs a SIMD, 71, 73 and 77 with 3, 4 and 6;
-// fewer registers a wave for three waves spill (81).  At D=256 one wave: 39 us
-// for what two, with spills, take 47.  Every sequence is cut into equal parts
-// of at most ceil(units / target), numbered densely over the sequences: at most
-// target + batch runs.
+// fewer registers a wave for three waves spill (81).  At D=256 one wave: 4 x 16384
+// tokens, 16 query heads, 37.7 us, for which two, with spills, take 47.0.  Every
+// sequence is cut into equal parts of at most ceil(units / target), numbered
+// densely over the sequences: at most target + batch runs.
 __host__ __device__ __forceinline__ int run_target(int hq, int hkv, int D, bool fp16) {
   const int waves = fp16 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : (D == 256 ? 1 : D == 128 ? 2 : 3);
   const int each = hkv * query_tiles(hq, hkv, fp16);
@@ -187,7 +187,7 @@ __device__ __forceinline__ half_t round_product(half_t q, float s) {
 // 16 lanes brings p into place.
 //
 // Bound by the reads of the pages: 8 x 32768 tokens, 8 kv heads, D=128 (302
-// MB) in 58 us, 5.2 TB/s, where a plain read of as much reaches 5.6.  Mixed
+// MB) in 60 us, 5.1 TB/s, where a plain read of as much reaches 5.6.  Mixed
 // lengths (32 of 300 to 8192, 165 MB) take 39 us, 4.2 TB/s: about 3 us until
 // the first page is there, and 10% for runs of unequal length.
 constexpr int kFp4 = 4, kFp8 = 0;            // operand formats of the instruction
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
 // 2^15: small weights stay above fp16's subnormals down to 2^-21 of it.  What p
 // counts from is held itself, not the score 7 binades above it: of scores over
 // 2^24 that difference is no number, and p would pass fp16's range.
-// Bound by the reads: D=128, 8 x 8192 tokens (268 MB) in 52 us, 5.2 TB/s.
+// Bound by the reads: D=128, 8 x 8192 tokens (268 MB) in 51 us, 5.2 TB/s.
 typedef half_t h8v_t __attribute__((ext_vector_type(8)));
 typedef half_t h4v_t __attribute__((ext_vector_type(4)));
 constexpr float kTop16 = 7.0f, kSlack16 = 8.0f;

@@ -363,8 +363,9 @@ hifa4_status hifa4_decode_fwd(const hifa4_problem* p, const hifa4_fwd_options* o
  * the page that the last append ended in, or to a multiple of 64; on HIF4 pages
  * not into the middle of an earlier page, whose V is no longer in v_tail: the
  * append would quantize that page's group from rows of the later one, without
- * an error.  A sequence that moves to another row of the batch takes its row of
- * v_tail along.
+ * an error.  (Until the next append the page keeps V^ as it was quantized with
+ * the tokens that were cut off.)  A sequence that moves to another row of the
+ * batch takes its row of v_tail along.
  * head_dim is 64, 128 or 256.  Calls of more pages than one launch holds (2^24
  * workgroups, 2^23 for an append to HIF4 pages of head_dim 256: a grid's threads
  * are counted in 32 bits; batch * max_pages reaches 2^30) are refused.  Every
@@ -400,7 +401,7 @@ size_t hifa4_paged_page_bytes(int32_t num_heads_kv, int32_t head_dim, int32_t op
  * kv head is undefined (no other page and no other head is touched); FP16 pages
  * hold it as it is.
  * max_new: a host bound of the tokens that one sequence gets (it sizes the
- * launch; further tokens are not stored).  An append may begin inside a page
+ * launch, for every sequence of the batch; further tokens are not stored).  An append may begin inside a page
  * and end in another; earlier tokens of the page must have come through
  * hifa4_paged_append, with the same v_tail, which must still hold them (above:
  * lengths that are cut back).  Asynchronous. */

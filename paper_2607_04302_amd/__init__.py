@@ -596,7 +596,8 @@ def hifa4_paged_append(cache: PagedCache, k, v, s=None, cu_new=None, max_new: Op
     cu_new one token per row of the batch, else sequence b gets the rows
     [cu_new[b], cu_new[b+1]).  cache.seq_lens counts the new tokens already.
     s: the Smooth-QK scales (the pages then hold k/s).  max_new: an upper bound
-    of the tokens per sequence (default: all of them)."""
+    of the tokens per sequence (default: all of them; it sizes the launch for
+    every row, so large batches give it)."""
     torch, dev = _torch(), cache.device
     if k.dim() != 3:
         raise ValueError("k is [total, heads_kv, head_dim]")

@@ -401,10 +401,10 @@ size_t hifa4_paged_page_bytes(int32_t num_heads_kv, int32_t head_dim, int32_t op
  * kv head is undefined (no other page and no other head is touched); FP16 pages
  * hold it as it is.
  * max_new: a host bound of the tokens that one sequence gets (it sizes the
- * launch, for every sequence of the batch; further tokens are not stored).  An append may begin inside a page
- * and end in another; earlier tokens of the page must have come through
- * hifa4_paged_append, with the same v_tail, which must still hold them (above:
- * lengths that are cut back).  Asynchronous. */
+ * launch, for every sequence of the batch; further tokens are not stored).  An
+ * append may begin inside a page and end in another; earlier tokens of the page
+ * must have come through hifa4_paged_append, with the same v_tail, which must
+ * still hold them (above: lengths that are cut back).  Asynchronous. */
 hifa4_status hifa4_paged_append(const hifa4_paged_cache* c, int32_t total_new, int32_t max_new,
                                 const int32_t* cu_new, const void* k, const void* v,
                                 const float* s, void* stream);

@@ -476,6 +476,136 @@ hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* 
                                int32_t first, int32_t last, int32_t* out_table, int32_t* out_lens,
                                float* out_weights, int32_t* freed, int32_t* num_freed, void* stream);
 
+/* Bytes of device workspace hifa4_paged_chunk_fwd needs (0 on invalid
+ * arguments).  It is bounded by the number of runs that fill the GPU and does
+ * not depend on the lengths. */
+size_t hifa4_paged_chunk_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q,
+                                         int32_t total_new, int32_t max_new);
+
+/* The attention of each sequence's last tokens over its cached tokens: chunks
+ * of prompts, drafted tokens that are checked, one token of each sequence, or
+ * all of these in one batch.  The new tokens of sequence b are the rows
+ * [cu_new[b], cu_new[b+1]) of q (DEVICE fp16 [total_new, num_heads_q, head_dim])
+ * and the last ones of its seq_lens[b] tokens, appended before; the i-th of n
+ * stands at position seq_lens[b] - n + i and sees the cached tokens up to its
+ * own.  cu_new: DEVICE int32 [batch+1], prefix sums from 0 to at most total_new
+ * (where they grow beyond that nothing is written).  q is smoothed with s when s
+ * is not NULL (q~ = fp16(q*s)); query head h reads kv head h / (num_heads_q /
+ * num_heads_kv).  With S_j = q~ k_j / sqrt(D) over the cached values that the
+ * token sees: p = softmax(S), o = sum_j p_j v_j (DEVICE fp16, like q), lse = log
+ * sum_j exp(S_j) (DEVICE fp32 [num_heads_q, total_new]).
+ * Scores, softmax and o are held in fp32.  The products take fp16 operands: q~,
+ * the cached values (on HIF4 pages exact down to 2^-14, below that rounded by at
+ * most 2^-24) and p, rounded to fp16 for the sum over v; o is divided by the sum
+ * of the rounded p, lse holds the sum of p itself.  A value that is not finite
+ * (FP16 pages) reaches the rows that see its token and no others.
+ * Rows that see no token (more new tokens than cached ones, pages that are none)
+ * get o = 0 and lse = -inf; rows of q behind cu_new[batch] leave o and lse as
+ * they were.  max_new: a host bound of the new tokens of one sequence (it sizes
+ * the launch; o and lse of further tokens are left as they were).
+ * workspace: DEVICE, >= hifa4_paged_chunk_workspace_bytes(); nothing in it has to
+ * start at zero and nothing is kept in it.  Sums are taken in a fixed order: equal
+ * inputs give equal bits.  Asynchronous. */
+hifa4_status hifa4_paged_chunk_fwd(const hifa4_paged_cache* c, int32_t num_heads_q,
+                                   int32_t total_new, int32_t max_new, const int32_t* cu_new,
+                                   const void* q, const float* s, void* o, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Deals out the pages of new tokens from a stack of free ones.  Row b holds
+ * seq_lens[b] tokens and asks for counts[b] more (DEVICE int32 [batch]; negative:
+ * none).  A row that asks for more than max_new (a host bound, which sizes the
+ * launch) or than fit its 64 max_pages places gets none and asks for none.  The
+ * others are served in order: a row gets its tokens if those that were asked for
+ * up to and with it are at most max_total and, where it needs pages, the pages
+ * needed up to and with it are at most the free ones; else it gets none.
+ *   free_pages   DEVICE int32 [capacity], num_free (DEVICE int32 [1]) entries of
+ *                which are free pages, the last one on top; the first page of
+ *                the first row that needs one is the top one;
+ *   block_table  gets the new pages at the places behind the old ones (the first
+ *                ceil(seq_lens[b]/64), which are read); what lies at other places
+ *                is left as it is;
+ *   out_lens     DEVICE int32 [batch], the lengths with the tokens that were got,
+ *                out_free DEVICE int32 [1] the pages left; each may be its
+ *                input's own buffer;
+ *   cu_new       DEVICE int32 [batch+1], prefix sums of the tokens that the rows
+ *                got (what hifa4_paged_append and hifa4_paged_chunk_fwd take);
+ *   positions    DEVICE int32 [max_total], of each of these tokens, row by row,
+ *                its place in its sequence, plus shift[b] (DEVICE int32 [batch] or
+ *                NULL: 0; the tokens that an eviction has taken out of a row keep
+ *                their positions);
+ *   slots        DEVICE int64 [max_total], 64 * page + place in the page (-1 where
+ *                the table names no page).
+ * Entries of positions and slots behind cu_new[batch] are -1.  No buffer overlaps
+ * another but as stated.  Asynchronous; it may be captured and replayed. */
+hifa4_status hifa4_paged_extend(int32_t batch, int32_t max_pages, int32_t* block_table,
+                                const int32_t* seq_lens, const int32_t* counts,
+                                const int32_t* free_pages, int32_t capacity, const int32_t* num_free,
+                                const int32_t* shift, int32_t max_total, int32_t max_new,
+                                int32_t* out_lens, int32_t* out_free, int32_t* cu_new,
+                                int32_t* positions, int64_t* slots, void* stream);
+
+/* Bytes of device workspace hifa4_paged_release needs (0 on invalid arguments). */
+size_t hifa4_paged_release_workspace_bytes(int32_t batch);
+
+/* Puts pages back on the stack of free ones: of each row of table (DEVICE int32
+ * [batch, max_pages]: a block table, or the evicted pages of hifa4_paged_evict) the
+ * entries at the places [first[b], to[b]) (DEVICE int32 [batch]; first may be
+ * NULL: 0; cut to the row), but for negative ones, which are none.  They end on
+ * top in order, the first row's first entry uppermost: a release of what
+ * hifa4_paged_extend has dealt out restores the stack.  Pages that find no place
+ * below `capacity` are dropped (the first ones); out_free (DEVICE int32 [1]) is
+ * the new number and may be num_free itself.  The table is left as it is: lengths
+ * say which of its places count.  A page is released once: one that several rows
+ * share, or that stands in the table twice, would be dealt out twice.
+ * workspace: DEVICE, >= hifa4_paged_release_workspace_bytes(), 4-byte aligned; one
+ * call at a time.  Asynchronous; it may be captured and replayed. */
+hifa4_status hifa4_paged_release(int32_t batch, int32_t max_pages, const int32_t* table,
+                                 const int32_t* first, const int32_t* to, int32_t* free_pages,
+                                 int32_t capacity, const int32_t* num_free, int32_t* out_free,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary positions (the step before Smooth-QK, whose scales act "after RoPE",
+ * Section 4.2).  The first rot_dim channels of a head are rotated in pairs, the
+ * others are copied: pair i of a token at position p becomes
+ *   (x cos(p w_i) - y sin(p w_i), x sin(p w_i) + y cos(p w_i)) * magnitude.
+ * Scaling of the frequencies w_i = base^(-2i/rot_dim): */
+typedef enum {
+  HIFA4_ROPE_NONE = 0,
+  HIFA4_ROPE_LINEAR = 1,  /* w_i / factor                                            */
+  HIFA4_ROPE_NTK = 2,     /* base * factor^(rot_dim/(rot_dim-2)) in place of base    */
+  HIFA4_ROPE_PARTS = 3    /* w_i (g + (1-g)/factor), where g goes from 0 to 1 as the
+                             turns original_len w_i / (2 pi) go from low to high     */
+} hifa4_rope_scaling;
+
+/* The frequencies in turns per position, as whole numbers of 2^-64 (modulo one
+ * turn): turns[i] = w_i / (2 pi) * 2^64 rounded, i < rot_dim/2, to a HOST array.
+ * rot_dim a positive multiple of 8 (at most 256); base > 1; factor >= 1 (ignored
+ * without scaling); original_len > 0 and 0 <= low < high with _PARTS. */
+hifa4_status hifa4_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                    double original_len, double low, double high, uint64_t* turns);
+
+/* Rotates q and k (DEVICE fp16).
+ *   rot_dim      a multiple of 8 up to head_dim (64, 128 or 256);
+ *   interleaved  0: pair i is the channels i and i + rot_dim/2; 1: 2i and 2i+1;
+ *   transposed   0 or 1: the transposed rotation, the inverse where the magnitude
+ *                is 1, and the gradient of q and k from that of q_out and k_out;
+ *   turns        DEVICE uint64 [rot_dim/2], from hifa4_rope_frequencies;
+ *   positions    DEVICE int32 [num_tokens]; rows of negative ones are no tokens:
+ *                their outputs are left as they were;
+ *   q, k         num_tokens rows of num_heads_q and num_heads_k heads, the rows
+ *                q_stride and k_stride elements apart (multiples of 8: parts of one
+ *                projection's rows); 0 heads: none;
+ *   q_out, k_out the same with strides of their own; each may be its input (with
+ *                its stride) and overlaps nothing else.
+ * Angles are exact modulo a turn at any position; the rotated values are computed
+ * in fp32 and rounded once.  Asynchronous. */
+hifa4_status hifa4_rope(int32_t head_dim, int32_t rot_dim, int32_t interleaved, int32_t transposed,
+                        float magnitude, const uint64_t* turns, int32_t num_tokens,
+                        const int32_t* positions, int32_t num_heads_q, const void* q,
+                        int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t num_heads_k,
+                        const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride,
+                        void* stream);
+
 /* Device self-test of the kernels' fp16 exponential: y[i] = fp16(2^x[i]) for
  * n fp16 inputs x (DEVICE, fp16 bits), evaluated by the same device routine
  * the attention kernel uses.  Asynchronous. */

@@ -11,7 +11,9 @@ Names mirror the C entry points:
   hifa4_attention_fwd, hifa4_workspace_bytes, hifa4_decode_fwd,
   hifa4_decode_workspace_bytes, hifa4_paged_page_bytes, hifa4_paged_append,
   hifa4_paged_gather, hifa4_paged_decode_fwd, hifa4_paged_decode_workspace_bytes,
-  hifa4_paged_evict, hifa4_selftest_exp2, hifa4_last_error.
+  hifa4_paged_evict, hifa4_paged_chunk_fwd, hifa4_paged_chunk_workspace_bytes,
+  hifa4_paged_extend, hifa4_paged_release, hifa4_rope, hifa4_selftest_exp2,
+  hifa4_last_error.
 """
 from __future__ import annotations
 
@@ -33,8 +35,10 @@ EXPORTED = ("hifa4_workspace_bytes", "hifa4_calibrate_workspace_bytes", "hifa4_c
             "hifa4_calibrate_smooth_qk_layers",
             "hifa4_quantize_qk", "hifa4_quantize_v", "hifa4_attention_fwd", "hifa4_decode_workspace_bytes",
             "hifa4_decode_fwd", "hifa4_paged_page_bytes", "hifa4_paged_append", "hifa4_paged_gather",
-            "hifa4_paged_decode_workspace_bytes", "hifa4_paged_decode_fwd", "hifa4_paged_evict", "hifa4_selftest_exp2",
-            "hifa4_last_error", "hifa4_attention_fwd_noalloc")
+            "hifa4_paged_decode_workspace_bytes", "hifa4_paged_decode_fwd", "hifa4_paged_evict",
+            "hifa4_paged_chunk_workspace_bytes", "hifa4_paged_chunk_fwd", "hifa4_paged_extend",
+            "hifa4_paged_release_workspace_bytes", "hifa4_paged_release", "hifa4_rope_frequencies", "hifa4_rope",
+            "hifa4_selftest_exp2", "hifa4_last_error", "hifa4_attention_fwd_noalloc")
 NOALLOC_SCRATCH_BYTES = 32 << 20
 PAGE_TOKENS = 64
 
@@ -120,6 +124,21 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.hifa4_paged_decode_fwd.argtypes = [P(PagedCacheDesc), i32, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]
     lib.hifa4_paged_evict.restype = ctypes.c_int
     lib.hifa4_paged_evict.argtypes = [i32, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    i64 = ctypes.c_int64
+    lib.hifa4_paged_chunk_workspace_bytes.restype = sz
+    lib.hifa4_paged_chunk_workspace_bytes.argtypes = [P(PagedCacheDesc), i32, i32, i32]
+    lib.hifa4_paged_chunk_fwd.restype = ctypes.c_int
+    lib.hifa4_paged_chunk_fwd.argtypes = [P(PagedCacheDesc), i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.hifa4_paged_extend.restype = ctypes.c_int
+    lib.hifa4_paged_extend.argtypes = [i32, i32, vp, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.hifa4_paged_release_workspace_bytes.restype = sz
+    lib.hifa4_paged_release_workspace_bytes.argtypes = [i32]
+    lib.hifa4_paged_release.restype = ctypes.c_int
+    lib.hifa4_paged_release.argtypes = [i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.hifa4_rope_frequencies.restype = ctypes.c_int
+    lib.hifa4_rope_frequencies.argtypes = [i32] + [ctypes.c_double, i32] + [ctypes.c_double] * 4 + [vp]
+    lib.hifa4_rope.restype = ctypes.c_int
+    lib.hifa4_rope.argtypes = [i32, i32, i32, i32, ctypes.c_float, vp, i32, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
     lib.hifa4_selftest_exp2.restype = ctypes.c_int
     lib.hifa4_selftest_exp2.argtypes = [vp, vp, ctypes.c_int64, vp]
     lib.hifa4_last_error.restype = ctypes.c_char_p
@@ -731,6 +750,233 @@ def hifa4_paged_evict(block_table, seq_lens, page_weights, budget: int, first: i
                 page_weights.data_ptr(), budget, first, last, out_table.data_ptr(), out_lens.data_ptr(),
                 out_weights.data_ptr(), freed.data_ptr(), num_freed.data_ptr(), _stream(dev))
     return freed, num_freed
+
+
+def hifa4_paged_chunk_workspace_bytes(cache: PagedCache, heads_q: int, total_new: int, max_new: int) -> int:
+    n = int(load_library().hifa4_paged_chunk_workspace_bytes(cache._ref, _count(heads_q, "heads_q"),
+                                                             _count(total_new, "total_new"), _count(max_new, "max_new")))
+    if not n:
+        raise Hifa4Error(f"hifa4_paged_chunk_workspace_bytes: {hifa4_last_error()}")
+    return n
+
+
+def hifa4_paged_chunk_fwd(cache: PagedCache, q, cu_new, s=None, max_new: Optional[int] = None, out=None, lse=None,
+                          workspace: Optional[Workspace] = None):
+    """The attention of each sequence's last tokens over the pages: q [total,
+    heads_q, head_dim] fp16, of sequence b the rows [cu_new[b], cu_new[b+1]), whose
+    tokens are the last ones of its cached tokens (appended before); a token sees
+    the cached ones up to its own.  max_new: an upper bound of the tokens per
+    sequence (default: all of them; it sizes the launch, so batches give it).
+    Returns (o like q, lse fp32 [heads_q, total]); rows that see nothing get 0 and
+    -inf, rows that no sequence has are left as they are (uninitialized where out
+    and lse are not given)."""
+    torch, dev = _torch(), cache.device
+    if q.dim() != 3:
+        raise ValueError("q is [total, heads_q, head_dim]")
+    total, hq = _count(q.shape[0], "the rows of q"), q.shape[1]
+    _shaped(q, torch.float16, (total, hq, cache.head_dim), dev, "q")
+    _shaped(cu_new, torch.int32, (cache.batch + 1,), dev, "cu_new")
+    if s is not None:
+        _shaped(s, torch.float32, (cache.heads_kv, cache.head_dim), dev, "s")
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _shaped(out, torch.float16, q.shape, dev, "out")
+    if lse is None:
+        lse = torch.empty((hq, total), dtype=torch.float32, device=dev)
+    else:
+        _shaped(lse, torch.float32, (hq, total), dev, "lse")
+    max_new = total if max_new is None else _count(max_new, "max_new")
+    key = (hq, total, max_new)
+    need = cache._workspace_bytes.get(key)
+    if need is None:
+        if len(cache._workspace_bytes) >= 4096:
+            cache._workspace_bytes.clear()
+        need = cache._workspace_bytes[key] = hifa4_paged_chunk_workspace_bytes(cache, hq, total, max_new)
+    stream = _stream(dev)
+    ws = _scratch(need, dev, stream) if workspace is None else workspace.get(need, dev)
+    _paged_call("hifa4_paged_chunk_fwd", dev, cache._ref, hq, total, max_new, cu_new.data_ptr(), q.data_ptr(), _ptr(s),
+                out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    return out, lse
+
+
+def hifa4_paged_extend(block_table, seq_lens, counts, free_pages, num_free, max_total: int, max_new: Optional[int] = None,
+                       shift=None, out_lens=None, out_free=None, cu_new=None, positions=None, slots=None):
+    """Deals out the pages of counts[b] new tokens for each row of block_table
+    [batch, max_pages] from the stack free_pages (int32, num_free[0] of them free,
+    the last on top).  Rows are served in order; one whose tokens would go beyond
+    max_total, or its pages beyond the free ones, gets none.  Works in place on
+    block_table and, unless out_lens and out_free are given, on seq_lens and
+    num_free.  Returns (cu_new int32 [batch+1], positions int32 [max_total], slots
+    int64 [max_total]): the prefix sums of the tokens that the rows got, and of each
+    its position (plus shift[b], the tokens that evictions took out) and its slot
+    (64 * page + place); -1 behind the last one.  max_new: an upper bound of the
+    tokens per row (default: max_total)."""
+    torch, dev = _torch(), block_table.device
+    if block_table.dim() != 2:
+        raise ValueError("block_table is [batch, max_pages]")
+    if free_pages.dim() != 1:
+        raise ValueError("free_pages is [capacity]")
+    i32 = torch.int32
+    shape = block_table.shape
+    rows, one = shape[:1], (1,)
+    total = (_count(max_total, "max_total"),)
+    max_new = max_total if max_new is None else _count(max_new, "max_new")
+    if max_total < 0:
+        raise ValueError("max_total must be >= 0")
+    _shaped(block_table, i32, shape, dev, "block_table")
+    _shaped(seq_lens, i32, rows, dev, "seq_lens")
+    _shaped(counts, i32, rows, dev, "counts")
+    _shaped(free_pages, i32, free_pages.shape, dev, "free_pages")
+    _shaped(num_free, i32, one, dev, "num_free")
+    if shift is not None:
+        _shaped(shift, i32, rows, dev, "shift")
+    if out_lens is None:
+        out_lens = seq_lens
+    else:
+        _shaped(out_lens, i32, rows, dev, "out_lens")
+    if out_free is None:
+        out_free = num_free
+    else:
+        _shaped(out_free, i32, one, dev, "out_free")
+    if cu_new is None:
+        cu_new = torch.empty(shape[0] + 1, dtype=i32, device=dev)
+    else:
+        _shaped(cu_new, i32, (shape[0] + 1,), dev, "cu_new")
+    if positions is None:
+        positions = torch.empty(total, dtype=i32, device=dev)
+    else:
+        _shaped(positions, i32, total, dev, "positions")
+    if slots is None:
+        slots = torch.empty(total, dtype=torch.int64, device=dev)
+    else:
+        _shaped(slots, torch.int64, total, dev, "slots")
+    _paged_call("hifa4_paged_extend", dev, shape[0], shape[1], block_table.data_ptr(), seq_lens.data_ptr(), counts.data_ptr(),
+                free_pages.data_ptr(), _count(free_pages.shape[0], "the free pages"), num_free.data_ptr(), _ptr(shift), max_total,
+                max_new, out_lens.data_ptr(), out_free.data_ptr(), cu_new.data_ptr(), positions.data_ptr(), slots.data_ptr(),
+                _stream(dev))
+    return cu_new, positions, slots
+
+
+def hifa4_paged_release(table, to, free_pages, num_free, first=None, out_free=None, workspace: Optional[Workspace] = None):
+    """Puts the entries at the places [first[b], to[b]) (first: default 0) of each
+    row of table [batch, max_pages] back on the stack free_pages, the first row's
+    first entry on top; negative entries are no pages.  num_free counts them
+    afterwards, unless out_free is given.  Returns out_free.  For the pages that
+    hifa4_paged_evict took out: hifa4_paged_release(freed, num_freed, ...)."""
+    torch, dev = _torch(), table.device
+    if table.dim() != 2:
+        raise ValueError("table is [batch, max_pages]")
+    if free_pages.dim() != 1:
+        raise ValueError("free_pages is [capacity]")
+    i32 = torch.int32
+    shape = table.shape
+    rows, one = shape[:1], (1,)
+    _shaped(table, i32, shape, dev, "table")
+    _shaped(to, i32, rows, dev, "to")
+    if first is not None:
+        _shaped(first, i32, rows, dev, "first")
+    _shaped(free_pages, i32, free_pages.shape, dev, "free_pages")
+    _shaped(num_free, i32, one, dev, "num_free")
+    if out_free is None:
+        out_free = num_free
+    else:
+        _shaped(out_free, i32, one, dev, "out_free")
+    need = 4 * (shape[0] + 1)
+    stream = _stream(dev)
+    ws = _scratch(need, dev, stream) if workspace is None else workspace.get(need, dev)
+    _paged_call("hifa4_paged_release", dev, shape[0], shape[1], table.data_ptr(), _ptr(first), to.data_ptr(),
+                free_pages.data_ptr(), _count(free_pages.shape[0], "the free pages"), num_free.data_ptr(), out_free.data_ptr(),
+                ws.data_ptr(), ws.numel(), stream)
+    return out_free
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions.
+ROPE_SCALINGS = ("none", "linear", "ntk", "parts")
+
+
+class Rope:
+    """Frequencies of the rotary positions of heads of head_dim channels, of which
+    the first rot_dim (default: all; a multiple of 8) are rotated.
+
+    base         w_i = base^(-2i/rot_dim) is the angle of pair i per position
+    interleaved  pairs are neighbouring channels (else i and i + rot_dim/2)
+    scaling      of the frequencies, for contexts longer than the trained one:
+                 "none"; "linear": w / factor; "ntk": base * factor^(r/(r-2));
+                 "parts": w (g + (1-g)/factor), where g goes from 0 to 1 as the
+                 turns over original_len positions go from low to high
+    magnitude    factor of the rotated values"""
+
+    def __init__(self, head_dim: int, rot_dim: Optional[int] = None, base: float = 10000.0, interleaved: bool = False,
+                 scaling: str = "none", factor: float = 1.0, original_len: float = 0.0, low: float = 1.0, high: float = 32.0,
+                 magnitude: float = 1.0, device="cuda"):
+        torch = _torch()
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {ROPE_SCALINGS}, got {scaling!r}")
+        if head_dim not in (64, 128, 256):
+            raise ValueError(f"head_dim must be 64, 128 or 256, got {head_dim}")
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        if rot_dim <= 0 or rot_dim > head_dim or rot_dim % 8:
+            raise ValueError(f"rot_dim must be a multiple of 8 between 8 and head_dim, got {rot_dim}")
+        turns = (ctypes.c_uint64 * (rot_dim // 2))()
+        _check(load_library().hifa4_rope_frequencies(rot_dim, base, ROPE_SCALINGS.index(scaling), factor, original_len, low, high,
+                                                     turns), "hifa4_rope_frequencies")
+        # uint64 bit patterns in an int64 tensor
+        signed = [t - 2 ** 64 if t >= 2 ** 63 else t for t in turns]
+        self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
+        self.device = self.turns.device
+        self.head_dim, self.rot_dim, self.interleaved, self.magnitude = head_dim, rot_dim, bool(interleaved), float(magnitude)
+
+
+def _rope_rows(t, tokens, head_dim, device, name):
+    """(heads, pointer, elements from token to token) of [tokens, heads, head_dim], each token's heads contiguous."""
+    torch = _torch()
+    if t is None:
+        return 0, None, 0
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype is not torch.float16:
+        raise ValueError(f"{name} must be {torch.float16}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != head_dim:
+        raise ValueError(f"{name} must be [{tokens}, heads, {head_dim}], got {list(t.shape)}")
+    heads = t.shape[1]
+    a, b, c = t.stride()
+    if tokens and (c != 1 or (heads > 1 and b != head_dim)):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    return _count(heads, "heads"), t.data_ptr(), max(a, heads * head_dim) if tokens <= 1 else a
+
+
+def hifa4_rope(rope: Rope, positions, q=None, k=None, q_out=None, k_out=None, transposed: bool = False):
+    """Rotates q [tokens, heads_q, head_dim] and k [tokens, heads_k, head_dim] (fp16;
+    either may be None; a token's heads are contiguous, tokens any multiple of 8
+    elements apart, so parts of one projection's rows will do) by the positions
+    int32 [tokens].  Rows of negative positions are no tokens: their outputs are
+    left as they are.  Returns (q_out, k_out), allocated unless given; q_out=q and
+    k_out=k work in place.  transposed: the transposed rotation, the gradient of q
+    and k from that of q_out and k_out (the inverse, where the magnitude is 1)."""
+    torch, dev = _torch(), rope.device
+    if positions.dim() != 1:
+        raise ValueError("positions is [tokens]")
+    tokens = _count(positions.shape[0], "the tokens")
+    _shaped(positions, torch.int32, (tokens,), dev, "positions")
+    d = rope.head_dim
+    hq, qp, qs = _rope_rows(q, tokens, d, dev, "q")
+    hk, kp, ks = _rope_rows(k, tokens, d, dev, "k")
+    for x, y, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if y is not None and (x is None or x.shape != y.shape):
+            raise ValueError(f"{name}_out needs a {name} of its shape")
+    if q is not None and q_out is None:
+        q_out = torch.empty((tokens, hq, d), dtype=torch.float16, device=dev)
+    if k is not None and k_out is None:
+        k_out = torch.empty((tokens, hk, d), dtype=torch.float16, device=dev)
+    _, qo, qos = _rope_rows(q_out, tokens, d, dev, "q_out")
+    _, ko, kos = _rope_rows(k_out, tokens, d, dev, "k_out")
+    _paged_call("hifa4_rope", dev, d, rope.rot_dim, int(rope.interleaved), int(bool(transposed)), rope.magnitude,
+                rope.turns.data_ptr(), tokens, positions.data_ptr(), hq, qp, qs, qo, qos, hk, kp, ks, ko, kos, _stream(dev))
+    return q_out, k_out
 
 
 def hifa4_selftest_exp2(x):

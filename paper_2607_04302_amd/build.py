@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhifa4.so")
 SOURCES = ["hifa4_api.cpp", "hifa4_quant.hip", "hifa4_attn.hip", "hifa4_decode.hip",
-           "hifa4_paged.hip", "hifa4_paged_decode.hip"]
+           "hifa4_paged.hip", "hifa4_paged_decode.hip", "hifa4_paged_chunk.hip", "hifa4_paged_tables.hip", "hifa4_rope.hip"]
 
 
 def hipcc() -> str:

@@ -16,6 +16,7 @@
 #include "hifa4_decode.h"
 #include "hifa4_internal.h"
 #include "hifa4_paged.h"
+#include "hifa4_rope.h"
 
 namespace {
 
@@ -463,6 +464,217 @@ hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* 
   a.num_freed = num_freed;
   const hipError_t e = hifa4::launch_paged_evict(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "paged evict");
+  return HIFA4_OK;
+}
+
+namespace {
+
+hifa4_status check_chunk(const hifa4_paged_cache* c, const hifa4::PagedCache& pc, int32_t hq, int32_t total, int32_t max_new) {
+  const hifa4_status st = check_query_heads(hq, c->batch, c->num_heads_kv);
+  if (st != HIFA4_OK) return st;
+  if (total < 0 || max_new < 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "total_new and max_new must be >= 0");
+  if ((int64_t)total * hq >= (1LL << 31)) return fail(HIFA4_ERR_UNSUPPORTED, "problem too large for 32-bit row indexing");
+  if (!hifa4::paged_chunk_fits(pc, hq, total, std::min(max_new, total)))
+    return fail(HIFA4_ERR_UNSUPPORTED, "%d new tokens (up to %d of each of %d sequences) are too many for one launch", total,
+                max_new, c->batch);
+  return HIFA4_OK;
+}
+
+}  // namespace
+
+size_t hifa4_paged_chunk_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q, int32_t total_new, int32_t max_new) {
+  hifa4::PagedCache pc;
+  if (check_paged(c, false, &pc) != HIFA4_OK || check_chunk(c, pc, num_heads_q, total_new, max_new) != HIFA4_OK) return 0;
+  return hifa4::paged_chunk_workspace(pc, num_heads_q, total_new, std::min(max_new, total_new));
+}
+
+hifa4_status hifa4_paged_chunk_fwd(const hifa4_paged_cache* c, int32_t num_heads_q, int32_t total_new, int32_t max_new,
+                                   const int32_t* cu_new, const void* q, const float* s, void* o, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  hifa4::PagedChunk a;
+  hifa4_status st = check_paged(c, true, &a.c);
+  if (st != HIFA4_OK) return st;
+  if ((st = check_chunk(c, a.c, num_heads_q, total_new, max_new)) != HIFA4_OK) return st;
+  if (!cu_new) return fail(HIFA4_ERR_INVALID_ARGUMENT, "cu_new is NULL");
+  if (total_new == 0 || max_new == 0) return HIFA4_OK;
+  if (!q || !o || !lse) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if ((st = check_aligned16({q, s, o, workspace})) != HIFA4_OK) return st;
+  if ((st = check_aligned4({cu_new, lse})) != HIFA4_OK) return st;
+  a.max_new = std::min(max_new, total_new);
+  const size_t need = hifa4::paged_chunk_workspace(a.c, num_heads_q, total_new, a.max_new);
+  if (!workspace || workspace_bytes < need)
+    return fail(HIFA4_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
+  a.hq = num_heads_q;
+  a.total = total_new;
+  a.cu = cu_new;
+  a.q = (const hifa4::half_t*)q;
+  a.s = s;
+  a.o = (hifa4::half_t*)o;
+  a.lse = lse;
+  a.scale = (float)(1.4426950408889634 / std::sqrt((double)c->head_dim));
+  a.ws = (uint8_t*)workspace;
+  const hipError_t e = hifa4::launch_paged_chunk(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged chunk kernels");
+  return HIFA4_OK;
+}
+
+namespace {
+
+hifa4_status check_table(int32_t batch, int32_t max_pages, int32_t capacity) {
+  if (batch <= 0 || max_pages <= 0 || capacity <= 0)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "batch, max_pages and capacity must be > 0");
+  if (max_pages >= (1 << 25) || (int64_t)batch * max_pages >= (1LL << 30) || batch >= (1 << 22))
+    return fail(HIFA4_ERR_UNSUPPORTED, "a table of %d x %d pages is too large", batch, max_pages);
+  return HIFA4_OK;
+}
+
+}  // namespace
+
+hifa4_status hifa4_paged_extend(int32_t batch, int32_t max_pages, int32_t* block_table, const int32_t* seq_lens,
+                                const int32_t* counts, const int32_t* free_pages, int32_t capacity, const int32_t* num_free,
+                                const int32_t* shift, int32_t max_total, int32_t max_new, int32_t* out_lens, int32_t* out_free,
+                                int32_t* cu_new, int32_t* positions, int64_t* slots, void* stream) {
+  hifa4_status st = check_table(batch, max_pages, capacity);
+  if (st != HIFA4_OK) return st;
+  if (max_total < 0 || max_new < 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "max_total and max_new must be >= 0");
+  if (!block_table || !seq_lens || !counts || !free_pages || !num_free || !out_lens || !out_free || !cu_new ||
+      (max_total > 0 && (!positions || !slots)))
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if ((st = check_aligned4({block_table, seq_lens, counts, free_pages, num_free, shift, out_lens, out_free, cu_new,
+                            positions})) != HIFA4_OK)
+    return st;
+  if (!aligned(slots, 8)) return fail(HIFA4_ERR_INVALID_ARGUMENT, "pointer %p is not 8-byte aligned", (void*)slots);
+  hifa4::PagedExtend a;
+  a.batch = batch;
+  a.max_pages = max_pages;
+  a.capacity = capacity;
+  a.max_total = max_total;
+  a.max_new = std::min(max_new, max_total);
+  a.table = block_table;
+  a.lens = seq_lens;
+  a.counts = counts;
+  a.free = free_pages;
+  a.num_free = num_free;
+  a.shift = shift;
+  a.out_lens = out_lens;
+  a.out_free = out_free;
+  a.cu = cu_new;
+  a.positions = positions;
+  a.slots = slots;
+  if ((size_t)batch * hifa4::extend_chunks(a.max_new) >= hifa4::kMaxGrid)
+    return fail(HIFA4_ERR_UNSUPPORTED, "up to %d new tokens of each of %d sequences are too many for one launch", a.max_new, batch);
+  const hipError_t e = hifa4::launch_paged_extend(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged extend");
+  return HIFA4_OK;
+}
+
+size_t hifa4_paged_release_workspace_bytes(int32_t batch) {
+  if (check_table(batch, 1, 1) != HIFA4_OK) return 0;
+  return ((size_t)batch + 1) * 4;
+}
+
+hifa4_status hifa4_paged_release(int32_t batch, int32_t max_pages, const int32_t* table, const int32_t* first,
+                                 const int32_t* to, int32_t* free_pages, int32_t capacity, const int32_t* num_free,
+                                 int32_t* out_free, void* workspace, size_t workspace_bytes, void* stream) {
+  hifa4_status st = check_table(batch, max_pages, capacity);
+  if (st != HIFA4_OK) return st;
+  if (!table || !to || !free_pages || !num_free || !out_free) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if ((st = check_aligned4({table, first, to, free_pages, num_free, out_free, workspace})) != HIFA4_OK) return st;
+  const size_t need = hifa4_paged_release_workspace_bytes(batch);
+  if (!workspace || workspace_bytes < need)
+    return fail(HIFA4_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
+  hifa4::PagedRelease a;
+  a.batch = batch;
+  a.max_pages = max_pages;
+  a.capacity = capacity;
+  a.table = table;
+  a.first = first;
+  a.to = to;
+  a.num_free = num_free;
+  a.free = free_pages;
+  a.out_free = out_free;
+  a.ws = (int*)workspace;
+  const hipError_t e = hifa4::launch_paged_release(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged release");
+  return HIFA4_OK;
+}
+
+hifa4_status hifa4_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                                    double low, double high, uint64_t* turns) {
+  if (rot_dim <= 0 || rot_dim % 8 || rot_dim > 256)
+    return fail(HIFA4_ERR_UNSUPPORTED, "rot_dim %d is no multiple of 8 between 8 and 256", rot_dim);
+  if (scaling < HIFA4_ROPE_NONE || scaling > HIFA4_ROPE_PARTS) return fail(HIFA4_ERR_INVALID_ARGUMENT, "unknown scaling %d", scaling);
+  if (!std::isfinite(base) || base <= 1.0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "base must be finite and > 1");
+  if (scaling != HIFA4_ROPE_NONE && (!std::isfinite(factor) || factor < 1.0))
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "factor must be finite and >= 1");
+  if (scaling == HIFA4_ROPE_PARTS && !(std::isfinite(original_len) && original_len > 0.0 && low >= 0.0 && high > low && std::isfinite(high)))
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "needs original_len > 0 and 0 <= low < high");
+  if (!turns) return fail(HIFA4_ERR_INVALID_ARGUMENT, "turns is NULL");
+  const double two_pi = 6.283185307179586476925;
+  if (scaling == HIFA4_ROPE_NTK) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double w = std::pow(base, -2.0 * i / rot_dim);
+    if (scaling == HIFA4_ROPE_LINEAR) w /= factor;
+    if (scaling == HIFA4_ROPE_PARTS) {
+      const double g = std::min(1.0, std::max(0.0, (original_len * w / two_pi - low) / (high - low)));
+      w *= g + (1.0 - g) / factor;
+    }
+    turns[i] = (uint64_t)std::llround(std::ldexp(w / two_pi, 62)) << 2;      // w <= 1: less than a sixth of a turn
+  }
+  return HIFA4_OK;
+}
+
+namespace {
+
+// One of q and k: heads > 0 rows that may be read, and written, by 16 bytes.
+hifa4_status rope_rows(hifa4::RopeRows* r, const char* name, int32_t tokens, int32_t D, int32_t heads, const void* x,
+                       int64_t x_stride, void* y, int64_t y_stride) {
+  *r = hifa4::RopeRows{(const hifa4::half_t*)x, (hifa4::half_t*)y, (long)x_stride, (long)y_stride, heads};
+  if (heads < 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "%s: heads must be >= 0", name);
+  if (heads == 0 || tokens == 0) return HIFA4_OK;
+  if (!x || !y) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  const int64_t row = (int64_t)heads * D;
+  if (x_stride < row || y_stride < row || x_stride % 8 || y_stride % 8)
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "%s: strides must be multiples of 8 of at least %lld", name, (long long)row);
+  if (x_stride >= (1LL << 31) || y_stride >= (1LL << 31)) return fail(HIFA4_ERR_UNSUPPORTED, "%s: strides of 2^31 elements and more", name);
+  if (x == y && x_stride != y_stride) return fail(HIFA4_ERR_INVALID_ARGUMENT, "%s: in place the strides must be equal", name);
+  return check_aligned16({x, y});
+}
+
+}  // namespace
+
+hifa4_status hifa4_rope(int32_t head_dim, int32_t rot_dim, int32_t interleaved, int32_t transposed, float magnitude,
+                        const uint64_t* turns, int32_t num_tokens, const int32_t* positions, int32_t num_heads_q, const void* q,
+                        int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t num_heads_k, const void* k,
+                        int64_t k_stride, void* k_out, int64_t k_out_stride, void* stream) {
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256)
+    return fail(HIFA4_ERR_UNSUPPORTED, "head_dim %d not in {64, 128, 256}", head_dim);
+  if (rot_dim <= 0 || rot_dim % 8 || rot_dim > head_dim)
+    return fail(HIFA4_ERR_UNSUPPORTED, "rot_dim %d is no multiple of 8 between 8 and head_dim", rot_dim);
+  if ((interleaved != 0 && interleaved != 1) || (transposed != 0 && transposed != 1))
+    return fail(HIFA4_ERR_INVALID_ARGUMENT, "interleaved and transposed must be 0 or 1");
+  if (!std::isfinite(magnitude)) return fail(HIFA4_ERR_INVALID_ARGUMENT, "magnitude must be finite");
+  if (num_tokens < 0) return fail(HIFA4_ERR_INVALID_ARGUMENT, "num_tokens must be >= 0");
+  hifa4::RopeArgs a;
+  hifa4_status st = rope_rows(&a.q, "q", num_tokens, head_dim, num_heads_q, q, q_stride, q_out, q_out_stride);
+  if (st != HIFA4_OK) return st;
+  if ((st = rope_rows(&a.k, "k", num_tokens, head_dim, num_heads_k, k, k_stride, k_out, k_out_stride)) != HIFA4_OK) return st;
+  if ((int64_t)num_heads_q + num_heads_k >= (1 << 24) || (int64_t)num_tokens >= (1 << 25))
+    return fail(HIFA4_ERR_UNSUPPORTED, "too many tokens or heads for one launch");
+  if (num_tokens == 0 || num_heads_q + num_heads_k == 0) return HIFA4_OK;
+  if (!turns || !positions) return fail(HIFA4_ERR_INVALID_ARGUMENT, "null tensor pointer");
+  if (!aligned(turns, 8)) return fail(HIFA4_ERR_INVALID_ARGUMENT, "pointer %p is not 8-byte aligned", (const void*)turns);
+  if ((st = check_aligned4({positions})) != HIFA4_OK) return st;
+  a.pos = positions;
+  a.turns = turns;
+  a.tokens = num_tokens;
+  a.D = head_dim;
+  a.rot = rot_dim;
+  a.interleaved = interleaved != 0;
+  a.transposed = transposed != 0;
+  a.magnitude = magnitude;
+  const hipError_t e = hifa4::launch_rope(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "rope");
   return HIFA4_OK;
 }
 

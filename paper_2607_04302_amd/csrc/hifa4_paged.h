@@ -107,6 +107,18 @@ struct PagedEvict {
   int *out_table, *out_lens, *freed, *num_freed;
   float* out_w;
 };
+struct PagedExtend {
+  int batch, max_pages, capacity, max_total, max_new;
+  int* table;
+  const int *lens, *counts, *free, *num_free, *shift;      // shift may be NULL: 0
+  int *out_lens, *out_free, *cu, *positions;
+  int64_t* slots;
+};
+struct PagedRelease {
+  int batch, max_pages, capacity;
+  const int *table, *first, *to, *num_free;                // first may be NULL: 0
+  int *free, *out_free, *ws;                               // ws [batch + 1]
+};
 struct PagedDecode {
   PagedCache c;
   int hq;
@@ -117,6 +129,18 @@ struct PagedDecode {
   const float* w_in;      // page weights, or NULL
   float* w_out;
   float decay, scale;     // scale = log2(e) / sqrt(D)
+  uint8_t* ws;
+};
+
+struct PagedChunk {
+  PagedCache c;
+  int hq, total, max_new;
+  const int* cu;          // [batch + 1]
+  const half_t* q;
+  const float* s;
+  half_t* o;
+  float* lse;             // [hq, total]
+  float scale;            // log2(e) / sqrt(D)
   uint8_t* ws;
 };
 
@@ -131,9 +155,17 @@ constexpr int paged_append_threads(int D, bool fp16) { return fp16 ? 256 : 2 * D
 bool paged_decode_fits(const PagedCache& c, int hq, bool weights);
 size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights);
 
+bool paged_chunk_fits(const PagedCache& c, int hq, int total, int max_new);
+size_t paged_chunk_workspace(const PagedCache& c, int hq, int total, int max_new);
+
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st);
 hipError_t launch_paged_gather(const PagedGather& a, hipStream_t st);
 hipError_t launch_paged_evict(const PagedEvict& a, hipStream_t st);
+// Workgroups that a row's new tokens are cut into.
+int extend_chunks(int max_new);
+hipError_t launch_paged_extend(const PagedExtend& a, hipStream_t st);
+hipError_t launch_paged_release(const PagedRelease& a, hipStream_t st);
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st);
+hipError_t launch_paged_chunk(const PagedChunk& a, hipStream_t st);
 
 }  // namespace hifa4

@@ -18,6 +18,7 @@
 #include "hifa4_device.h"
 #include "hifa4_packed.h"
 #include "hifa4_paged.h"
+#include "hifa4_paged_device.h"
 #include "hifa4_words.h"
 
 #include <algorithm>
@@ -25,7 +26,6 @@
 namespace hifa4 {
 
 typedef int i8v_t __attribute__((ext_vector_type(8)));
-typedef float f4v_t __attribute__((ext_vector_type(4)));
 typedef short s2v_t __attribute__((ext_vector_type(2)));
 
 // Query heads that a wave takes: the 16 columns of a matrix product, four for
@@ -61,9 +61,6 @@ struct Run {
   int first, count;               // the sequence's runs: [first, first + count)
 };
 
-__device__ __forceinline__ int pages_of(const PagedCache& c, int b) {
-  return b < c.batch ? (paged_len(c, b) + kPage - 1) / kPage : 0;
-}
 // The sequences are dealt to the lanes of a wave (b, b + 64, ...), the units of
 // a lane's first kHeldSeqs in registers.
 constexpr int kHeldSeqs = 4;
@@ -146,15 +143,6 @@ size_t paged_decode_workspace(const PagedCache& c, int hq, bool weights) {
   return slots * hq * (c.D + 2) * 4 + (size_t)c.batch * 8 + (weights ? (size_t)c.batch * c.max_pages * page_units(c.D, c.fp16) * hq * 8 : 0);
 }
 
-// q s to fp16, the exact product rounded once: the fp32 product made odd where
-// it is not exact, so that the second rounding is the only one.
-__device__ __forceinline__ half_t round_product(half_t q, float s) {
-  const float p = (float)q * s, e = fmaf((float)q, s, -p);
-  uint32_t b = __float_as_uint(p);
-  if ((__float_as_uint(e) ^ b) & 0x80000000u) b -= e != 0.0f;      // |p| is above the product: one step toward zero
-  return (half_t)__uint_as_float(e != 0.0f ? b | 1u : b);
-}
-
 // ---------------------------------------------------------------------------
 // HIF4 pages.  One wave per (run, kv head, four query heads).
 //
@@ -200,18 +188,6 @@ constexpr int kDigitRow = 68;
 // float whose bits are byte << 21 = b 2^-96, and an operand's sum is 4 values.
 constexpr uint32_t kUnit = 127 + 94;
 
-// x and y lane values of (own, partner) exchanges
-__device__ __forceinline__ float max_across_rows(float v) {      // over the four lanes of a column
-  const Pair32 p = pair32(__float_as_uint(v));
-  v = fmaxf(__uint_as_float(p.x), __uint_as_float(p.y));
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float sum_across_rows(float v) {
-  v = add_with_partner(v);
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 // over the four pieces of a query (the same bits in each of the four lanes)
 __device__ __forceinline__ float sum_pieces(float v) {
   v += __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xB1, 0xF, 0xF, true));
@@ -250,18 +226,6 @@ struct Part {
   uint32_t e2;
   uint32_t base;           // G bytes of the 64 G, in the record's order
 };
-// A scalar address that the compiler takes as given: sums with a lane's 32-bit
-// offset stay in that form instead of becoming 64-bit vector additions.
-typedef const __attribute__((address_space(1))) uint8_t* global_ptr;
-__device__ __forceinline__ global_ptr scalar_address(const uint8_t* p) {
-  global_ptr g = (global_ptr)p;
-  asm("" : "+s"(g));
-  return g;
-}
-template <typename T>
-__device__ __forceinline__ T load_at(global_ptr p, uint32_t offset) {
-  return *(const __attribute__((address_space(1))) T*)(p + offset);
-}
 template <int G>
 __device__ __forceinline__ void load_part(Part<G>& p, const uint8_t* part, uint32_t lane, uint32_t base_lane) {
   typedef unsigned u4v_t __attribute__((ext_vector_type(4)));
@@ -361,20 +325,6 @@ __device__ __forceinline__ void products(const Part<G>& p, float* spread, int la
 // The FP8 operand of two words, each twice (x: the FP4 lane j's, y: lane 2 + j's).
 __device__ __forceinline__ i8v_t fp8_operand(uint4 x, uint4 y) {
   return i8v_t{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
-}
-
-// Nothing is scheduled across: a page's loads stay between the last use of the
-// registers that they fill and the next page's, K's before V's, so that they
-// need no registers of their own and a wait for K's does not wait for V's.
-__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
-
-// The pages of a run, as their records: 64 table entries at a time, one a lane.
-struct Pages {
-  int mine, base;
-};
-__device__ __forceinline__ void load_pages(Pages& p, const PagedCache& c, int b, int from, int last, int lane) {
-  p.base = from;
-  p.mine = from + lane <= last ? c.table[(size_t)b * c.max_pages + from + lane] : -1;
 }
 
 // The digits of four query heads' rows (q: the first of them, `rows` exist) in
@@ -630,20 +580,8 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : G == 2 ? 2 : 3) k_runs_hif4(P
 // counts from is held itself, not the score 7 binades above it: of scores over
 // 2^24 that difference is no number, and p would pass fp16's range.
 // Bound by the reads: D=128, 8 x 8192 tokens (268 MB) in 51 us, 5.2 TB/s.
-typedef half_t h8v_t __attribute__((ext_vector_type(8)));
 typedef half_t h4v_t __attribute__((ext_vector_type(4)));
 constexpr float kTop16 = 7.0f, kSlack16 = 8.0f;
-
-template <int N, int kStep>
-__device__ __forceinline__ void load_operands(h8v_t (&x)[N], const uint8_t* p, uint32_t lane) {
-  constexpr int kSome = 4096 / kStep;
-#pragma unroll
-  for (int i = 0; i < N; i += kSome) {
-    const global_ptr at = scalar_address(p + kStep * i);
-#pragma unroll
-    for (int u = 0; u < kSome; ++u) x[i + u] = load_at<h8v_t>(at, 16 * lane + kStep * u);
-  }
-}
 
 template <int G>
 __global__ void __launch_bounds__(64, G == 1 ? 3 : G == 2 ? 2 : 1) k_runs_fp16(PagedDecode a, int tiles) {

@@ -1,0 +1,112 @@
+// Rotary positions: the pair (x, y) of frequency w at position p becomes
+//   (x cos pw - y sin pw, x sin pw + y cos pw) times a magnitude;
+// the pairs are the channels (i, i + r/2) or (2i, 2i + 1) of the first r.
+//
+// Angles are counted in turns, as whole numbers of 2^-64: p times the frequency's
+// turns, taken modulo one turn, is an integer product whose carry is dropped.  It
+// is as near at position 2^30 as at position 1 (an angle in fp32 is off by 2^-24 of
+// itself: by 0.06 rad at a million).  What is left of the angle after its quarter
+// turns lies within pi/4, where the series of sine and cosine are cut behind the
+// 9th and 10th power (errors below 2^-28).  The rotated values are rounded once, to
+// fp16.
+#include "hifa4_rope.h"
+
+#include <algorithm>
+
+namespace hifa4 {
+
+typedef half_t h8v_t __attribute__((ext_vector_type(8)));
+typedef half_t h4v_t __attribute__((ext_vector_type(4)));
+
+// (cos, sin) of 2 pi times the fraction t 2^-64.
+__device__ __forceinline__ float2 unit_of(uint64_t t) {
+  const uint32_t quarter = (uint32_t)((t + (1ull << 61)) >> 62);
+  const int rest = (int)(uint32_t)((t - ((uint64_t)quarter << 62)) >> 32);       // within 2^29, units of 2^-32
+  const float x = (float)rest * 0x1.921fb6p-30f, z = x * x;                     // 2 pi 2^-32
+  float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
+  s = fmaf(s, z, 8.3333333e-3f);
+  s = fmaf(s, z, -1.6666667e-1f);
+  s = fmaf(s * z, x, x);
+  float c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
+  c = fmaf(c, z, -1.3888889e-3f);
+  c = fmaf(c, z, 4.1666667e-2f);
+  c = fmaf(c, z, -0.5f);
+  c = fmaf(c, z, 1.0f);
+  const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+  return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
+}
+
+// A lane keeps its place in the head (2 V channels: V and their partners, or V pairs,
+// or 2 V that are only copied) and its V angles, and goes through the heads of one token.
+template <int V, bool kInterleaved>
+__global__ void __launch_bounds__(256) k_rope(RopeArgs a, int units, int slices) {
+  typedef half_t vec_t __attribute__((ext_vector_type(V)));
+  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int token = (int)(item / slices), slice = (int)(item % slices), lane = threadIdx.x & 63;
+  if (token >= a.tokens) return;
+  const int pos = a.pos[token];
+  if (pos < 0) return;
+  const int u = lane % units, per = 64 / units, heads = a.q.heads + a.k.heads;
+  const bool rotates = u < a.rot / (2 * V);
+  const int at0 = kInterleaved || !rotates ? 2 * V * u : V * u, at1 = kInterleaved || !rotates ? at0 + V : at0 + a.rot / 2;
+  float2 w[V];
+  if (rotates) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      w[i] = unit_of((uint64_t)pos * a.turns[V * u + i]);
+      w[i].x *= a.magnitude;
+      w[i].y *= a.transposed ? -a.magnitude : a.magnitude;
+    }
+  }
+  for (int h = slice * per + lane / units; h < heads; h += slices * per) {
+    const bool is_q = h < a.q.heads;
+    const RopeRows& r = is_q ? a.q : a.k;
+    const int head = is_q ? h : h - a.q.heads;
+    const half_t* x = r.x + token * r.x_stride + (long)head * a.D;
+    half_t* y = r.y + token * r.y_stride + (long)head * a.D;
+    const vec_t x0 = *reinterpret_cast<const vec_t*>(x + at0), x1 = *reinterpret_cast<const vec_t*>(x + at1);
+    vec_t y0 = x0, y1 = x1;
+    if (rotates) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (kInterleaved) {
+          const vec_t& in = i < V / 2 ? x0 : x1;
+          const float p = (float)in[2 * i % V], q = (float)in[2 * i % V + 1];
+          vec_t& out = i < V / 2 ? y0 : y1;
+          out[2 * i % V] = (half_t)(p * w[i].x - q * w[i].y);
+          out[2 * i % V + 1] = (half_t)(p * w[i].y + q * w[i].x);
+        } else {
+          const float p = (float)x0[i], q = (float)x1[i];
+          y0[i] = (half_t)(p * w[i].x - q * w[i].y);
+          y1[i] = (half_t)(p * w[i].y + q * w[i].x);
+        }
+      }
+    }
+    *reinterpret_cast<vec_t*>(y + at0) = y0;
+    *reinterpret_cast<vec_t*>(y + at1) = y1;
+  }
+}
+
+template <int V>
+static void launch(const RopeArgs& a, hipStream_t st) {
+  const int units = a.D / (2 * V), per = 64 / units, heads = a.q.heads + a.k.heads;
+  // a token's heads are shared out among waves while there are few tokens
+  const int most = (heads + per - 1) / per;
+  const int slices = std::max(1, std::min(most, 4096 / std::max(1, a.tokens)));
+  const long items = (long)a.tokens * slices;
+  const dim3 grid((unsigned)((items + 3) / 4));
+  if (a.interleaved)
+    k_rope<V, true><<<grid, 256, 0, st>>>(a, units, slices);
+  else
+    k_rope<V, false><<<grid, 256, 0, st>>>(a, units, slices);
+}
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st) {
+  if (a.rot % 16 == 0)
+    launch<8>(a, st);
+  else
+    launch<4>(a, st);
+  return hipGetLastError();
+}
+
+}  // namespace hifa4

@@ -27,6 +27,7 @@ typedef half_t h4v_t __attribute__((ext_vector_type(4)));
 // What the heaviest key so far counts: between 2^kTop and 2^(kTop + kSlack), below
 // fp16's range; the softmax's reference moves when a score passes that.
 constexpr float kTop = 7.0f, kSlack = 8.0f;
+constexpr float kNoRef = -1e30f;        // before any key
 
 // ---------------------------------------------------------------------------
 // The plan: items (sequence, tile of rows, run of pages), the same for every kv head.
@@ -121,8 +122,8 @@ __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const 
       it.tile = t - 1 - (r - at) % t;
       it.runs = n;
       const long pages = tile_pages(s, group, cut, it.tile);
-      it.begin = (int)(pages * it.run / n);
-      it.end = (int)(pages * (it.run + 1) / n);
+      it.begin = __builtin_amdgcn_readfirstlane((int)(pages * it.run / n));
+      it.end = __builtin_amdgcn_readfirstlane((int)(pages * (it.run + 1) / n));
       it.join = n > 1 ? it.join + it.tile : -1;
       it.slot = n > 1 ? it.slot + it.tile * n : -1;
       return true;
@@ -273,7 +274,7 @@ struct Rows16 {
 template <int G>
 __device__ __forceinline__ void start(Rows16<G>& x) {
   const f4v_t z = {0.0f, 0.0f, 0.0f, 0.0f};
-  x.ref = -1e30f;
+  x.ref = kNoRef;
   x.l = 0.0f;
   x.sum = z;
 #pragma unroll
@@ -284,8 +285,6 @@ __device__ __forceinline__ void start(Rows16<G>& x) {
 // operands; keys behind `seen` (the row's limit in the page) do not count.
 template <int G, bool kFp16>
 __device__ __forceinline__ void soften(Rows16<G>& x, f4v_t (&s)[4], h8v_t (&p)[2], float scale, bool masked, int seen, int k) {
-#pragma unroll
-  for (int t = 0; t < 4; ++t) s[t] *= scale;
   if (masked) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -298,6 +297,7 @@ __device__ __forceinline__ void soften(Rows16<G>& x, f4v_t (&s)[4], h8v_t (&p)[2
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int v = 0; v < 4; ++v) top = fmaxf(top, s[t][v]);
+  top *= scale;
   if (__builtin_amdgcn_ballot_w64(top - x.ref > kTop + kSlack)) {
     const float to = fmaxf(x.ref, max_across_rows(top) - kTop), f = __builtin_amdgcn_exp2f(x.ref - to);
     x.ref = to;
@@ -306,12 +306,20 @@ __device__ __forceinline__ void soften(Rows16<G>& x, f4v_t (&s)[4], h8v_t (&p)[2
 #pragma unroll
     for (int c = 0; c < 4 * G; ++c) x.o[c] *= f;
   }
+  // The exponent in one operation, the product not rounded; of scores over 2^20 it is
+  // rounded as the reference's was (half a step there is more than p's range).
+  float by = scale;
+  if (__builtin_amdgcn_ballot_w64(fabsf(x.ref) > 0x1p20f && x.ref != kNoRef)) {
+    by = 1.0f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] *= scale;
+  }
   float l = 0.0f;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      s[t][v] = __builtin_amdgcn_exp2f(s[t][v] - x.ref);
+      s[t][v] = __builtin_amdgcn_exp2f(fmaf(s[t][v], by, -x.ref));
       l += s[t][v];
     }
   x.l += l;
@@ -516,6 +524,202 @@ __global__ void __launch_bounds__(64, chunk_waves(64 * G, kFp16, NB)) k_chunk_ro
 }
 
 // ---------------------------------------------------------------------------
+// Many rows: kWaves waves of 32 rows each share a page, whose operands they make in
+// LDS (two pages' room: the next one is made while this one is used).  A record's KiB
+// unit of fp16 operands is what a wave reads for one operand of a product, 16 bytes a
+// lane in lane order, so neither reads nor writes have bank conflicts.
+// Units of a page: K [t][c], then V [channels / 16][c].
+constexpr int kWideRows = 32;           // of a wave
+
+// A quarter of a tile's part of a HIF4 record: the words (t, c) of two t.
+struct HifQuad {
+  uint4 code;
+  uint32_t e3, e2;
+  uint2 base;
+};
+template <int G>
+__device__ __forceinline__ void load_quad(HifQuad& q, const uint8_t* rec, int at, int lane) {
+  typedef unsigned u4v_t __attribute__((ext_vector_type(4)));
+  typedef unsigned u2v_t __attribute__((ext_vector_type(2)));
+  const int tile = at / 2 % G, half = at & 1;
+  const uint8_t* part = rec + at / (2 * G) * (2304 * G);
+  const global_ptr code = (global_ptr)(part + 2048 * tile + 1024 * half);
+  const global_ptr meta = (global_ptr)(part + 2048 * G);
+  q.code = __builtin_bit_cast(uint4, load_at<u4v_t>(code, 16 * lane));
+  if (G == 1)
+    q.e3 = load_at<uint16_t>(meta, 2 * lane);
+  else
+    q.e3 = load_at<uint32_t>(meta, 2 * G * lane + 4 * (tile >> 1));
+  q.e2 = load_at<uint8_t>(meta, 128 * G + G * lane + tile);
+  q.base = __builtin_bit_cast(uint2, load_at<u2v_t>(meta, 192 * G + 16 * G * ((lane & 15) >> 2) + 16 * tile + 8 * half));
+}
+template <int G>
+__device__ __forceinline__ void store_quad(h8v_t* page, const HifQuad& q, int at, int lane) {
+  const int tile = at / 2 % G, half = at & 1;
+  const bool is_v = at >= 2 * G;
+  const uint32_t e3 = (G == 1 ? (q.e3 & 0xFFu) | ((q.e3 & 0xFF00u) << 8) : q.e3) >> (8 * (tile & 1) + 4 * half);
+  const uint32_t e2 = (q.e2 * 0x10001u) >> (4 * half);
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const half_t b = (half_t)__uint_as_float((((u ? q.base.y : q.base.x) >> (8 * (lane & 3)) & 0xFFu) << 21) + 0x30000000u);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint32_t word = u ? (c ? q.code.w : q.code.z) : (c ? q.code.y : q.code.x);
+      const uint32_t two = 0x3C003C00u - exponent_bit(e3, 2 * u + c) - exponent_bit(e2, 2 * u + c);
+      const int t = 2 * half + u, unit = is_v ? 8 * G + (4 * tile + t) * 2 + c : t * 2 * G + 2 * tile + c;
+      page[64 * unit + lane] = hif4_operand(word, h2_t{b, b} * __builtin_bit_cast(h2_t, two));
+    }
+  }
+}
+
+// What a wave fetches of a page, and puts into LDS.
+template <int G, bool kFp16, int kWaves>
+struct WideShare {
+  static constexpr int kAll = kFp16 ? 16 * G : 4 * G, kMine = (kAll + kWaves - 1) / kWaves;
+  h8v_t unit[kFp16 ? kMine : 1];
+  HifQuad quad[kFp16 ? 1 : kMine];
+  __device__ __forceinline__ void load(const uint8_t* rec, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int at = wave + kWaves * i;
+      if (kAll % kWaves && at >= kAll) break;
+      if constexpr (kFp16)
+        unit[i] = load_at<h8v_t>((global_ptr)(rec + 1024 * at), 16 * lane);
+      else
+        load_quad<G>(quad[i], rec, at, lane);
+    }
+  }
+  __device__ __forceinline__ void store(h8v_t* page, int wave, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int at = wave + kWaves * i;
+      if (kAll % kWaves && at >= kAll) break;
+      if constexpr (kFp16)
+        page[64 * at + lane] = unit[i];
+      else
+        store_quad<G>(page, quad[i], at, lane);
+    }
+  }
+};
+
+template <int G, bool kFp16, int kWaves>
+__global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut) {
+  constexpr int D = 64 * G, kRows = kWideRows * kWaves, NB = 2, kUnits = 16 * G;
+  extern __shared__ __align__(16) uint8_t smem[];
+  h8v_t* const pages = reinterpret_cast<h8v_t*>(smem);
+  const int lane = threadIdx.x & 63, n = lane & 15, k = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
+  Item it;
+  int joins;
+  const bool there = find_item(a, group, cut, blockIdx.x / a.c.hkv, lane, it, joins);
+  const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *ws.joins = joins;
+  if (!there) return;
+  if (it.runs > 1 && it.run == 0 && head == 0 && threadIdx.x == 0) ws.split[it.join] = Split{it.b, it.tile, it.slot, it.runs};
+
+  // pages from here on that are some; the table's entries 64 at a time, one a lane
+  Pages pg;
+  pg.base = it.begin - 64;
+  int page_at = 0;                        // the page that next() has found
+  const auto next = [&](int j) {
+    for (; j < it.end; ++j) {
+      if (j - pg.base >= 64) load_pages(pg, a.c, it.b, j, it.end - 1, lane);
+      page_at = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
+      if ((unsigned)page_at < (unsigned)a.c.num_pages) break;
+    }
+    return __builtin_amdgcn_readfirstlane(j);
+  };
+  const auto record = [&] {
+    const size_t at = (size_t)__builtin_amdgcn_readfirstlane(page_at) * a.c.hkv + head;
+    return a.c.pool + at * paged_record_bytes(D, kFp16);
+  };
+  WideShare<G, kFp16, kWaves> share;
+  int j = next(it.begin);
+  if (j < it.end) share.load(record(), wave, lane);
+
+  const int row0 = it.tile * kRows + wave * kWideRows;      // the wave's first row
+  Row row[NB];
+  Rows16<G> x[NB];
+  h8v_t q[NB][2 * G];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    row[i] = row_of(a, it, group, head, row0 + 16 * i + n);
+    load_query<G, kFp16>(q[i], a, row[i], head, k);
+    start(x[i]);
+  }
+  // keys that every row of the wave sees, and that any of them sees: up to these
+  const int first_token = row0 / group, last_token = min(it.seq.n - 1, (row0 + kWideRows - 1) / group);
+  const int all_see = it.seq.base + first_token, some_see = first_token < it.seq.n ? it.seq.base + last_token : -1;
+
+  int ahead = next(j + 1), at = 0;
+  if (j < it.end) share.store(pages, wave, lane);
+  if (ahead < it.end) share.load(record(), wave, lane);
+  __syncthreads();
+  while (j < it.end) {
+    const h8v_t* page = pages + 64 * kUnits * at + lane;
+    const int now = j;
+    j = ahead;
+    if (j < it.end) {
+      share.store(pages + 64 * kUnits * (at ^ 1), wave, lane);
+      ahead = next(j + 1);
+      if (ahead < it.end) share.load(record(), wave, lane);
+    }
+    if (now * kPage <= some_see) {
+      const bool masked = now * kPage + kPage - 1 > all_see;
+      f4v_t s[NB][4];
+      h8v_t p[NB][2];
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < 2 * G; ++c)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const h8v_t kr = page[64 * (t * 2 * G + c)];
+#pragma unroll
+          for (int i = 0; i < NB; ++i) s[i][t] = product(kr, q[i][c], s[i][t]);
+        }
+#pragma unroll
+      for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], s[i], p[i], a.scale, masked, row[i].limit - now * kPage, k);
+#pragma unroll
+      for (int u = 0; u < 4 * G; ++u) {
+        h8v_t v[2] = {page[64 * (8 * G + 2 * u)], page[64 * (8 * G + 2 * u + 1)]};
+        if (kFp16 && masked) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (now * kPage + 16 * k + 8 * c + e > some_see) v[c][e] = (half_t)0;
+          if (__builtin_amdgcn_ballot_w64(any_not_finite(v[0]) || any_not_finite(v[1]))) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) add_not_finite<G>(x[i], v, u, row[i].limit - now * kPage, k);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (!(v[c][e] < (half_t)INFINITY && v[c][e] > -(half_t)INFINITY)) v[c][e] = (half_t)0;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < NB; ++i) x[i].o[u] = product(v[c], p[i][c], x[i].o[u]);
+      }
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+    }
+    at ^= 1;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) finish<G>(a, ws, it, x[i], row[i], head, kRows, wave * kWideRows + 16 * i + n, k);
+}
+
+// ---------------------------------------------------------------------------
 // Joining the runs of a split tile's rows: with m the largest of their references,
 // o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in the
 // runs' order.  One workgroup per row; its threads share out channels and runs.
@@ -575,10 +779,17 @@ __global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCu
 }
 
 // ---------------------------------------------------------------------------
+// Waves of a workgroup that share a page.
+constexpr int wide_waves(int D, bool fp16) { return 4; }
+
 static bool chunk_cut(const PagedCache& c, int hq, int total, int max_new, ChunkCut* cut) {
   const size_t group = hq / c.hkv;
-  cut->rows = max_new * group <= 16 || c.D == 256 ? 16 : 32;
-  cut->target = std::max(1, 1024 * chunk_waves(c.D, c.fp16, cut->rows / 16) / c.hkv);
+  const size_t most = max_new * group;
+  cut->rows = most <= 16 ? 16 : most <= 32 ? (c.D == 256 ? 16 : 32) : kWideRows * wide_waves(c.D, c.fp16);
+  if (cut->rows <= 32)
+    cut->target = std::max(1, 1024 * chunk_waves(c.D, c.fp16, cut->rows / 16) / c.hkv);
+  else
+    cut->target = std::max(1, 1024 * (c.D == 256 ? 1 : 2) / wide_waves(c.D, c.fp16) / c.hkv);
   const size_t tiles = std::min((size_t)c.batch * ((max_new * group + cut->rows - 1) / cut->rows),
                                 (size_t)total * group / cut->rows + c.batch);
   const size_t runs = std::max<size_t>(1, ((size_t)c.max_pages + kMinRun - 1) / kMinRun);
@@ -601,33 +812,32 @@ size_t paged_chunk_workspace(const PagedCache& c, int hq, int total, int max_new
 }
 
 template <int G, bool kFp16>
-static void launch_rows(const PagedChunk& a, const ChunkCut& cut, hipStream_t st) {
+static hipError_t launch_rows(const PagedChunk& a, const ChunkCut& cut, hipStream_t st) {
   const dim3 grid((unsigned)((size_t)cut.items * a.c.hkv));
-  if (G == 4 || cut.rows == 16)
+  if (cut.rows > 32) {
+    constexpr int kWaves = wide_waves(64 * G, kFp16);
+    constexpr size_t kLds = (size_t)2 * 16 * G * 1024;
+    if (kLds > 65536) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_chunk_wide<G, kFp16, kWaves>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+      if (e != hipSuccess) return e;
+    }
+    k_chunk_wide<G, kFp16, kWaves><<<grid, 64 * kWaves, kLds, st>>>(a, cut);
+  } else if (G == 4 || cut.rows == 16)
     k_chunk_rows<G, kFp16, 1><<<grid, 64, 0, st>>>(a, cut);
   else
     k_chunk_rows<G == 4 ? 1 : G, kFp16, 2><<<grid, 64, 0, st>>>(a, cut);
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_chunk(const PagedChunk& a, hipStream_t st) {
   ChunkCut cut;
   if (!chunk_cut(a.c, a.hq, a.total, a.max_new, &cut)) return hipErrorInvalidValue;
-  if (a.c.fp16) {
-    if (a.c.D == 64)
-      launch_rows<1, true>(a, cut, st);
-    else if (a.c.D == 128)
-      launch_rows<2, true>(a, cut, st);
-    else
-      launch_rows<4, true>(a, cut, st);
-  } else {
-    if (a.c.D == 64)
-      launch_rows<1, false>(a, cut, st);
-    else if (a.c.D == 128)
-      launch_rows<2, false>(a, cut, st);
-    else
-      launch_rows<4, false>(a, cut, st);
-  }
-  const hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (a.c.fp16)
+    e = a.c.D == 64 ? launch_rows<1, true>(a, cut, st) : a.c.D == 128 ? launch_rows<2, true>(a, cut, st) : launch_rows<4, true>(a, cut, st);
+  else
+    e = a.c.D == 64 ? launch_rows<1, false>(a, cut, st) : a.c.D == 128 ? launch_rows<2, false>(a, cut, st) : launch_rows<4, false>(a, cut, st);
   if (e != hipSuccess || !cut.joins) return e;
   k_chunk_join<<<dim3((unsigned)((size_t)cut.joins * a.c.hkv * cut.rows)), kChunkJoin, 0, st>>>(a, cut);
   return hipGetLastError();

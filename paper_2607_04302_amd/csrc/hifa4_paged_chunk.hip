@@ -126,6 +126,15 @@ __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const 
       it.end = __builtin_amdgcn_readfirstlane((int)(pages * (it.run + 1) / n));
       it.join = n > 1 ? it.join + it.tile : -1;
       it.slot = n > 1 ? it.slot + it.tile * n : -1;
+      it.seq.first = __builtin_amdgcn_readfirstlane(s.first);      // (the same in every lane: kept in scalar registers)
+      it.seq.n = __builtin_amdgcn_readfirstlane(s.n);
+      it.seq.len = __builtin_amdgcn_readfirstlane(s.len);
+      it.seq.base = __builtin_amdgcn_readfirstlane(s.base);
+      it.run = __builtin_amdgcn_readfirstlane(it.run);
+      it.tile = __builtin_amdgcn_readfirstlane(it.tile);
+      it.runs = __builtin_amdgcn_readfirstlane(n);
+      it.join = __builtin_amdgcn_readfirstlane(it.join);
+      it.slot = __builtin_amdgcn_readfirstlane(it.slot);
       return true;
     }
     at += t * n;
@@ -530,6 +539,7 @@ __global__ void __launch_bounds__(64, chunk_waves(64 * G, kFp16, NB)) k_chunk_ro
 // lane in lane order, so neither reads nor writes have bank conflicts.
 // Units of a page: K [t][c], then V [channels / 16][c].
 constexpr int kWideRows = 32;           // of a wave
+constexpr int kMatrix = 0x008, kDsRead = 0x100;      // kinds of instructions to the scheduler
 
 // A quarter of a tile's part of a HIF4 record: the words (t, c) of two t.
 struct HifQuad {
@@ -652,6 +662,7 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
   const int first_token = row0 / group, last_token = min(it.seq.n - 1, (row0 + kWideRows - 1) / group);
   const int all_see = it.seq.base + first_token, some_see = first_token < it.seq.n ? it.seq.base + last_token : -1;
 
+  const bool late = false;
   int ahead = next(j + 1), at = 0;
   if (j < it.end) share.store(pages, wave, lane);
   if (ahead < it.end) share.load(record(), wave, lane);
@@ -660,11 +671,14 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
     const h8v_t* page = pages + 64 * kUnits * at + lane;
     const int now = j;
     j = ahead;
-    if (j < it.end) {
-      share.store(pages + 64 * kUnits * (at ^ 1), wave, lane);
-      ahead = next(j + 1);
-      if (ahead < it.end) share.load(record(), wave, lane);
-    }
+    const auto make_next = [&] {
+      if (j < it.end) {
+        share.store(pages + 64 * kUnits * (at ^ 1), wave, lane);
+        ahead = next(j + 1);
+        if (ahead < it.end) share.load(record(), wave, lane);
+      }
+    };
+    if (!late) make_next();
     if (now * kPage <= some_see) {
       const bool masked = now * kPage + kPage - 1 > all_see;
       f4v_t s[NB][4];
@@ -673,20 +687,45 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
       for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+      // Operands come four units ahead of their products: a wave's own products have to
+      // cover LDS's latency, there are two waves a SIMD.
+      h8v_t next4[2][4];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int c = 0; c < 2 * G; ++c)
+      for (int t = 0; t < 4; ++t) next4[0][t] = page[64 * (t * 2 * G)];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const h8v_t kr = page[64 * (t * 2 * G + c)];
+      for (int c = 0; c < 2 * G; ++c) {
+        if (c + 1 < 2 * G)
 #pragma unroll
-          for (int i = 0; i < NB; ++i) s[i][t] = product(kr, q[i][c], s[i][t]);
-        }
+          for (int t = 0; t < 4; ++t) next4[(c + 1) & 1][t] = page[64 * (t * 2 * G + c + 1)];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < NB; ++i) s[i][t] = product(next4[c & 1][t], q[i][c], s[i][t]);
+      }
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+#pragma unroll
+      for (int c = 0; c < 2 * G; ++c) {
+        if (c + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
+      }
+      keep_order();
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) next4[0][u] = page[64 * (8 * G + u)];
 #pragma unroll
       for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], s[i], p[i], a.scale, masked, row[i].limit - now * kPage, k);
+      keep_order();
+      const bool odd_values = kFp16 && masked;
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int u = 0; u < 4 * G; ++u) {
-        h8v_t v[2] = {page[64 * (8 * G + 2 * u)], page[64 * (8 * G + 2 * u + 1)]};
-        if (kFp16 && masked) {
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+      if (odd_values) {
+#pragma unroll
+        for (int u = 0; u < 4 * G; ++u) {
+          h8v_t v[2] = {page[64 * (8 * G + 2 * u)], page[64 * (8 * G + 2 * u + 1)]};
 #pragma unroll
           for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -701,17 +740,32 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
               for (int e = 0; e < 8; ++e)
                 if (!(v[c][e] < (half_t)INFINITY && v[c][e] > -(half_t)INFINITY)) v[c][e] = (half_t)0;
           }
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) x[i].o[u] = product(v[c], p[i][c], x[i].o[u]);
+        }
+      } else {
+#pragma unroll
+        for (int g = 0; g < 2 * G; ++g) {
+          if (g + 1 < 2 * G)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) next4[(g + 1) & 1][u] = page[64 * (8 * G + 4 * g + 4 + u)];
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) x[i].o[2 * g + u / 2] = product(next4[g & 1][u], p[i][u & 1], x[i].o[2 * g + u / 2]);
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int i = 0; i < NB; ++i) x[i].o[u] = product(v[c], p[i][c], x[i].o[u]);
+        for (int g = 0; g < 2 * G; ++g) {
+          if (g + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+          __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
+        }
+        keep_order();
       }
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+      __builtin_amdgcn_s_setprio(0);
     }
+    if (late) make_next();
     at ^= 1;
     __syncthreads();
   }
@@ -721,66 +775,87 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
 
 // ---------------------------------------------------------------------------
 // Joining the runs of a split tile's rows: with m the largest of their references,
-// o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in the
-// runs' order.  One workgroup per row; its threads share out channels and runs.
+// o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in a fixed
+// order.  kFew: a workgroup takes 32 channels of a row, its threads share out the runs
+// (many, where there are few rows); else a wave takes a row.  The workgroups go
+// through the split tiles that there are.
 constexpr int kChunkJoin = 256;
 
+struct Joined {
+  float m, l, sum;
+  f4v_t o;
+};
+__device__ __forceinline__ void join_pair(Joined& x, const Joined& y) {
+  const float to = fmaxf(x.m, y.m), ref = to == -INFINITY ? 0.0f : to;
+  const float f = __builtin_amdgcn_exp2f(x.m - ref), g = __builtin_amdgcn_exp2f(y.m - ref);
+  x.m = to;
+  x.l = x.l * f + y.l * g;
+  x.sum = x.sum * f + y.sum * g;
+  x.o = x.o * f + y.o * g;
+}
+
+template <int G, bool kFew>
 __global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCut cut) {
-  __shared__ f4v_t part[kChunkJoin];
-  __shared__ float4 part_ml[kChunkJoin / 16];
-  const int tid = threadIdx.x, D = a.c.D, cols = D / 4, sets = kChunkJoin / cols;
-  const int row_in_tile = blockIdx.x % cut.rows, head = blockIdx.x / cut.rows % a.c.hkv, at = blockIdx.x / cut.rows / a.c.hkv;
+  constexpr int D = 64 * G, kCols = kFew ? 8 : D / 4, kSets = (kFew ? kChunkJoin : 64) / kCols, kAhead = 4;
+  __shared__ Joined part[kFew ? kChunkJoin : 1];
+  const int lane = threadIdx.x & 63, at_set = kFew ? threadIdx.x : lane, col = at_set % kCols, set = at_set / kCols;
   const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
-  if (at >= *ws.joins) return;
-  const Split sp = ws.split[at];
-  const int group = a.hq / a.c.hkv;
-  Item it;
-  it.b = sp.b;
-  it.tile = sp.tile;
-  it.seq = chunk_seq(a, sp.b);
-  const Row row = row_of(a, it, group, head, sp.tile * cut.rows + row_in_tile);
-  if (row.limit == -2) return;
-  const int col = tid % cols, set = tid / cols;
-  f4v_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-  float m = -INFINITY, l = 0.0f, sum = 0.0f;
-  for (int i = set; i < sp.runs; i += sets) {
-    const size_t from = ((size_t)(sp.slot + i) * a.c.hkv + head) * cut.rows + row_in_tile;
-    const float4 ml = ws.ml[from];
-    if (ml.x == -INFINITY) continue;      // nothing of this run counts: its o may be anything
-    const f4v_t y = *reinterpret_cast<const f4v_t*>(ws.o + from * D + 4 * col);
-    const float to = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - to), g = __builtin_amdgcn_exp2f(ml.x - to);
-    m = to;
-    l = l * f + ml.y * g;
-    sum = sum * f + ml.z * g;
-    o = o * f + y * g;
-  }
-  part[set * cols + col] = o;
-  if (col == 0) part_ml[set] = make_float4(m, l, sum, 0.0f);
-  __syncthreads();
-  if (set) return;
-  float top = -INFINITY;
-  for (int i = 0; i < sets; ++i) top = fmaxf(top, part_ml[i].x);
-  if (top == -INFINITY) top = 0.0f;
-  l = sum = 0.0f;
-  o = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < sets; ++i) {
-    const float4 ml = part_ml[i];
-    const float f = __builtin_amdgcn_exp2f(ml.x - top);
-    l += ml.y * f;
-    sum += ml.z * f;
-    o += part[i * cols + col] * f;
-  }
-  *reinterpret_cast<h4v_t*>(a.o + (size_t)row.at * D + 4 * col) = __builtin_convertvector(o * (sum == 0.0f ? 0.0f : 1.0f / sum), h4v_t);
-  if (col == 0) {
-    const int token = row.at / a.hq;
-    a.lse[(size_t)(row.at - token * a.hq) * a.total + token] =
-        l == 0.0f ? -INFINITY : (float)(((double)top + (double)__log2f(l)) * 0.6931471805599453);
+  const int group = a.hq / a.c.hkv, slices = kFew ? D / 32 : 1, rows = *ws.joins * a.c.hkv * cut.rows;
+  const int step = kFew ? gridDim.x : 4 * gridDim.x;
+  for (int item = kFew ? blockIdx.x : 4 * blockIdx.x + (threadIdx.x >> 6); item < rows * slices; item += step) {
+    const int at = item / slices, row_in_tile = at % cut.rows, head = at / cut.rows % a.c.hkv;
+    const Split sp = ws.split[at / cut.rows / a.c.hkv];
+    const int ch = (item % slices) * 32 + 4 * col;
+    Item it;
+    it.seq = chunk_seq(a, sp.b);
+    const Row row = row_of(a, it, group, head, sp.tile * cut.rows + row_in_tile);
+    if (row.limit == -2) continue;
+    Joined x = {-INFINITY, 0.0f, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+    for (int i = set; i < sp.runs; i += kAhead * kSets) {
+      float4 ml[kAhead];
+      f4v_t y[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const size_t from = ((size_t)(sp.slot + min(i + u * kSets, sp.runs - 1)) * a.c.hkv + head) * cut.rows + row_in_tile;
+        ml[u] = ws.ml[from];
+        y[u] = *reinterpret_cast<const f4v_t*>(ws.o + from * D + ch);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u * kSets < sp.runs) join_pair(x, Joined{ml[u].x, ml[u].y, ml[u].z, y[u]});
+    }
+    if constexpr (kFew) {
+      part[threadIdx.x] = x;
+      __syncthreads();
+      if (set == 0) {
+#pragma unroll 4
+        for (int i = 1; i < kSets; ++i) join_pair(x, part[i * kCols + col]);
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int d = kCols; d < 64; d <<= 1) {
+        Joined y;
+        y.m = __shfl_xor(x.m, d);
+        y.l = __shfl_xor(x.l, d);
+        y.sum = __shfl_xor(x.sum, d);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y.o[v] = __shfl_xor(x.o[v], d);
+        join_pair(x, y);
+      }
+    }
+    if (set) continue;
+    *reinterpret_cast<h4v_t*>(a.o + (size_t)row.at * D + ch) = __builtin_convertvector(x.o * (x.sum == 0.0f ? 0.0f : 1.0f / x.sum), h4v_t);
+    if (ch == 0) {
+      const int token = row.at / a.hq;
+      a.lse[(size_t)(row.at - token * a.hq) * a.total + token] =
+          x.l == 0.0f ? -INFINITY : (float)(((double)x.m + (double)__log2f(x.l)) * 0.6931471805599453);
+    }
   }
 }
 
-// ---------------------------------------------------------------------------
 // Waves of a workgroup that share a page.
-constexpr int wide_waves(int D, bool fp16) { return 4; }
+constexpr int wide_waves(int D, bool fp16) { return D == 128 ? 8 : 4; }
 
 static bool chunk_cut(const PagedCache& c, int hq, int total, int max_new, ChunkCut* cut) {
   const size_t group = hq / c.hkv;
@@ -830,6 +905,15 @@ static hipError_t launch_rows(const PagedChunk& a, const ChunkCut& cut, hipStrea
   return hipGetLastError();
 }
 
+template <int G>
+static void launch_join(const PagedChunk& a, const ChunkCut& cut, hipStream_t st) {
+  const size_t rows = (size_t)cut.joins * a.c.hkv * cut.rows;
+  if (rows <= 2048)
+    k_chunk_join<G, true><<<dim3((unsigned)(rows * (2 * G))), kChunkJoin, 0, st>>>(a, cut);
+  else
+    k_chunk_join<G, false><<<dim3((unsigned)std::min<size_t>(2048, rows / 4)), kChunkJoin, 0, st>>>(a, cut);
+}
+
 hipError_t launch_paged_chunk(const PagedChunk& a, hipStream_t st) {
   ChunkCut cut;
   if (!chunk_cut(a.c, a.hq, a.total, a.max_new, &cut)) return hipErrorInvalidValue;
@@ -839,7 +923,12 @@ hipError_t launch_paged_chunk(const PagedChunk& a, hipStream_t st) {
   else
     e = a.c.D == 64 ? launch_rows<1, false>(a, cut, st) : a.c.D == 128 ? launch_rows<2, false>(a, cut, st) : launch_rows<4, false>(a, cut, st);
   if (e != hipSuccess || !cut.joins) return e;
-  k_chunk_join<<<dim3((unsigned)((size_t)cut.joins * a.c.hkv * cut.rows)), kChunkJoin, 0, st>>>(a, cut);
+  if (a.c.D == 64)
+    launch_join<1>(a, cut, st);
+  else if (a.c.D == 128)
+    launch_join<2>(a, cut, st);
+  else
+    launch_join<4>(a, cut, st);
   return hipGetLastError();
 }
 

@@ -31,13 +31,15 @@ constexpr float kNoRef = -1e30f;        // before any key
 
 // ---------------------------------------------------------------------------
 // The plan: items (sequence, tile of rows, run of pages), the same for every kv head.
+// Sequences of few rows and of many are cut apart, each kind by its own kernel's sizes.
 constexpr int kMinRun = 4;              // pages that a run has at least, on average
 
-// How a launch cuts its work: rows a tile, items aimed at, and its bounds (per kv head).
+// How one kind's work is cut: rows a tile, items aimed at, and its bounds (per kv head).
 // A tile of P pages has at most 1 + P / per runs and, where it is split, fewer than
 // 2 P / per; sum P / per over the tiles is at most the target (in fp32: and one more).
 struct ChunkCut {
   int rows, target;
+  int above, upto;                      // sequences of more than `above` rows and at most `upto`
   int items, slots, joins;              // items, runs of split tiles, split tiles: at most
 };
 struct ChunkSeq {
@@ -64,25 +66,39 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const PagedChunk& a, int b) {
   return s;
 }
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
-__device__ __forceinline__ int tiles_of(const ChunkSeq& s, int group, const ChunkCut& cut) { return ceil_div(s.n * group, cut.rows); }
+__device__ __forceinline__ int tiles_of(const ChunkSeq& s, int group, const ChunkCut& cut) {
+  const int rows = s.n * group;
+  return rows > cut.above && rows <= cut.upto ? ceil_div(rows, cut.rows) : 0;
+}
 // Pages that the rows of a tile see.
 __device__ __forceinline__ int tile_pages(const ChunkSeq& s, int group, const ChunkCut& cut, int tile) {
   const int last = min(s.n - 1, ((tile + 1) * cut.rows - 1) / group);
   return max(0, s.base + last + kPage) / kPage;
 }
+// Sum over the wave, the same bits in every lane.
+template <int kCtrl, int kRowMask, bool kBound>
+__device__ __forceinline__ float add_dpp(float x) {
+  return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kCtrl, kRowMask, 0xF, kBound));
+}
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return x;
+  x = add_dpp<0x111, 0xF, true>(x);      // row_shr 1, 2, 4, 8
+  x = add_dpp<0x112, 0xF, true>(x);
+  x = add_dpp<0x114, 0xF, true>(x);
+  x = add_dpp<0x118, 0xF, true>(x);
+  x = add_dpp<0x142, 0xA, false>(x);     // lane 15 of each row to the next
+  x = add_dpp<0x143, 0xC, false>(x);
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
 }
 
 // The item numbered r (found by a whole wave); false: no such item.  `joins`: the
 // split tiles.  There are no items at all where the counts are no prefix sums of
 // `total` (more rows than the launch and the workspace were sized for).
 __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const ChunkCut& cut, int r, int lane, Item& it, int& joins) {
+  const ChunkSeq held = chunk_seq(a, lane);                 // the first 64 sequences are read once
+  const auto seq = [&](int b) { return b < 64 ? held : chunk_seq(a, b); };
   float work = 0.0f, tokens = 0.0f;
   for (int b = lane; b < a.c.batch; b += 64) {
-    const ChunkSeq s = chunk_seq(a, b);
+    const ChunkSeq s = seq(b);
     tokens += (float)s.n;
     work += (float)tiles_of(s, group, cut) * (float)ceil_div(s.len, kPage);
   }
@@ -92,7 +108,7 @@ __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const 
   const auto runs_of = [per](const ChunkSeq& s) { return max(1, ceil_div(ceil_div(s.len, kPage), per)); };
   int items = 0, tiles = 0, slots = 0;
   for (int b = lane; b < a.c.batch; b += 64) {
-    const ChunkSeq s = chunk_seq(a, b);
+    const ChunkSeq s = seq(b);
     const int t = tiles_of(s, group, cut), n = runs_of(s);
     items += t * n;
     if (n > 1) {
@@ -112,7 +128,13 @@ __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const 
   it.join = __builtin_amdgcn_readlane(upto_tiles - tiles, src);
   it.slot = __builtin_amdgcn_readlane(upto_slots - slots, src);
   for (int b = src; b < a.c.batch; b += 64) {
-    const ChunkSeq s = chunk_seq(a, b);
+    ChunkSeq s = held;
+    if (b >= 64) s = chunk_seq(a, b);
+    const int from = b < 64 ? src : 0;                      // (the same in every lane: kept in scalar registers)
+    s.first = __builtin_amdgcn_readlane(s.first, from);
+    s.n = __builtin_amdgcn_readlane(s.n, from);
+    s.len = __builtin_amdgcn_readlane(s.len, from);
+    s.base = __builtin_amdgcn_readlane(s.base, from);
     const int t = tiles_of(s, group, cut), n = runs_of(s);
     if (r < at + t * n) {
       // a sequence's first pages first, of those the tiles that see most
@@ -126,10 +148,6 @@ __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const 
       it.end = __builtin_amdgcn_readfirstlane((int)(pages * (it.run + 1) / n));
       it.join = n > 1 ? it.join + it.tile : -1;
       it.slot = n > 1 ? it.slot + it.tile * n : -1;
-      it.seq.first = __builtin_amdgcn_readfirstlane(s.first);      // (the same in every lane: kept in scalar registers)
-      it.seq.n = __builtin_amdgcn_readfirstlane(s.n);
-      it.seq.len = __builtin_amdgcn_readfirstlane(s.len);
-      it.seq.base = __builtin_amdgcn_readfirstlane(s.base);
       it.run = __builtin_amdgcn_readfirstlane(it.run);
       it.tile = __builtin_amdgcn_readfirstlane(it.tile);
       it.runs = __builtin_amdgcn_readfirstlane(n);
@@ -146,8 +164,8 @@ __device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const 
   return false;
 }
 
-// Workspace: o [slots][hkv][rows][D], then (m, l, l^, -) [slots][hkv][rows], then the
-// split tiles, then their number.
+// Workspace of a kind: o [slots][hkv][rows][D], then (m, l, l^, -) [slots][hkv][rows],
+// then the split tiles, then their number.  Sequences of many rows come first.
 struct Split {
   int b, tile, slot, runs;
 };
@@ -157,7 +175,10 @@ struct ChunkWs {
   Split* split;
   int* joins;
 };
-__host__ __device__ __forceinline__ ChunkWs chunk_ws(uint8_t* ws, const PagedCache& c, const ChunkCut& cut) {
+__host__ __device__ __forceinline__ size_t chunk_ws_bytes(const PagedCache& c, const ChunkCut& cut) {
+  return (size_t)cut.slots * c.hkv * cut.rows * (c.D + 4) * 4 + cut.joins * sizeof(Split) + 16;
+}
+__device__ __forceinline__ ChunkWs chunk_ws(uint8_t* ws, const PagedCache& c, const ChunkCut& cut) {
   const size_t rows = (size_t)cut.slots * c.hkv * cut.rows;
   ChunkWs w;
   w.o = reinterpret_cast<float*>(ws);
@@ -165,9 +186,6 @@ __host__ __device__ __forceinline__ ChunkWs chunk_ws(uint8_t* ws, const PagedCac
   w.split = reinterpret_cast<Split*>(w.ml + rows);
   w.joins = reinterpret_cast<int*>(w.split + cut.joins);
   return w;
-}
-static size_t chunk_ws_bytes(const PagedCache& c, const ChunkCut& cut) {
-  return (size_t)cut.slots * c.hkv * cut.rows * (c.D + 4) * 4 + cut.joins * sizeof(Split) + 16;
 }
 
 // ---------------------------------------------------------------------------
@@ -348,37 +366,37 @@ __device__ __forceinline__ h8v_t ones() { return h8v_t{1, 1, 1, 1, 1, 1, 1, 1}; 
 // also where they are infinite or NaN.  Of the keys that no row sees they are cleared;
 // of the others what is not finite is counted, per sign, over the keys that a row sees
 // (products of ones; NaN under both signs), added where it counts, and cleared.
-__device__ __forceinline__ bool any_not_finite(const h8v_t& v) {
-  typedef uint32_t u4v_t __attribute__((ext_vector_type(4)));
-  const u4v_t x = (__builtin_bit_cast(u4v_t, v) & 0x7C007C00u) + 0x04000400u;
-  return ((x[0] | x[1] | x[2] | x[3]) & 0x80008000u) != 0;
-}
-__device__ __forceinline__ h8v_t seen_keys(int seen, int first) {
-  h8v_t x;
+typedef uint32_t u4v_t __attribute__((ext_vector_type(4)));
+// Bit 15 of each half that is not finite.
+__device__ __forceinline__ u4v_t not_finite(u4v_t x) { return ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ bool any(u4v_t x) { return (x[0] | x[1] | x[2] | x[3]) != 0; }
+// All bits of the halves whose bit 15 is set, and 1.0 in them.
+__device__ __forceinline__ u4v_t whole(u4v_t x) { return (x - (x >> 15)) | x; }
+__device__ __forceinline__ u4v_t one(u4v_t x) { return (x >> 1) - (x >> 5); }
+// All bits of the first `n` halves (cut to 0 .. 8).
+__device__ __forceinline__ u4v_t first_halves(int n) {
+  u4v_t m;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = first + i <= seen ? (half_t)1 : (half_t)0;
-  return x;
+  for (int d = 0; d < 4; ++d) {
+    const int some = max(0, min(2, n - 2 * d));
+    m[d] = (uint32_t)(0xFFFFFFFFull << (16 * some) >> 32);
+  }
+  return m;
 }
 template <int G>
-__device__ __forceinline__ void add_not_finite(Rows16<G>& x, const h8v_t (&v)[2], int ct, int seen, int k) {
-  const half_t inf = (half_t)INFINITY;
+__device__ __forceinline__ void add_not_finite(Rows16<G>& x, const u4v_t (&v)[2], int ct, int seen, int k) {
   f4v_t up = {0.0f, 0.0f, 0.0f, 0.0f}, down = up;
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    h8v_t is_up, is_down;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      is_up[i] = v[c][i] < inf ? (half_t)0 : (half_t)1;
-      is_down[i] = v[c][i] > -inf ? (half_t)0 : (half_t)1;
-    }
-    const h8v_t who = seen_keys(seen, 16 * k + 8 * c);
-    up = product(is_up, who, up);
-    down = product(is_down, who, down);
+    const u4v_t odd = not_finite(v[c]), nan = ((v[c] & 0x03FF03FFu) + 0x7FFF7FFFu), minus = v[c];
+    const h8v_t who = __builtin_bit_cast(h8v_t, first_halves(seen + 1 - 16 * k - 8 * c) & 0x3C003C00u);
+    up = product(__builtin_bit_cast(h8v_t, one(odd & (nan | ~minus))), who, up);
+    down = product(__builtin_bit_cast(h8v_t, one(odd & (nan | minus))), who, down);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (up[i] > 0.0f) x.o[ct][i] += INFINITY;
-    if (down[i] > 0.0f) x.o[ct][i] -= INFINITY;
+    x.o[ct][i] += up[i] > 0.0f ? INFINITY : 0.0f;
+    x.o[ct][i] -= down[i] > 0.0f ? INFINITY : 0.0f;
   }
 }
 
@@ -408,23 +426,39 @@ __device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, c
 }
 
 // ---------------------------------------------------------------------------
-// Waves a SIMD whose registers the compiler may use, for tiles of 16 nb rows.
-constexpr int chunk_waves(int D, bool fp16, int nb) { return D == 256 || (fp16 && D == 128 && nb == 2) ? 1 : 2; }
-
-// One wave per (item, kv head): 16 NB rows; a page's operands come straight from its
-// record, one 16-byte load a lane for each KiB.
-template <int G, bool kFp16, int NB>
-__global__ void __launch_bounds__(64, chunk_waves(64 * G, kFp16, NB)) k_chunk_rows(PagedChunk a, ChunkCut cut) {
+// Few rows over HIF4 pages.
+// One wave per (item, kv head): 16 NB rows; the operands are made of a page's record
+// in registers, one 16-byte load a lane for each KiB.  K of the next page is fetched once
+// this one's has been used, V while the scores are made.
+template <int G, int NB>
+__device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, int item, int head, int lane) {
   constexpr int D = 64 * G, kRows = 16 * NB;
-  const int lane = threadIdx.x, n = lane & 15, k = lane >> 4;
-  const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
+  const int n = lane & 15, k = lane >> 4, group = a.hq / a.c.hkv;
   Item it;
   int joins;
-  const bool there = find_item(a, group, cut, blockIdx.x / a.c.hkv, lane, it, joins);
-  const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
-  if (blockIdx.x == 0 && lane == 0) *ws.joins = joins;
+  const bool there = find_item(a, group, cut, item, lane, it, joins);
+  const ChunkWs ws = chunk_ws(ws_at, a.c, cut);
+  if (item == 0 && head == 0 && lane == 0) *ws.joins = joins;
   if (!there) return;
   if (it.runs > 1 && it.run == 0 && head == 0 && lane == 0) ws.split[it.join] = Split{it.b, it.tile, it.slot, it.runs};
+
+  // the pages of the run that are some
+  Pages pg;
+  pg.base = it.begin - 64;
+  int page_at = 0;
+  const auto next = [&](int j) {
+    for (; j < it.end; ++j) {
+      if (j - pg.base >= 64) load_pages(pg, a.c, it.b, j, it.end - 1, lane);
+      page_at = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
+      if ((unsigned)page_at < (unsigned)a.c.num_pages) break;
+    }
+    return __builtin_amdgcn_readfirstlane(j);
+  };
+  const auto record = [&] {
+    const size_t at = (size_t)__builtin_amdgcn_readfirstlane(page_at) * a.c.hkv + head;
+    return a.c.pool + at * paged_record_bytes(D, false);
+  };
+  int j = next(it.begin);
 
   Row row[NB];
   Rows16<G> x[NB];
@@ -432,97 +466,51 @@ __global__ void __launch_bounds__(64, chunk_waves(64 * G, kFp16, NB)) k_chunk_ro
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
     row[i] = row_of(a, it, group, head, it.tile * kRows + 16 * i + n);
-    load_query<G, kFp16>(q[i], a, row[i], head, k);
+    load_query<G, false>(q[i], a, row[i], head, k);
     start(x[i]);
   }
-  // keys that every row of the tile sees, and that any of them sees: up to these
-  const int first_token = it.tile * kRows / group, last_token = min(it.seq.n - 1, (it.tile * kRows + kRows - 1) / group);
-  const int all_see = it.seq.base + first_token, some_see = it.seq.base + last_token;
+  const int first_token = it.tile * kRows / group;          // every row of the tile sees the keys up to its
+  const int all_see = it.seq.base + first_token;
 
-  Pages pg;
-  load_pages(pg, a.c, it.b, it.begin, it.end - 1, lane);
-  for (int j = it.begin; j < it.end; ++j) {
-    if (j - pg.base >= 64) load_pages(pg, a.c, it.b, j, it.end - 1, lane);
-    const int page = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
-    if ((unsigned)page >= (unsigned)a.c.num_pages) continue;
-    const uint8_t* rec = a.c.pool + ((size_t)page * a.c.hkv + head) * paged_record_bytes(D, kFp16);
-    const bool masked = j * kPage + kPage - 1 > all_see;
+  const uint8_t* rec = record();
+  HifPart<G> k4, v4;
+  if (j < it.end) load_hif4<G>(k4, rec, lane);
+  while (j < it.end) {
+    const int now = j;
+    const bool masked = now * kPage + kPage - 1 > all_see;
+    keep_order();
+    load_hif4<G>(v4, rec + 2304 * G, lane);
+    keep_order();
     f4v_t s[NB][4];
+    h8v_t p[NB][2];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int t = 0; t < 4; ++t) s[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-    h8v_t p[NB][2];
-    if constexpr (kFp16) {
-      h8v_t kr[8 * G], vr[8 * G];       // K [t][D/32], V [D/16][c]
-      load_operands<8 * G, 1024>(kr, rec, lane);
 #pragma unroll
-      for (int c = 0; c < 2 * G; ++c)
+    for (int c = 0; c < 2 * G; ++c)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) {
+        const h8v_t kr = part_operand<G>(k4, c >> 1, t, c & 1, lane);
 #pragma unroll
-          for (int i = 0; i < NB; ++i) s[i][t] = product(kr[2 * G * t + c], q[i][c], s[i][t]);
-      keep_order();
-      load_operands<8 * G, 1024>(vr, rec + 128 * D, lane);
-      keep_order();
-#pragma unroll
-      for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], s[i], p[i], a.scale, masked, row[i].limit - j * kPage, k);
-      if (masked) {
-        bool odd_values = false;
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (j * kPage + 16 * k + 8 * c + i > some_see)
-#pragma unroll
-              for (int u = 0; u < 4 * G; ++u) vr[2 * u + c][i] = (half_t)0;
-#pragma unroll
-        for (int u = 0; u < 8 * G; ++u) odd_values |= any_not_finite(vr[u]);
-        if (__builtin_amdgcn_ballot_w64(odd_values)) {
-#pragma unroll
-          for (int u = 0; u < 4 * G; ++u) {
-            const h8v_t v[2] = {vr[2 * u], vr[2 * u + 1]};
-#pragma unroll
-            for (int i = 0; i < NB; ++i) add_not_finite<G>(x[i], v, u, row[i].limit - j * kPage, k);
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (!(v[c][i] < (half_t)INFINITY && v[c][i] > -(half_t)INFINITY)) vr[2 * u + c][i] = (half_t)0;
-          }
-        }
+        for (int i = 0; i < NB; ++i) s[i][t] = product(kr, q[i][c], s[i][t]);
       }
+    keep_order();
+    j = next(j + 1);
+    rec = record();
+    if (j < it.end) load_hif4<G>(k4, rec, lane);
+    keep_order();
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+    for (int i = 0; i < NB; ++i) soften<G, false>(x[i], s[i], p[i], a.scale, masked, row[i].limit - now * kPage, k);
+    keep_order();
 #pragma unroll
-        for (int u = 0; u < 4 * G; ++u)
+    for (int u = 0; u < 4 * G; ++u)
 #pragma unroll
-          for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr[2 * u + c], p[i][c], x[i].o[u]);
-    } else {
-      HifPart<G> kp, vp;
-      load_hif4<G>(kp, rec, lane);
+      for (int c = 0; c < 2; ++c) {
+        const h8v_t vr = part_operand<G>(v4, u >> 2, u & 3, c, lane);
 #pragma unroll
-      for (int c = 0; c < 2 * G; ++c)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const h8v_t kr = part_operand<G>(kp, c >> 1, t, c & 1, lane);
-#pragma unroll
-          for (int i = 0; i < NB; ++i) s[i][t] = product(kr, q[i][c], s[i][t]);
-        }
-      keep_order();
-      load_hif4<G>(vp, rec + 2304 * G, lane);
-      keep_order();
-#pragma unroll
-      for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], s[i], p[i], a.scale, masked, row[i].limit - j * kPage, k);
-#pragma unroll
-      for (int u = 0; u < 4 * G; ++u)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const h8v_t vr = part_operand<G>(vp, u >> 2, u & 3, c, lane);
-#pragma unroll
-          for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr, p[i][c], x[i].o[u]);
-        }
-    }
+        for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr, p[i][c], x[i].o[u]);
+      }
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -532,13 +520,18 @@ __global__ void __launch_bounds__(64, chunk_waves(64 * G, kFp16, NB)) k_chunk_ro
   for (int i = 0; i < NB; ++i) finish<G>(a, ws, it, x[i], row[i], head, kRows, 16 * i + n, k);
 }
 
+template <int G, int NB>
+__global__ void __launch_bounds__(64, G == 4 ? 1 : 2) k_chunk_rows(PagedChunk a, ChunkCut cut, int few_ws) {
+  chunk_rows<G, NB>(a, cut, a.ws + few_ws, blockIdx.x / a.c.hkv, blockIdx.x % a.c.hkv, threadIdx.x);
+}
+
 // ---------------------------------------------------------------------------
-// Many rows: kWaves waves of 32 rows each share a page, whose operands they make in
+// Many rows: kWaves waves of 16 NB rows each share a page, whose operands they make in
 // LDS (two pages' room: the next one is made while this one is used).  A record's KiB
 // unit of fp16 operands is what a wave reads for one operand of a product, 16 bytes a
-// lane in lane order, so neither reads nor writes have bank conflicts.
+// lane in lane order, so neither reads nor writes have bank conflicts.  Over FP16 pages
+// a few rows are a workgroup of one wave.
 // Units of a page: K [t][c], then V [channels / 16][c].
-constexpr int kWideRows = 32;           // of a wave
 constexpr int kMatrix = 0x008, kDsRead = 0x100;      // kinds of instructions to the scheduler
 
 // A quarter of a tile's part of a HIF4 record: the words (t, c) of two t.
@@ -582,47 +575,64 @@ __device__ __forceinline__ void store_quad(h8v_t* page, const HifQuad& q, int at
   }
 }
 
-// What a wave fetches of a page, and puts into LDS.
-template <int G, bool kFp16, int kWaves>
-struct WideShare {
-  static constexpr int kAll = kFp16 ? 16 * G : 4 * G, kMine = (kAll + kWaves - 1) / kWaves;
-  h8v_t unit[kFp16 ? kMine : 1];
-  HifQuad quad[kFp16 ? 1 : kMine];
+// What a wave fetches of a HIF4 page, and puts into LDS as operands.
+template <int G, int kWaves>
+struct HifShare {
+  static constexpr int kAll = 4 * G, kMine = (kAll + kWaves - 1) / kWaves;
+  HifQuad quad[kMine];
   __device__ __forceinline__ void load(const uint8_t* rec, int wave, int lane) {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int at = wave + kWaves * i;
-      if (kAll % kWaves && at >= kAll) break;
-      if constexpr (kFp16)
-        unit[i] = load_at<h8v_t>((global_ptr)(rec + 1024 * at), 16 * lane);
-      else
-        load_quad<G>(quad[i], rec, at, lane);
-    }
+    for (int i = 0; i < kMine; ++i) load_quad<G>(quad[i], rec, wave + kWaves * i, lane);
   }
   __device__ __forceinline__ void store(h8v_t* page, int wave, int lane) const {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int at = wave + kWaves * i;
-      if (kAll % kWaves && at >= kAll) break;
-      if constexpr (kFp16)
-        page[64 * at + lane] = unit[i];
-      else
-        store_quad<G>(page, quad[i], at, lane);
+    for (int i = 0; i < kMine; ++i) store_quad<G>(page, quad[i], wave + kWaves * i, lane);
+  }
+};
+// A wave's share of an FP16 page, which is operands as it stands: copied to LDS past
+// the registers.  M0 and the copy that takes its LDS address from it are one statement:
+// the compiler keeps no value of its own in M0.
+template <int kBytes, int kStep>
+struct CopyPieces {
+  static __device__ __forceinline__ void run(uint64_t from, uint32_t to, uint32_t lane_bytes) {
+    if constexpr (kBytes > 0) {
+      CopyPieces<kBytes - kStep, kStep>::run(from, to, lane_bytes);
+      asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1"
+                   :
+                   : "v"(lane_bytes + (kBytes - kStep)), "s"(from), "s"(to), "n"(kBytes - kStep)
+                   : "memory", "m0", "scc");
     }
   }
 };
+__device__ __forceinline__ uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+template <int G, int kWaves>
+__device__ __forceinline__ void copy_share(h8v_t* page, const uint8_t* rec, int wave, int lane) {
+  const uint64_t from = (uint64_t)(uintptr_t)(rec + 16384 * G / kWaves * wave);
+  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(page + 1024 * G / kWaves * wave);
+  CopyPieces<16384 * G / kWaves, 1024>::run((uint64_t)scalar((uint32_t)from) | (uint64_t)scalar((uint32_t)(from >> 32)) << 32, scalar(to),
+                                            16 * lane);
+}
+__device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0)
 
-template <int G, bool kFp16, int kWaves>
-__global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut) {
-  constexpr int D = 64 * G, kRows = kWideRows * kWaves, NB = 2, kUnits = 16 * G;
+template <int G, bool kFp16, int kWaves, int NB>
+__global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut, ChunkCut few, int few_ws) {
+  constexpr int D = 64 * G, kMine = 16 * NB, kRows = kMine * kWaves, kUnits = 16 * G;
+  static_assert(16 * G % kWaves == 0 && 4 * G % kWaves == 0, "equal shares");
   extern __shared__ __align__(16) uint8_t smem[];
   h8v_t* const pages = reinterpret_cast<h8v_t*>(smem);
   const int lane = threadIdx.x & 63, n = lane & 15, k = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv;
+  const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv, number = blockIdx.x / a.c.hkv;
+  if constexpr (!kFp16) {
+    if (number >= cut.items) {            // behind the sequences of many rows those of few, an item a wave
+      const int item = (number - cut.items) * kWaves + wave;
+      if (item < few.items) chunk_rows<G, 1>(a, few, a.ws + few_ws, item, head, lane);
+      return;
+    }
+  }
   Item it;
   int joins;
-  const bool there = find_item(a, group, cut, blockIdx.x / a.c.hkv, lane, it, joins);
+  const bool there = find_item(a, group, cut, number, lane, it, joins);
   const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
   if (blockIdx.x == 0 && threadIdx.x == 0) *ws.joins = joins;
   if (!there) return;
@@ -644,11 +654,16 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
     const size_t at = (size_t)__builtin_amdgcn_readfirstlane(page_at) * a.c.hkv + head;
     return a.c.pool + at * paged_record_bytes(D, kFp16);
   };
-  WideShare<G, kFp16, kWaves> share;
+  HifShare<G, kWaves> share;
   int j = next(it.begin);
-  if (j < it.end) share.load(record(), wave, lane);
+  if (j < it.end) {
+    if constexpr (kFp16)
+      copy_share<G, kWaves>(pages, record(), wave, lane);
+    else
+      share.load(record(), wave, lane);
+  }
 
-  const int row0 = it.tile * kRows + wave * kWideRows;      // the wave's first row
+  const int row0 = it.tile * kRows + wave * kMine;      // the wave's first row
   Row row[NB];
   Rows16<G> x[NB];
   h8v_t q[NB][2 * G];
@@ -659,26 +674,32 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
     start(x[i]);
   }
   // keys that every row of the wave sees, and that any of them sees: up to these
-  const int first_token = row0 / group, last_token = min(it.seq.n - 1, (row0 + kWideRows - 1) / group);
+  const int first_token = row0 / group, last_token = min(it.seq.n - 1, (row0 + kMine - 1) / group);
   const int all_see = it.seq.base + first_token, some_see = first_token < it.seq.n ? it.seq.base + last_token : -1;
 
-  const bool late = false;
   int ahead = next(j + 1), at = 0;
-  if (j < it.end) share.store(pages, wave, lane);
-  if (ahead < it.end) share.load(record(), wave, lane);
+  if constexpr (kFp16) {
+    wait_copies();
+  } else {
+    if (j < it.end) share.store(pages, wave, lane);
+    if (ahead < it.end) share.load(record(), wave, lane);
+  }
   __syncthreads();
   while (j < it.end) {
     const h8v_t* page = pages + 64 * kUnits * at + lane;
     const int now = j;
     j = ahead;
-    const auto make_next = [&] {
-      if (j < it.end) {
-        share.store(pages + 64 * kUnits * (at ^ 1), wave, lane);
+    if (j < it.end) {
+      h8v_t* const other = pages + 64 * kUnits * (at ^ 1);
+      if constexpr (kFp16) {
+        copy_share<G, kWaves>(other, record(), wave, lane);
+        ahead = next(j + 1);
+      } else {
+        share.store(other, wave, lane);
         ahead = next(j + 1);
         if (ahead < it.end) share.load(record(), wave, lane);
       }
-    };
-    if (!late) make_next();
+    }
     if (now * kPage <= some_see) {
       const bool masked = now * kPage + kPage - 1 > all_see;
       f4v_t s[NB][4];
@@ -725,25 +746,21 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
       if (odd_values) {
 #pragma unroll
         for (int u = 0; u < 4 * G; ++u) {
-          h8v_t v[2] = {page[64 * (8 * G + 2 * u)], page[64 * (8 * G + 2 * u + 1)]};
+          keep_order();
+          u4v_t v[2];
 #pragma unroll
           for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (now * kPage + 16 * k + 8 * c + e > some_see) v[c][e] = (half_t)0;
-          if (__builtin_amdgcn_ballot_w64(any_not_finite(v[0]) || any_not_finite(v[1]))) {
+            v[c] = __builtin_bit_cast(u4v_t, page[64 * (8 * G + 2 * u + c)]) & first_halves(some_see - now * kPage + 1 - 16 * k - 8 * c);
+          if (__builtin_amdgcn_ballot_w64(any(not_finite(v[0]) | not_finite(v[1])))) {
 #pragma unroll
             for (int i = 0; i < NB; ++i) add_not_finite<G>(x[i], v, u, row[i].limit - now * kPage, k);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (!(v[c][e] < (half_t)INFINITY && v[c][e] > -(half_t)INFINITY)) v[c][e] = (half_t)0;
+            for (int c = 0; c < 2; ++c) v[c] &= ~whole(not_finite(v[c]));
           }
 #pragma unroll
           for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int i = 0; i < NB; ++i) x[i].o[u] = product(v[c], p[i][c], x[i].o[u]);
+            for (int i = 0; i < NB; ++i) x[i].o[u] = product(__builtin_bit_cast(h8v_t, v[c]), p[i][c], x[i].o[u]);
         }
       } else {
 #pragma unroll
@@ -765,12 +782,12 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
       }
       __builtin_amdgcn_s_setprio(0);
     }
-    if (late) make_next();
     at ^= 1;
+    if constexpr (kFp16) wait_copies();
     __syncthreads();
   }
 #pragma unroll
-  for (int i = 0; i < NB; ++i) finish<G>(a, ws, it, x[i], row[i], head, kRows, wave * kWideRows + 16 * i + n, k);
+  for (int i = 0; i < NB; ++i) finish<G>(a, ws, it, x[i], row[i], head, kRows, wave * kMine + 16 * i + n, k);
 }
 
 // ---------------------------------------------------------------------------
@@ -795,11 +812,10 @@ __device__ __forceinline__ void join_pair(Joined& x, const Joined& y) {
 }
 
 template <int G, bool kFew>
-__global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCut cut) {
+__device__ __forceinline__ void join_tiles(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, Joined* part) {
   constexpr int D = 64 * G, kCols = kFew ? 8 : D / 4, kSets = (kFew ? kChunkJoin : 64) / kCols, kAhead = 4;
-  __shared__ Joined part[kFew ? kChunkJoin : 1];
   const int lane = threadIdx.x & 63, at_set = kFew ? threadIdx.x : lane, col = at_set % kCols, set = at_set / kCols;
-  const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
+  const ChunkWs ws = chunk_ws(ws_at, a.c, cut);
   const int group = a.hq / a.c.hkv, slices = kFew ? D / 32 : 1, rows = *ws.joins * a.c.hkv * cut.rows;
   const int step = kFew ? gridDim.x : 4 * gridDim.x;
   for (int item = kFew ? blockIdx.x : 4 * blockIdx.x + (threadIdx.x >> 6); item < rows * slices; item += step) {
@@ -853,20 +869,24 @@ __global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCu
     }
   }
 }
+template <int G, bool kFew>
+__global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCut cut, ChunkCut few, int few_ws) {
+  __shared__ Joined part[kFew ? kChunkJoin : 1];
+  if (cut.joins) join_tiles<G, kFew>(a, cut, a.ws, part);
+  if (few.joins) join_tiles<G, kFew>(a, few, a.ws + few_ws, part);
+}
+
+// ---------------------------------------------------------------------------
+// Rows (of one sequence and kv head) up to which a wave of its own takes them.
+constexpr int kFewRows = 32;
 
 // Waves of a workgroup that share a page.
-constexpr int wide_waves(int D, bool fp16) { return D == 128 ? 8 : 4; }
+constexpr int wide_waves(int D) { return D == 128 ? 8 : 4; }
 
-static bool chunk_cut(const PagedCache& c, int hq, int total, int max_new, ChunkCut* cut) {
-  const size_t group = hq / c.hkv;
-  const size_t most = max_new * group;
-  cut->rows = most <= 16 ? 16 : most <= 32 ? (c.D == 256 ? 16 : 32) : kWideRows * wide_waves(c.D, c.fp16);
-  if (cut->rows <= 32)
-    cut->target = std::max(1, 1024 * chunk_waves(c.D, c.fp16, cut->rows / 16) / c.hkv);
-  else
-    cut->target = std::max(1, 1024 * (c.D == 256 ? 1 : 2) / wide_waves(c.D, c.fp16) / c.hkv);
-  const size_t tiles = std::min((size_t)c.batch * ((max_new * group + cut->rows - 1) / cut->rows),
-                                (size_t)total * group / cut->rows + c.batch);
+// Sizes of one kind: sequences of more than `above` rows, of which there are at most
+// `most`, with `all` rows in total.
+static bool cut_kind(const PagedCache& c, size_t all, size_t most, size_t batch, ChunkCut* cut) {
+  const size_t tiles = std::min(batch * ((most + cut->rows - 1) / cut->rows), all / cut->rows + batch);
   const size_t runs = std::max<size_t>(1, ((size_t)c.max_pages + kMinRun - 1) / kMinRun);
   const size_t items = std::min(tiles * runs, tiles + cut->target + 1);
   const size_t joins = runs == 1 ? 0 : std::min(tiles, (size_t)cut->target + 1);
@@ -876,60 +896,87 @@ static bool chunk_cut(const PagedCache& c, int hq, int total, int max_new, Chunk
   cut->slots = runs == 1 ? 0 : (int)std::min(tiles * runs, (size_t)2 * cut->target + 2);
   return true;
 }
+struct ChunkCuts {
+  int waves;                            // of a workgroup that takes many rows; 1: there are but few
+  ChunkCut many, few;
+  int few_ws;                           // offset in the workspace
+  size_t blocks, joined, bytes;         // workgroups, rows that may be joined
+};
+static bool chunk_cuts(const PagedCache& c, int hq, int total, int max_new, ChunkCuts* x) {
+  const size_t group = hq / c.hkv, most = max_new * group, all = (size_t)total * group;
+  if (most >= (size_t)1 << 30) return false;
+  const bool wide = most > kFewRows;
+  x->waves = wide ? wide_waves(c.D) : 1;
+  x->many = ChunkCut{wide ? 32 * x->waves : 0, 0, c.fp16 ? 0 : kFewRows, 1 << 30, 0, 0, 0};
+  x->few = ChunkCut{16, 0, 0, kFewRows, 0, 0, 0};
+  const int waves = 1024 * (c.D == 256 ? 1 : 2);            // that the chip holds
+  if (c.fp16) {
+    if (!wide) x->many.rows = most <= 16 ? 16 : 32;
+    x->many.target = std::max(1, waves / x->waves / c.hkv);
+    if (!cut_kind(c, all, most, c.batch, &x->many)) return false;
+  } else {
+    if (!wide && most > 16 && c.D != 256) x->few.rows = 32;
+    x->few.target = std::max(1, waves / (wide ? 2 : 1) / c.hkv);
+    if (!cut_kind(c, all, std::min(most, (size_t)kFewRows), c.batch, &x->few)) return false;
+    x->many.target = std::max(1, waves / x->waves / c.hkv);
+    if (wide && !cut_kind(c, all, most, std::min((size_t)c.batch, all / (kFewRows + 1)), &x->many)) return false;
+  }
+  const size_t many = (chunk_ws_bytes(c, x->many) + 255) / 256 * 256;
+  x->few_ws = (int)many;
+  x->bytes = many + chunk_ws_bytes(c, x->few);
+  x->blocks = (x->many.items + ((size_t)x->few.items + x->waves - 1) / x->waves) * c.hkv;
+  x->joined = ((size_t)x->many.joins * x->many.rows + (size_t)x->few.joins * x->few.rows) * c.hkv;
+  return many < (size_t)1 << 31 && x->blocks < max_grid(64 * x->waves);
+}
 
 bool paged_chunk_fits(const PagedCache& c, int hq, int total, int max_new) {
-  ChunkCut cut;
-  return chunk_cut(c, hq, total, max_new, &cut);
+  ChunkCuts x;
+  return chunk_cuts(c, hq, total, max_new, &x);
 }
 size_t paged_chunk_workspace(const PagedCache& c, int hq, int total, int max_new) {
-  ChunkCut cut;
-  return chunk_cut(c, hq, total, max_new, &cut) ? chunk_ws_bytes(c, cut) : 0;
+  ChunkCuts x;
+  return chunk_cuts(c, hq, total, max_new, &x) ? x.bytes : 0;
 }
 
-template <int G, bool kFp16>
-static hipError_t launch_rows(const PagedChunk& a, const ChunkCut& cut, hipStream_t st) {
-  const dim3 grid((unsigned)((size_t)cut.items * a.c.hkv));
-  if (cut.rows > 32) {
-    constexpr int kWaves = wide_waves(64 * G, kFp16);
-    constexpr size_t kLds = (size_t)2 * 16 * G * 1024;
-    if (kLds > 65536) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_chunk_wide<G, kFp16, kWaves>),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
-      if (e != hipSuccess) return e;
-    }
-    k_chunk_wide<G, kFp16, kWaves><<<grid, 64 * kWaves, kLds, st>>>(a, cut);
-  } else if (G == 4 || cut.rows == 16)
-    k_chunk_rows<G, kFp16, 1><<<grid, 64, 0, st>>>(a, cut);
-  else
-    k_chunk_rows<G == 4 ? 1 : G, kFp16, 2><<<grid, 64, 0, st>>>(a, cut);
+template <int G, bool kFp16, int kWaves, int NB>
+static hipError_t launch_wide(const PagedChunk& a, const ChunkCuts& x, hipStream_t st) {
+  constexpr size_t kLds = (size_t)2 * 16 * G * 1024;
+  const auto kernel = k_chunk_wide<G, kFp16, kWaves, NB>;
+  if (kLds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((unsigned)x.blocks), 64 * kWaves, kLds, st>>>(a, x.many, x.few, x.few_ws);
   return hipGetLastError();
 }
-
 template <int G>
-static void launch_join(const PagedChunk& a, const ChunkCut& cut, hipStream_t st) {
-  const size_t rows = (size_t)cut.joins * a.c.hkv * cut.rows;
-  if (rows <= 2048)
-    k_chunk_join<G, true><<<dim3((unsigned)(rows * (2 * G))), kChunkJoin, 0, st>>>(a, cut);
+static hipError_t launch_chunk(const PagedChunk& a, const ChunkCuts& x, hipStream_t st) {
+  hipError_t e;
+  if (a.c.fp16) {
+    e = x.waves > 1            ? launch_wide<G, true, wide_waves(64 * G), 2>(a, x, st)
+        : x.many.rows == 16 ? launch_wide<G, true, 1, 1>(a, x, st)
+                            : launch_wide<G, true, 1, 2>(a, x, st);
+  } else if (x.waves > 1) {
+    e = launch_wide<G, false, wide_waves(64 * G), 2>(a, x, st);
+  } else {
+    if (G == 4 || x.few.rows == 16)
+      k_chunk_rows<G, 1><<<dim3((unsigned)x.blocks), 64, 0, st>>>(a, x.few, x.few_ws);
+    else
+      k_chunk_rows<G == 4 ? 1 : G, 2><<<dim3((unsigned)x.blocks), 64, 0, st>>>(a, x.few, x.few_ws);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || x.joined == 0) return e;
+  if (x.joined <= 2048)
+    k_chunk_join<G, true><<<dim3((unsigned)(x.joined * (2 * G))), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   else
-    k_chunk_join<G, false><<<dim3((unsigned)std::min<size_t>(2048, rows / 4)), kChunkJoin, 0, st>>>(a, cut);
+    k_chunk_join<G, false><<<dim3((unsigned)std::min<size_t>(2048, x.joined / 4)), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_chunk(const PagedChunk& a, hipStream_t st) {
-  ChunkCut cut;
-  if (!chunk_cut(a.c, a.hq, a.total, a.max_new, &cut)) return hipErrorInvalidValue;
-  hipError_t e;
-  if (a.c.fp16)
-    e = a.c.D == 64 ? launch_rows<1, true>(a, cut, st) : a.c.D == 128 ? launch_rows<2, true>(a, cut, st) : launch_rows<4, true>(a, cut, st);
-  else
-    e = a.c.D == 64 ? launch_rows<1, false>(a, cut, st) : a.c.D == 128 ? launch_rows<2, false>(a, cut, st) : launch_rows<4, false>(a, cut, st);
-  if (e != hipSuccess || !cut.joins) return e;
-  if (a.c.D == 64)
-    launch_join<1>(a, cut, st);
-  else if (a.c.D == 128)
-    launch_join<2>(a, cut, st);
-  else
-    launch_join<4>(a, cut, st);
-  return hipGetLastError();
+  ChunkCuts x;
+  if (!chunk_cuts(a.c, a.hq, a.total, a.max_new, &x)) return hipErrorInvalidValue;
+  return a.c.D == 64 ? launch_chunk<1>(a, x, st) : a.c.D == 128 ? launch_chunk<2>(a, x, st) : launch_chunk<4>(a, x, st);
 }
 
 }  // namespace hifa4

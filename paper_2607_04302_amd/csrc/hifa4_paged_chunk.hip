@@ -12,10 +12,11 @@
 // so far (2^7 to 2^15), and o is divided by the sum of the rounded p: a row that
 // rests on one key has exactly that key's value.  LSE takes the sum of p itself.
 //
-// The rows of a sequence, (token, query head of the kv head), are cut into tiles,
-// and a tile's pages into runs where there are too few tiles to fill the chip; a
-// second kernel joins the runs of a row.  Lengths and counts are read on the
-// device, so a captured call follows them.
+// The rows of a sequence, (token, query head of the kv head), are cut into tiles.
+// All tiles' pages, one after another, are cut into equal shares, one for each
+// workgroup that the chip holds: a share ends where it ends, inside a tile too, and
+// a second kernel joins the parts of the tiles that were cut.  Lengths and counts
+// are read on the device, so a captured call follows them.
 #include "hifa4_paged_device.h"
 
 #include <algorithm>
@@ -30,27 +31,18 @@ constexpr float kTop = 7.0f, kSlack = 8.0f;
 constexpr float kNoRef = -1e30f;        // before any key
 
 // ---------------------------------------------------------------------------
-// The plan: items (sequence, tile of rows, run of pages), the same for every kv head.
-// Sequences of few rows and of many are cut apart, each kind by its own kernel's sizes.
-constexpr int kMinRun = 4;              // pages that a run has at least, on average
-
-// How one kind's work is cut: rows a tile, items aimed at, and its bounds (per kv head).
-// A tile of P pages has at most 1 + P / per runs and, where it is split, fewer than
-// 2 P / per; sum P / per over the tiles is at most the target (in fp32: and one more).
+// The plan, the same for every kv head.  Sequences of few rows and of many are two
+// kinds of work, each with its own tiles and shares.
 struct ChunkCut {
-  int rows, target;
+  int rows;                             // of a tile
   int above, upto;                      // sequences of more than `above` rows and at most `upto`
-  int items, slots, joins;              // items, runs of split tiles, split tiles: at most
+  int shares;                           // at most
+  int tile_cost, least, whole;          // in pages: what a tile costs beside its own; the least share; a tile's
+                                        // part of fewer than `whole` is left with the rest of it
 };
 struct ChunkSeq {
   int first, n;                         // row of q, new tokens (those that the launch holds)
   int len, base;                        // cached tokens, position of the first new one
-};
-struct Item {
-  int b, tile, run, runs;
-  int begin, end;                       // pages
-  int slot, join;                       // of the tile's first run, and its place among the split tiles; -1: not split
-  ChunkSeq seq;
 };
 
 // Counts outside the contract are cut, so that no access leaves q, o and lse.
@@ -65,127 +57,188 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const PagedChunk& a, int b) {
   }
   return s;
 }
-__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// The same in scalar registers.
+__device__ __forceinline__ ChunkSeq seq_of(const PagedChunk& a, int b) {
+  const ChunkSeq s = chunk_seq(a, scalar(b));
+  return ChunkSeq{scalar(s.first), scalar(s.n), scalar(s.len), scalar(s.base)};
+}
 __device__ __forceinline__ int tiles_of(const ChunkSeq& s, int group, const ChunkCut& cut) {
   const int rows = s.n * group;
-  return rows > cut.above && rows <= cut.upto ? ceil_div(rows, cut.rows) : 0;
+  return rows > cut.above && rows <= cut.upto ? (rows + cut.rows - 1) / cut.rows : 0;
 }
 // Pages that the rows of a tile see.
 __device__ __forceinline__ int tile_pages(const ChunkSeq& s, int group, const ChunkCut& cut, int tile) {
   const int last = min(s.n - 1, ((tile + 1) * cut.rows - 1) / group);
   return max(0, s.base + last + kPage) / kPage;
 }
-// Sum over the wave, the same bits in every lane.
-template <int kCtrl, int kRowMask, bool kBound>
-__device__ __forceinline__ float add_dpp(float x) {
-  return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kCtrl, kRowMask, 0xF, kBound));
-}
-__device__ __forceinline__ float wave_sum(float x) {
-  x = add_dpp<0x111, 0xF, true>(x);      // row_shr 1, 2, 4, 8
-  x = add_dpp<0x112, 0xF, true>(x);
-  x = add_dpp<0x114, 0xF, true>(x);
-  x = add_dpp<0x118, 0xF, true>(x);
-  x = add_dpp<0x142, 0xA, false>(x);     // lane 15 of each row to the next
-  x = add_dpp<0x143, 0xC, false>(x);
-  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+// Cost of a sequence's first `tiles` tiles, counted in 1/group of a key: tile t's is
+// tile_cost pages and the keys that it sees, about base + (t + 1) rows / group.
+__device__ __forceinline__ long tiles_cost(const ChunkSeq& s, int group, const ChunkCut& cut, long tiles) {
+  return tiles * group * (kPage * cut.tile_cost + max(0, s.base)) + cut.rows * (tiles * (tiles + 1) / 2);
 }
 
-// The item numbered r (found by a whole wave); false: no such item.  `joins`: the
-// split tiles.  There are no items at all where the counts are no prefix sums of
-// `total` (more rows than the launch and the workspace were sized for).
-__device__ __forceinline__ bool find_item(const PagedChunk& a, int group, const ChunkCut& cut, int r, int lane, Item& it, int& joins) {
-  const ChunkSeq held = chunk_seq(a, lane);                 // the first 64 sequences are read once
-  const auto seq = [&](int b) { return b < 64 ? held : chunk_seq(a, b); };
-  float work = 0.0f, tokens = 0.0f;
-  for (int b = lane; b < a.c.batch; b += 64) {
-    const ChunkSeq s = seq(b);
-    tokens += (float)s.n;
-    work += (float)tiles_of(s, group, cut) * (float)ceil_div(s.len, kPage);
+// Sequences are in the order of the lanes that count them: b, b + 64, ..., then b + 1.
+struct ChunkPlan {
+  long before, upto, all;               // cost of the lanes before this one, up to it, of all
+};
+__device__ __forceinline__ int next_sequence(const PagedChunk& a, int b) {
+  if (b + 64 < a.c.batch) return b + 64;
+  b = (b & 63) + 1;
+  return b < 64 && b < a.c.batch ? b : -1;
+}
+__device__ __forceinline__ long wave_last(long x) {
+  return (long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, 63) |
+                (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32);
+}
+__device__ __forceinline__ void count_costs(ChunkPlan& p, const PagedChunk& a, const ChunkSeq& first, int group, const ChunkCut& cut, int lane) {
+  long mine = tiles_cost(first, group, cut, tiles_of(first, group, cut));
+  for (int b = lane + 64; b < a.c.batch; b += 64) {
+    const ChunkSeq s = chunk_seq(a, b);
+    mine += tiles_cost(s, group, cut, tiles_of(s, group, cut));
   }
-  joins = 0;
-  if (wave_sum(tokens) > (float)a.total * 1.001f) return false;
-  const int per = max(kMinRun, (int)ceilf(fminf(wave_sum(work) / (float)cut.target, 0x1p25f)));
-  const auto runs_of = [per](const ChunkSeq& s) { return max(1, ceil_div(ceil_div(s.len, kPage), per)); };
-  int items = 0, tiles = 0, slots = 0;
-  for (int b = lane; b < a.c.batch; b += 64) {
-    const ChunkSeq s = seq(b);
-    const int t = tiles_of(s, group, cut), n = runs_of(s);
-    items += t * n;
-    if (n > 1) {
-      tiles += t;
-      slots += t * n;
-    }
+  long sum = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long x = __shfl_up(sum, d);
+    if (lane >= d) sum += x;
   }
-  const int upto = wave_scan(items), upto_tiles = wave_scan(tiles), upto_slots = wave_scan(slots);
-  if (__builtin_amdgcn_readlane(upto, 63) > cut.items || __builtin_amdgcn_readlane(upto_slots, 63) > cut.slots ||
-      __builtin_amdgcn_readlane(upto_tiles, 63) > cut.joins)
-    return false;
-  joins = __builtin_amdgcn_readlane(upto_tiles, 63);
-  const unsigned long long who = __builtin_amdgcn_ballot_w64(r < upto);
-  if (!who) return false;
+  p.before = sum - mine;
+  p.upto = sum;
+  p.all = wave_last(sum);
+}
+
+// A place between two pages of the work: before page `page` of a tile, which is not
+// behind its last one; tile may be the number of the sequence's tiles.  b < 0: the end.
+struct Place {
+  int b, tile, page;
+};
+__device__ __forceinline__ bool same_tile(const Place& x, const Place& y) { return x.b == y.b && x.tile == y.tile; }
+__device__ __forceinline__ Place place_at(const ChunkPlan& p, const PagedChunk& a, int group, const ChunkCut& cut, long x) {
+  const unsigned long long who = __builtin_amdgcn_ballot_w64(x < p.upto);
+  if (!who) return Place{-1, 0, 0};
   const int src = __builtin_ctzll(who);
-  int at = __builtin_amdgcn_readlane(upto - items, src);
-  it.join = __builtin_amdgcn_readlane(upto_tiles - tiles, src);
-  it.slot = __builtin_amdgcn_readlane(upto_slots - slots, src);
+  x -= (long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)p.before, src) |
+              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(p.before >> 32), src) << 32);
   for (int b = src; b < a.c.batch; b += 64) {
-    ChunkSeq s = held;
-    if (b >= 64) s = chunk_seq(a, b);
-    const int from = b < 64 ? src : 0;                      // (the same in every lane: kept in scalar registers)
-    s.first = __builtin_amdgcn_readlane(s.first, from);
-    s.n = __builtin_amdgcn_readlane(s.n, from);
-    s.len = __builtin_amdgcn_readlane(s.len, from);
-    s.base = __builtin_amdgcn_readlane(s.base, from);
-    const int t = tiles_of(s, group, cut), n = runs_of(s);
-    if (r < at + t * n) {
-      // a sequence's first pages first, of those the tiles that see most
-      it.b = b;
-      it.seq = s;
-      it.run = (r - at) / t;
-      it.tile = t - 1 - (r - at) % t;
-      it.runs = n;
-      const long pages = tile_pages(s, group, cut, it.tile);
-      it.begin = __builtin_amdgcn_readfirstlane((int)(pages * it.run / n));
-      it.end = __builtin_amdgcn_readfirstlane((int)(pages * (it.run + 1) / n));
-      it.join = n > 1 ? it.join + it.tile : -1;
-      it.slot = n > 1 ? it.slot + it.tile * n : -1;
-      it.run = __builtin_amdgcn_readfirstlane(it.run);
-      it.tile = __builtin_amdgcn_readfirstlane(it.tile);
-      it.runs = __builtin_amdgcn_readfirstlane(n);
-      it.join = __builtin_amdgcn_readfirstlane(it.join);
-      it.slot = __builtin_amdgcn_readfirstlane(it.slot);
-      return true;
+    const ChunkSeq s = seq_of(a, b);
+    const int tiles = tiles_of(s, group, cut);
+    const long cost = tiles_cost(s, group, cut, tiles);
+    if (x >= cost) {
+      x -= cost;
+      continue;
     }
-    at += t * n;
-    if (n > 1) {
-      it.join += t;
-      it.slot += t * n;
+    int t = 0, behind = tiles;           // the tile with cost(t) <= x < cost(t + 1)
+    while (behind - t > 1) {
+      const int mid = (t + behind) / 2;
+      if (tiles_cost(s, group, cut, mid) <= x)
+        t = mid;
+      else
+        behind = mid;
     }
+    const long from = tiles_cost(s, group, cut, t), to = tiles_cost(s, group, cut, t + 1);
+    const int pages = tile_pages(s, group, cut, t);
+    int page = scalar((int)((double)(x - from) / (double)(to - from) * (double)pages));
+    if (page < cut.whole) page = 0;
+    if (page && pages - page < cut.whole) return Place{b, t + 1, 0};
+    return Place{b, t, page};
   }
-  return false;
+  return Place{-1, 0, 0};
 }
 
-// Workspace of a kind: o [slots][hkv][rows][D], then (m, l, l^, -) [slots][hkv][rows],
-// then the split tiles, then their number.  Sequences of many rows come first.
+// A share of the work, walked tile by tile.
+struct Share {
+  Place at, to;                         // pages from at.page on
+  ChunkSeq seq;
+  int tiles, end;                       // of the sequence; the tile's last page (behind it) in the share
+  bool ends;                            // the tile ends in the share
+};
+__device__ __forceinline__ Share share_of(const ChunkPlan& p, const PagedChunk& a, int group, const ChunkCut& cut, int number, int shares) {
+  Share s;
+  // equal parts: at least `least` pages and a tile's cost
+  const long least = (long)group * kPage * (cut.least + cut.tile_cost);
+  const int parts = scalar((int)max(1L, min((long)min(shares, cut.shares), p.all / least)));
+  s.at = s.to = Place{-1, 0, 0};
+  if (number >= parts || p.all == 0) return s;
+  const long each = p.all / parts, rest = p.all % parts;
+  s.at = place_at(p, a, group, cut, each * number + rest * number / parts);
+  if (number + 1 < parts) s.to = place_at(p, a, group, cut, each * (number + 1) + rest * (number + 1) / parts);
+  if (s.at.b >= 0) {
+    s.seq = seq_of(a, s.at.b);
+    s.tiles = tiles_of(s.seq, group, cut);
+  }
+  return s;
+}
+// The tile at s.at, or the next that there is; false: the share is over.
+__device__ __forceinline__ bool enter_tile(Share& s, const PagedChunk& a, int group, const ChunkCut& cut) {
+  for (;;) {
+    if (s.at.b < 0 || (same_tile(s.at, s.to) && s.at.page >= s.to.page)) return false;
+    if (s.at.tile < s.tiles) break;
+    s.at = Place{next_sequence(a, s.at.b), 0, 0};
+    if (s.at.b < 0) return false;
+    s.seq = seq_of(a, s.at.b);
+    s.tiles = tiles_of(s.seq, group, cut);
+  }
+  s.ends = !same_tile(s.at, s.to);
+  s.end = s.ends ? tile_pages(s.seq, group, cut, s.at.tile) : s.to.page;
+  return true;
+}
+__device__ __forceinline__ void leave_tile(Share& s) {
+  if (s.ends)
+    s.at = Place{s.at.b, s.at.tile + 1, 0};
+  else
+    s.at.page = s.end;
+}
+// The pages of a tile that are some: the table's entries 64 at a time, one a lane.
+struct TilePages {
+  Pages pg;
+  int b, end, page;                     // `page`: of the pool, the one found last
+};
+__device__ __forceinline__ TilePages pages_of_tile(const Share& s) { return TilePages{Pages{0, s.at.page - 64}, s.at.b, s.end, 0}; }
+// The first at or behind place j, or `end`.
+__device__ __forceinline__ int next_page(TilePages& x, const PagedChunk& a, int j, int lane) {
+  for (; j < x.end; ++j) {
+    if (j - x.pg.base >= 64) load_pages(x.pg, a.c, x.b, j, x.end - 1, lane);
+    x.page = __builtin_amdgcn_readlane(x.pg.mine, j - x.pg.base);
+    if ((unsigned)x.page < (unsigned)a.c.num_pages) break;
+  }
+  return scalar(j);
+}
+template <int D, bool kFp16>
+__device__ __forceinline__ const uint8_t* record_of(const TilePages& x, const PagedChunk& a, int head) {
+  return a.c.pool + ((size_t)scalar(x.page) * a.c.hkv + head) * paged_record_bytes(D, kFp16);
+}
+
+// Workspace of a kind: o [shares][2][hkv][rows][D], then (m, l, l^, -) [shares][2][hkv]
+// [rows], then what the shares cut.  A share leaves the part of a tile that began
+// before it in its first place, that of one that goes on behind it in its second.
+enum { kCutAfter = 1, kCutBefore = 2, kWithin = 4 };      // a tile goes on behind the share; began before it; both
 struct Split {
-  int b, tile, slot, runs;
+  int how, tile;                        // the tile that begins in the share and goes on behind it
+  ChunkSeq seq;
 };
 struct ChunkWs {
   float* o;
   float4* ml;
   Split* split;
-  int* joins;
 };
 __host__ __device__ __forceinline__ size_t chunk_ws_bytes(const PagedCache& c, const ChunkCut& cut) {
-  return (size_t)cut.slots * c.hkv * cut.rows * (c.D + 4) * 4 + cut.joins * sizeof(Split) + 16;
+  return (size_t)2 * cut.shares * c.hkv * cut.rows * (c.D + 4) * 4 + cut.shares * sizeof(Split);
 }
 __device__ __forceinline__ ChunkWs chunk_ws(uint8_t* ws, const PagedCache& c, const ChunkCut& cut) {
-  const size_t rows = (size_t)cut.slots * c.hkv * cut.rows;
+  const size_t rows = (size_t)2 * cut.shares * c.hkv * cut.rows;
   ChunkWs w;
   w.o = reinterpret_cast<float*>(ws);
   w.ml = reinterpret_cast<float4*>(w.o + rows * c.D);
   w.split = reinterpret_cast<Split*>(w.ml + rows);
-  w.joins = reinterpret_cast<int*>(w.split + cut.joins);
   return w;
+}
+__device__ __forceinline__ Split split_of(const PagedChunk& a, const Share& s) {
+  Split x = {0, 0, {0, 0, 0, 0}};
+  const bool before = s.at.b >= 0 && s.at.page > 0, within = before && same_tile(s.at, s.to);
+  if (before) x.how = within ? kWithin : kCutBefore;
+  if (s.to.b >= 0 && s.to.page > 0 && !within) x = Split{x.how | kCutAfter, s.to.tile, chunk_seq(a, s.to.b)};
+  return x;
 }
 
 // ---------------------------------------------------------------------------
@@ -265,10 +318,10 @@ struct Row {
   int limit;                            // the last key that it sees; -1: none, -2: no such row
   int at;                               // row of q and o (token, query head)
 };
-__device__ __forceinline__ Row row_of(const PagedChunk& a, const Item& it, int group, int head, int row) {
+__device__ __forceinline__ Row row_of(const PagedChunk& a, const ChunkSeq& s, int group, int head, int row) {
   const int token = row / group, g = row - token * group;
-  if (token >= it.seq.n) return Row{-2, 0};
-  return Row{max(-1, it.seq.base + token), (it.seq.first + token) * a.hq + head * group + g};
+  if (token >= s.n) return Row{-2, 0};
+  return Row{max(-1, s.base + token), (s.first + token) * a.hq + head * group + g};
 }
 
 // The query's operands: step c's channels of lane k, in the order of the keys'.
@@ -365,7 +418,8 @@ __device__ __forceinline__ h8v_t ones() { return h8v_t{1, 1, 1, 1, 1, 1, 1, 1}; 
 // Values of FP16 pages that some rows of a tile must not see: 0 times them has to be 0
 // also where they are infinite or NaN.  Of the keys that no row sees they are cleared;
 // of the others what is not finite is counted, per sign, over the keys that a row sees
-// (products of ones; NaN under both signs), added where it counts, and cleared.
+// (products of ones; NaN under both signs), and cleared: what it makes of the row's sums
+// is added when the tile ends.
 typedef uint32_t u4v_t __attribute__((ext_vector_type(4)));
 // Bit 15 of each half that is not finite.
 __device__ __forceinline__ u4v_t not_finite(u4v_t x) { return ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }
@@ -383,8 +437,9 @@ __device__ __forceinline__ u4v_t first_halves(int n) {
   }
   return m;
 }
-template <int G>
-__device__ __forceinline__ void add_not_finite(Rows16<G>& x, const u4v_t (&v)[2], int ct, int seen, int k) {
+// Bits 0 to 3: the lane's channels to which an infinity or NaN comes, 4 to 7: to which a
+// negative infinity or NaN does.
+__device__ __forceinline__ int count_not_finite(const u4v_t (&v)[2], int seen, int k) {
   f4v_t up = {0.0f, 0.0f, 0.0f, 0.0f}, down = up;
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
@@ -393,21 +448,21 @@ __device__ __forceinline__ void add_not_finite(Rows16<G>& x, const u4v_t (&v)[2]
     up = product(__builtin_bit_cast(h8v_t, one(odd & (nan | ~minus))), who, up);
     down = product(__builtin_bit_cast(h8v_t, one(odd & (nan | minus))), who, down);
   }
+  int bits = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x.o[ct][i] += up[i] > 0.0f ? INFINITY : 0.0f;
-    x.o[ct][i] -= down[i] > 0.0f ? INFINITY : 0.0f;
-  }
+  for (int i = 0; i < 4; ++i) bits |= (up[i] > 0.0f ? 1 << i : 0) | (down[i] > 0.0f ? 16 << i : 0);
+  return bits;
 }
 
-// Leaves 16 rows of an item: rounded and divided, or as a run's share.
+// Leaves 16 rows of a tile: rounded and divided, or (`part` >= 0, a place of the
+// workspace) as a share's part.
 template <int G>
-__device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, const Item& it, Rows16<G>& x, const Row& r, int head,
+__device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, long part, Rows16<G>& x, const Row& r, int head,
                                        int tile_rows, int row_in_tile, int k) {
   constexpr int D = 64 * G;
   const float l = sum_across_rows(x.l);
   if (r.limit == -2) return;
-  if (it.runs == 1) {
+  if (part < 0) {
     const float by = x.sum[0] == 0.0f ? 0.0f : 1.0f / x.sum[0];
 #pragma unroll
     for (int c = 0; c < 4 * G; ++c)
@@ -419,110 +474,97 @@ __device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, c
     }
     return;
   }
-  const size_t at = ((size_t)(it.slot + it.run) * a.c.hkv + head) * tile_rows + row_in_tile;
+  const size_t at = ((size_t)part * a.c.hkv + head) * tile_rows + row_in_tile;
 #pragma unroll
   for (int c = 0; c < 4 * G; ++c) *reinterpret_cast<f4v_t*>(ws.o + at * D + 16 * c + 4 * k) = x.o[c];
   if (k == 0) ws.ml[at] = make_float4(l == 0.0f ? -INFINITY : x.ref, l, x.sum[0], 0.0f);
 }
+// The place of a share's part of its present tile; -1: the whole tile is the share's.
+__device__ __forceinline__ long part_of(const Share& s, int number) {
+  return s.at.page > 0 ? 2L * number : s.ends ? -1L : 2L * number + 1;
+}
 
 // ---------------------------------------------------------------------------
 // Few rows over HIF4 pages.
-// One wave per (item, kv head): 16 NB rows; the operands are made of a page's record
-// in registers, one 16-byte load a lane for each KiB.  K of the next page is fetched once
-// this one's has been used, V while the scores are made.
+// One wave per (share, kv head): tiles of 16 NB rows; the operands are made of a page's
+// record in registers, one 16-byte load a lane for each KiB.  K of the next page is
+// fetched once this one's has been used, V while the scores are made.
 template <int G, int NB>
-__device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, int item, int head, int lane) {
+__device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, const ChunkPlan& plan, int number,
+                                           int shares, int head, int lane) {
   constexpr int D = 64 * G, kRows = 16 * NB;
   const int n = lane & 15, k = lane >> 4, group = a.hq / a.c.hkv;
-  Item it;
-  int joins;
-  const bool there = find_item(a, group, cut, item, lane, it, joins);
   const ChunkWs ws = chunk_ws(ws_at, a.c, cut);
-  if (item == 0 && head == 0 && lane == 0) *ws.joins = joins;
-  if (!there) return;
-  if (it.runs > 1 && it.run == 0 && head == 0 && lane == 0) ws.split[it.join] = Split{it.b, it.tile, it.slot, it.runs};
-
-  // the pages of the run that are some
-  Pages pg;
-  pg.base = it.begin - 64;
-  int page_at = 0;
-  const auto next = [&](int j) {
-    for (; j < it.end; ++j) {
-      if (j - pg.base >= 64) load_pages(pg, a.c, it.b, j, it.end - 1, lane);
-      page_at = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
-      if ((unsigned)page_at < (unsigned)a.c.num_pages) break;
-    }
-    return __builtin_amdgcn_readfirstlane(j);
-  };
-  const auto record = [&] {
-    const size_t at = (size_t)__builtin_amdgcn_readfirstlane(page_at) * a.c.hkv + head;
-    return a.c.pool + at * paged_record_bytes(D, false);
-  };
-  int j = next(it.begin);
-
-  Row row[NB];
-  Rows16<G> x[NB];
-  h8v_t q[NB][2 * G];
-#pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    row[i] = row_of(a, it, group, head, it.tile * kRows + 16 * i + n);
-    load_query<G, false>(q[i], a, row[i], head, k);
-    start(x[i]);
-  }
-  const int first_token = it.tile * kRows / group;          // every row of the tile sees the keys up to its
-  const int all_see = it.seq.base + first_token;
-
-  const uint8_t* rec = record();
+  Share s = share_of(plan, a, group, cut, number, shares);
+  if (head == 0 && lane == 0) ws.split[number] = split_of(a, s);
   HifPart<G> k4, v4;
-  if (j < it.end) load_hif4<G>(k4, rec, lane);
-  while (j < it.end) {
-    const int now = j;
-    const bool masked = now * kPage + kPage - 1 > all_see;
-    keep_order();
-    load_hif4<G>(v4, rec + 2304 * G, lane);
-    keep_order();
-    f4v_t s[NB][4];
-    h8v_t p[NB][2];
+  for (; enter_tile(s, a, group, cut); leave_tile(s)) {
+    TilePages tp = pages_of_tile(s);
+    int j = next_page(tp, a, s.at.page, lane);
+    const uint8_t* rec = record_of<D, false>(tp, a, head);
+    if (j < s.end) load_hif4<G>(k4, rec, lane);
+    Row row[NB];
+    Rows16<G> x[NB];
+    h8v_t q[NB][2 * G];
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < NB; ++i) {
+      row[i] = row_of(a, s.seq, group, head, s.at.tile * kRows + 16 * i + n);
+      load_query<G, false>(q[i], a, row[i], head, k);
+      start(x[i]);
+    }
+    const int all_see = s.seq.base + s.at.tile * kRows / group;     // every row of the tile sees the keys up to this one
+    while (j < s.end) {
+      const int key0 = j * kPage;
+      const bool masked = key0 + kPage - 1 > all_see;
+      keep_order();
+      load_hif4<G>(v4, rec + 2304 * G, lane);
+      keep_order();
+      f4v_t sc[NB][4];
+      h8v_t p[NB][2];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) s[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int c = 0; c < 2 * G; ++c)
+        for (int t = 0; t < 4; ++t) sc[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const h8v_t kr = part_operand<G>(k4, c >> 1, t, c & 1, lane);
+      for (int c = 0; c < 2 * G; ++c)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) s[i][t] = product(kr, q[i][c], s[i][t]);
-      }
-    keep_order();
-    j = next(j + 1);
-    rec = record();
-    if (j < it.end) load_hif4<G>(k4, rec, lane);
-    keep_order();
+        for (int t = 0; t < 4; ++t) {
+          const h8v_t kr = part_operand<G>(k4, c >> 1, t, c & 1, lane);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) soften<G, false>(x[i], s[i], p[i], a.scale, masked, row[i].limit - now * kPage, k);
-    keep_order();
+          for (int i = 0; i < NB; ++i) sc[i][t] = product(kr, q[i][c], sc[i][t]);
+        }
+      keep_order();
+      j = next_page(tp, a, j + 1, lane);
+      rec = record_of<D, false>(tp, a, head);
+      if (j < s.end) load_hif4<G>(k4, rec, lane);
+      keep_order();
 #pragma unroll
-    for (int u = 0; u < 4 * G; ++u)
+      for (int i = 0; i < NB; ++i) soften<G, false>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
+      keep_order();
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const h8v_t vr = part_operand<G>(v4, u >> 2, u & 3, c, lane);
+      for (int u = 0; u < 4 * G; ++u)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr, p[i][c], x[i].o[u]);
-      }
+        for (int c = 0; c < 2; ++c) {
+          const h8v_t vr = part_operand<G>(v4, u >> 2, u & 3, c, lane);
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+          for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr, p[i][c], x[i].o[u]);
+        }
 #pragma unroll
-      for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+    }
+    const long part = part_of(s, number);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) finish<G>(a, ws, part, x[i], row[i], head, kRows, 16 * i + n, k);
   }
-#pragma unroll
-  for (int i = 0; i < NB; ++i) finish<G>(a, ws, it, x[i], row[i], head, kRows, 16 * i + n, k);
 }
 
 template <int G, int NB>
-__global__ void __launch_bounds__(64, G == 4 ? 1 : 2) k_chunk_rows(PagedChunk a, ChunkCut cut, int few_ws) {
-  chunk_rows<G, NB>(a, cut, a.ws + few_ws, blockIdx.x / a.c.hkv, blockIdx.x % a.c.hkv, threadIdx.x);
+__global__ void __launch_bounds__(64, G == 4 ? 1 : 2) k_chunk_rows(PagedChunk a, ChunkCut cut) {
+  ChunkPlan plan;
+  count_costs(plan, a, chunk_seq(a, threadIdx.x), a.hq / a.c.hkv, cut, threadIdx.x);
+  chunk_rows<G, NB>(a, cut, a.ws, plan, blockIdx.x / a.c.hkv, cut.shares, blockIdx.x % a.c.hkv, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -604,198 +646,226 @@ struct CopyPieces {
     }
   }
 };
-__device__ __forceinline__ uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 template <int G, int kWaves>
 __device__ __forceinline__ void copy_share(h8v_t* page, const uint8_t* rec, int wave, int lane) {
   const uint64_t from = (uint64_t)(uintptr_t)(rec + 16384 * G / kWaves * wave);
   const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(page + 1024 * G / kWaves * wave);
-  CopyPieces<16384 * G / kWaves, 1024>::run((uint64_t)scalar((uint32_t)from) | (uint64_t)scalar((uint32_t)(from >> 32)) << 32, scalar(to),
+  CopyPieces<16384 * G / kWaves, 1024>::run((uint64_t)(uint32_t)scalar((int)from) | (uint64_t)(uint32_t)scalar((int)(from >> 32)) << 32, (uint32_t)scalar((int)to),
                                             16 * lane);
 }
 __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0)
 
+// How many of a head's workgroups take the sequences of many rows where there are both
+// kinds: by the time that their pages take.  A page of 16 rows on one of a workgroup's
+// waves counts kFewTime of one of 256 rows on all of them.
+constexpr float kFewTime = 0.2f;
+__device__ __forceinline__ int many_shares(long many, long few, int shares) {
+  if (few == 0) return shares;
+  if (many == 0) return 0;
+  const float m = (float)many, f = kFewTime * (float)few;
+  return max(1, min(shares - 1, (int)((float)shares * m / (m + f) + 0.5f)));
+}
+
 template <int G, bool kFp16, int kWaves, int NB>
-__global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut, ChunkCut few, int few_ws) {
+__global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut, ChunkCut few, size_t few_ws) {
   constexpr int D = 64 * G, kMine = 16 * NB, kRows = kMine * kWaves, kUnits = 16 * G;
   static_assert(16 * G % kWaves == 0 && 4 * G % kWaves == 0, "equal shares");
   extern __shared__ __align__(16) uint8_t smem[];
   h8v_t* const pages = reinterpret_cast<h8v_t*>(smem);
   const int lane = threadIdx.x & 63, n = lane & 15, k = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int wave = scalar((int)(threadIdx.x >> 6));
   const int head = blockIdx.x % a.c.hkv, group = a.hq / a.c.hkv, number = blockIdx.x / a.c.hkv;
+  const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
+  ChunkPlan plan;
+  const ChunkSeq first = chunk_seq(a, lane);                // the first 64 sequences are read once
+  count_costs(plan, a, first, group, cut, lane);
+  int shares = cut.shares;
   if constexpr (!kFp16) {
-    if (number >= cut.items) {            // behind the sequences of many rows those of few, an item a wave
-      const int item = (number - cut.items) * kWaves + wave;
-      if (item < few.items) chunk_rows<G, 1>(a, few, a.ws + few_ws, item, head, lane);
+    ChunkPlan other;
+    count_costs(other, a, first, group, few, lane);
+    shares = scalar(many_shares(plan.all, other.all, cut.shares));
+    const int rest = cut.shares - shares;
+    Split* const split = chunk_ws(a.ws + few_ws, a.c, few).split;
+    if (number >= shares) {               // the rest of the workgroups: a share a wave
+      if (head == 0 && threadIdx.x == 0) ws.split[number] = Split{};
+      chunk_rows<G, 1>(a, few, a.ws + few_ws, other, wave * rest + number - shares, rest * kWaves, head, lane);
       return;
     }
+    if (head == 0 && lane == 0) split[rest * kWaves + number * kWaves + wave] = Split{};
   }
-  Item it;
-  int joins;
-  const bool there = find_item(a, group, cut, number, lane, it, joins);
-  const ChunkWs ws = chunk_ws(a.ws, a.c, cut);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *ws.joins = joins;
-  if (!there) return;
-  if (it.runs > 1 && it.run == 0 && head == 0 && threadIdx.x == 0) ws.split[it.join] = Split{it.b, it.tile, it.slot, it.runs};
-
-  // pages from here on that are some; the table's entries 64 at a time, one a lane
-  Pages pg;
-  pg.base = it.begin - 64;
-  int page_at = 0;                        // the page that next() has found
-  const auto next = [&](int j) {
-    for (; j < it.end; ++j) {
-      if (j - pg.base >= 64) load_pages(pg, a.c, it.b, j, it.end - 1, lane);
-      page_at = __builtin_amdgcn_readlane(pg.mine, j - pg.base);
-      if ((unsigned)page_at < (unsigned)a.c.num_pages) break;
-    }
-    return __builtin_amdgcn_readfirstlane(j);
-  };
-  const auto record = [&] {
-    const size_t at = (size_t)__builtin_amdgcn_readfirstlane(page_at) * a.c.hkv + head;
-    return a.c.pool + at * paged_record_bytes(D, kFp16);
-  };
+  Share s = share_of(plan, a, group, cut, number, shares);
+  if (head == 0 && threadIdx.x == 0) ws.split[number] = split_of(a, s);
   HifShare<G, kWaves> share;
-  int j = next(it.begin);
-  if (j < it.end) {
-    if constexpr (kFp16)
-      copy_share<G, kWaves>(pages, record(), wave, lane);
-    else
-      share.load(record(), wave, lane);
-  }
-
-  const int row0 = it.tile * kRows + wave * kMine;      // the wave's first row
-  Row row[NB];
-  Rows16<G> x[NB];
-  h8v_t q[NB][2 * G];
-#pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    row[i] = row_of(a, it, group, head, row0 + 16 * i + n);
-    load_query<G, kFp16>(q[i], a, row[i], head, k);
-    start(x[i]);
-  }
-  // keys that every row of the wave sees, and that any of them sees: up to these
-  const int first_token = row0 / group, last_token = min(it.seq.n - 1, (row0 + kMine - 1) / group);
-  const int all_see = it.seq.base + first_token, some_see = first_token < it.seq.n ? it.seq.base + last_token : -1;
-
-  int ahead = next(j + 1), at = 0;
-  if constexpr (kFp16) {
-    wait_copies();
-  } else {
-    if (j < it.end) share.store(pages, wave, lane);
-    if (ahead < it.end) share.load(record(), wave, lane);
-  }
-  __syncthreads();
-  while (j < it.end) {
-    const h8v_t* page = pages + 64 * kUnits * at + lane;
-    const int now = j;
-    j = ahead;
-    if (j < it.end) {
-      h8v_t* const other = pages + 64 * kUnits * (at ^ 1);
-      if constexpr (kFp16) {
-        copy_share<G, kWaves>(other, record(), wave, lane);
-        ahead = next(j + 1);
-      } else {
-        share.store(other, wave, lane);
-        ahead = next(j + 1);
-        if (ahead < it.end) share.load(record(), wave, lane);
-      }
+  // what is not finite and comes to the lane's sums: [channels / 16][lane][16 rows]
+  uint8_t* const odd_sums = smem + 2 * 1024 * kUnits + (wave * 4 * G * 64 + lane) * NB;
+  for (; enter_tile(s, a, group, cut); leave_tile(s)) {
+    // page j is in LDS, page `ahead` on its way (HIF4) or next to be copied
+    TilePages tp = pages_of_tile(s);
+    int j = next_page(tp, a, s.at.page, lane), at = 0;
+    if (j < s.end) {
+      if constexpr (kFp16)
+        copy_share<G, kWaves>(pages, record_of<D, true>(tp, a, head), wave, lane);
+      else
+        share.load(record_of<D, false>(tp, a, head), wave, lane);
     }
-    if (now * kPage <= some_see) {
-      const bool masked = now * kPage + kPage - 1 > all_see;
-      f4v_t s[NB][4];
-      h8v_t p[NB][2];
+    const int row0 = s.at.tile * kRows + wave * kMine;      // the wave's first row
+    Row row[NB];
+    Rows16<G> x[NB];
+    h8v_t q[NB][2 * G];
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) s[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-      // Operands come four units ahead of their products: a wave's own products have to
-      // cover LDS's latency, there are two waves a SIMD.
-      h8v_t next4[2][4];
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) next4[0][t] = page[64 * (t * 2 * G)];
-#pragma unroll
-      for (int c = 0; c < 2 * G; ++c) {
-        if (c + 1 < 2 * G)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) next4[(c + 1) & 1][t] = page[64 * (t * 2 * G + c + 1)];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < NB; ++i) s[i][t] = product(next4[c & 1][t], q[i][c], s[i][t]);
-      }
-      __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
-#pragma unroll
-      for (int c = 0; c < 2 * G; ++c) {
-        if (c + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
-      }
-      keep_order();
-      __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) next4[0][u] = page[64 * (8 * G + u)];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], s[i], p[i], a.scale, masked, row[i].limit - now * kPage, k);
-      keep_order();
-      const bool odd_values = kFp16 && masked;
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
-      if (odd_values) {
-#pragma unroll
-        for (int u = 0; u < 4 * G; ++u) {
-          keep_order();
-          u4v_t v[2];
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            v[c] = __builtin_bit_cast(u4v_t, page[64 * (8 * G + 2 * u + c)]) & first_halves(some_see - now * kPage + 1 - 16 * k - 8 * c);
-          if (__builtin_amdgcn_ballot_w64(any(not_finite(v[0]) | not_finite(v[1])))) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) add_not_finite<G>(x[i], v, u, row[i].limit - now * kPage, k);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) v[c] &= ~whole(not_finite(v[c]));
-          }
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < NB; ++i) x[i].o[u] = product(__builtin_bit_cast(h8v_t, v[c]), p[i][c], x[i].o[u]);
+    for (int i = 0; i < NB; ++i) {
+      row[i] = row_of(a, s.seq, group, head, row0 + 16 * i + n);
+      load_query<G, kFp16>(q[i], a, row[i], head, k);
+      start(x[i]);
+    }
+    // keys that every row of the wave sees, and that any of them sees: up to these
+    const int first_token = row0 / group, last_token = min(s.seq.n - 1, (row0 + kMine - 1) / group);
+    const int all_see = s.seq.base + first_token, some_see = first_token < s.seq.n ? s.seq.base + last_token : -1;
+    bool any_odd = false;
+    int ahead = next_page(tp, a, j + 1, lane);
+    if constexpr (kFp16) {
+      wait_copies();
+    } else {
+      if (j < s.end) share.store(pages, wave, lane);
+      if (ahead < s.end) share.load(record_of<D, false>(tp, a, head), wave, lane);
+    }
+    __syncthreads();
+    while (j < s.end) {
+      const h8v_t* page = pages + 64 * kUnits * at + lane;
+      const int key0 = j * kPage;
+      j = ahead;
+      if (j < s.end) {
+        h8v_t* const other = pages + 64 * kUnits * (at ^ 1);
+        if constexpr (kFp16) {
+          copy_share<G, kWaves>(other, record_of<D, true>(tp, a, head), wave, lane);
+          ahead = next_page(tp, a, j + 1, lane);
+        } else {
+          share.store(other, wave, lane);
+          ahead = next_page(tp, a, j + 1, lane);
+          if (ahead < s.end) share.load(record_of<D, false>(tp, a, head), wave, lane);
         }
-      } else {
+      }
+      if (key0 <= some_see) {
+        const bool masked = key0 + kPage - 1 > all_see;
+        f4v_t sc[NB][4];
+        h8v_t p[NB][2];
 #pragma unroll
-        for (int g = 0; g < 2 * G; ++g) {
-          if (g + 1 < 2 * G)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) next4[(g + 1) & 1][u] = page[64 * (8 * G + 4 * g + 4 + u)];
+          for (int t = 0; t < 4; ++t) sc[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+        // Operands come four units ahead of their products: a wave's own products have to
+        // cover LDS's latency, there are two waves a SIMD.
+        h8v_t next4[2][4];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-          for (int u = 0; u < 4; ++u)
+        for (int t = 0; t < 4; ++t) next4[0][t] = page[64 * (t * 2 * G)];
 #pragma unroll
-            for (int i = 0; i < NB; ++i) x[i].o[2 * g + u / 2] = product(next4[g & 1][u], p[i][u & 1], x[i].o[2 * g + u / 2]);
+        for (int c = 0; c < 2 * G; ++c) {
+          if (c + 1 < 2 * G)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) next4[(c + 1) & 1][t] = page[64 * (t * 2 * G + c + 1)];
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) sc[i][t] = product(next4[c & 1][t], q[i][c], sc[i][t]);
         }
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
 #pragma unroll
-        for (int g = 0; g < 2 * G; ++g) {
-          if (g + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+        for (int c = 0; c < 2 * G; ++c) {
+          if (c + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
           __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
         }
         keep_order();
-      }
-      __builtin_amdgcn_s_setprio(0);
-    }
-    at ^= 1;
-    if constexpr (kFp16) wait_copies();
-    __syncthreads();
-  }
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-  for (int i = 0; i < NB; ++i) finish<G>(a, ws, it, x[i], row[i], head, kRows, wave * kMine + 16 * i + n, k);
+        for (int u = 0; u < 4; ++u) next4[0][u] = page[64 * (8 * G + u)];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
+        keep_order();
+        const bool odd_values = kFp16 && masked;
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+        if (odd_values) {
+          bool odd = false;
+#pragma unroll 1
+          for (int u = 0; u < 8 * G; ++u)
+            odd |= any(not_finite(__builtin_bit_cast(u4v_t, page[64 * (8 * G + u)]) & first_halves(some_see - key0 + 1 - 16 * k - 8 * (u & 1))));
+          const bool found = __builtin_amdgcn_ballot_w64(odd) != 0;
+          if (found) {
+#pragma unroll 1
+            for (int u = 0; u < 4 * G; ++u) {
+              u4v_t v[2];
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+                v[c] = __builtin_bit_cast(u4v_t, page[64 * (8 * G + 2 * u + c)]) & first_halves(some_see - key0 + 1 - 16 * k - 8 * c);
+#pragma unroll
+              for (int i = 0; i < NB; ++i) {
+                uint8_t* const bits = odd_sums + u * 64 * NB + i;
+                *bits = (uint8_t)(count_not_finite(v, row[i].limit - key0, k) | (any_odd ? *bits : 0));
+              }
+            }
+            any_odd = true;
+          }
+#pragma unroll
+          for (int u = 0; u < 4 * G; ++u)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              u4v_t v = __builtin_bit_cast(u4v_t, page[64 * (8 * G + 2 * u + c)]) & first_halves(some_see - key0 + 1 - 16 * k - 8 * c);
+              if (found) v &= ~whole(not_finite(v));
+#pragma unroll
+              for (int i = 0; i < NB; ++i) x[i].o[u] = product(__builtin_bit_cast(h8v_t, v), p[i][c], x[i].o[u]);
+            }
+        } else {
+#pragma unroll
+          for (int g = 0; g < 2 * G; ++g) {
+            if (g + 1 < 2 * G)
+#pragma unroll
+              for (int u = 0; u < 4; ++u) next4[(g + 1) & 1][u] = page[64 * (8 * G + 4 * g + 4 + u)];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+              for (int i = 0; i < NB; ++i) x[i].o[2 * g + u / 2] = product(next4[g & 1][u], p[i][u & 1], x[i].o[2 * g + u / 2]);
+          }
+#pragma unroll
+          for (int g = 0; g < 2 * G; ++g) {
+            if (g + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
+          }
+          keep_order();
+        }
+        __builtin_amdgcn_s_setprio(0);
+      }
+      at ^= 1;
+      if constexpr (kFp16) wait_copies();
+      __syncthreads();
+    }
+    if (any_odd) {
+#pragma unroll
+      for (int u = 0; u < 4 * G; ++u)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const int bits = odd_sums[u * 64 * NB + i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[i].o[u][e] += bits >> e & 1 ? INFINITY : 0.0f;
+            x[i].o[u][e] -= bits >> (4 + e) & 1 ? INFINITY : 0.0f;
+          }
+        }
+    }
+    const long part = part_of(s, number);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) finish<G>(a, ws, part, x[i], row[i], head, kRows, wave * kMine + 16 * i + n, k);
+  }
 }
 
 // ---------------------------------------------------------------------------
-// Joining the runs of a split tile's rows: with m the largest of their references,
-// o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in a fixed
-// order.  kFew: a workgroup takes 32 channels of a row, its threads share out the runs
-// (many, where there are few rows); else a wave takes a row.  The workgroups go
-// through the split tiles that there are.
+// Joining the parts of a row that several shares hold: with m the largest of their
+// references, o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in
+// the shares' order.  kFew: a workgroup takes 32 channels of a row, its threads share out
+// the parts (many, where there are few rows); else a wave takes a row.
 constexpr int kChunkJoin = 256;
 
 struct Joined {
@@ -811,34 +881,47 @@ __device__ __forceinline__ void join_pair(Joined& x, const Joined& y) {
   x.o = x.o * f + y.o * g;
 }
 
+constexpr int kJoinRows = 16;           // of a workgroup where a wave takes a row
+
 template <int G, bool kFew>
-__device__ __forceinline__ void join_tiles(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, Joined* part) {
+__device__ __forceinline__ void join_tile(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, int block, Joined* part) {
   constexpr int D = 64 * G, kCols = kFew ? 8 : D / 4, kSets = (kFew ? kChunkJoin : 64) / kCols, kAhead = 4;
   const int lane = threadIdx.x & 63, at_set = kFew ? threadIdx.x : lane, col = at_set % kCols, set = at_set / kCols;
   const ChunkWs ws = chunk_ws(ws_at, a.c, cut);
-  const int group = a.hq / a.c.hkv, slices = kFew ? D / 32 : 1, rows = *ws.joins * a.c.hkv * cut.rows;
-  const int step = kFew ? gridDim.x : 4 * gridDim.x;
-  for (int item = kFew ? blockIdx.x : 4 * blockIdx.x + (threadIdx.x >> 6); item < rows * slices; item += step) {
-    const int at = item / slices, row_in_tile = at % cut.rows, head = at / cut.rows % a.c.hkv;
-    const Split sp = ws.split[at / cut.rows / a.c.hkv];
-    const int ch = (item % slices) * 32 + 4 * col;
-    Item it;
-    it.seq = chunk_seq(a, sp.b);
-    const Row row = row_of(a, it, group, head, sp.tile * cut.rows + row_in_tile);
+  const int group = a.hq / a.c.hkv;
+  // workgroups of a share and head: kFew rows times slices of 32 channels, else sets of kJoinRows rows
+  const int per = kFew ? cut.rows * (D / 32) : cut.rows / kJoinRows;
+  const int first = block / per / a.c.hkv, head = block / per % a.c.hkv;
+  const Split sp = ws.split[first];
+  if (!(sp.how & kCutAfter)) return;
+  // the shares that lie within the tile, then the one that it ends in
+  int parts = 2;
+  for (int from = first + 1; from < cut.shares; from += 64) {
+    const bool goes_on = from + lane < cut.shares && (ws.split[from + lane].how & kWithin);
+    const unsigned long long stops = ~__builtin_amdgcn_ballot_w64(goes_on);
+    parts += stops ? __builtin_ctzll(stops) : 64;
+    if (stops) break;
+  }
+  const int ch = (kFew ? block % per % (D / 32) * 32 : 0) + 4 * col;
+#pragma unroll
+  for (int r = 0; r < (kFew ? 1 : kJoinRows / 4); ++r) {
+    const int row_in_tile = kFew ? block % per / (D / 32) : block % per * kJoinRows + 4 * r + (int)(threadIdx.x >> 6);
+    const Row row = row_of(a, sp.seq, group, head, sp.tile * cut.rows + row_in_tile);
     if (row.limit == -2) continue;
     Joined x = {-INFINITY, 0.0f, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int i = set; i < sp.runs; i += kAhead * kSets) {
+    for (int i = set; i < parts; i += kAhead * kSets) {
       float4 ml[kAhead];
       f4v_t y[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const size_t from = ((size_t)(sp.slot + min(i + u * kSets, sp.runs - 1)) * a.c.hkv + head) * cut.rows + row_in_tile;
+        const int share = first + min(i + u * kSets, parts - 1);
+        const size_t from = (((size_t)2 * share + (share == first)) * a.c.hkv + head) * cut.rows + row_in_tile;
         ml[u] = ws.ml[from];
         y[u] = *reinterpret_cast<const f4v_t*>(ws.o + from * D + ch);
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
-        if (i + u * kSets < sp.runs) join_pair(x, Joined{ml[u].x, ml[u].y, ml[u].z, y[u]});
+        if (i + u * kSets < parts) join_pair(x, Joined{ml[u].x, ml[u].y, ml[u].z, y[u]});
     }
     if constexpr (kFew) {
       part[threadIdx.x] = x;
@@ -869,64 +952,66 @@ __device__ __forceinline__ void join_tiles(const PagedChunk& a, const ChunkCut& 
     }
   }
 }
+__host__ __device__ __forceinline__ size_t join_blocks(const PagedCache& c, const ChunkCut& cut, bool few) {
+  return cut.shares < 2 ? 0 : (size_t)cut.shares * c.hkv * (few ? cut.rows * (c.D / 32) : cut.rows / kJoinRows);
+}
 template <int G, bool kFew>
-__global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCut cut, ChunkCut few, int few_ws) {
+__global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCut cut, ChunkCut few, size_t few_ws) {
   __shared__ Joined part[kFew ? kChunkJoin : 1];
-  if (cut.joins) join_tiles<G, kFew>(a, cut, a.ws, part);
-  if (few.joins) join_tiles<G, kFew>(a, few, a.ws + few_ws, part);
+  const int many = (int)join_blocks(a.c, cut, kFew), block = blockIdx.x;
+  if (block < many)
+    join_tile<G, kFew>(a, cut, a.ws, block, part);
+  else
+    join_tile<G, kFew>(a, few, a.ws + few_ws, block - many, part);
 }
 
 // ---------------------------------------------------------------------------
 // Rows (of one sequence and kv head) up to which a wave of its own takes them.
 constexpr int kFewRows = 32;
-
 // Waves of a workgroup that share a page.
 constexpr int wide_waves(int D) { return D == 128 ? 8 : 4; }
-
-// Sizes of one kind: sequences of more than `above` rows, of which there are at most
-// `most`, with `all` rows in total.
-static bool cut_kind(const PagedCache& c, size_t all, size_t most, size_t batch, ChunkCut* cut) {
-  const size_t tiles = std::min(batch * ((most + cut->rows - 1) / cut->rows), all / cut->rows + batch);
-  const size_t runs = std::max<size_t>(1, ((size_t)c.max_pages + kMinRun - 1) / kMinRun);
-  const size_t items = std::min(tiles * runs, tiles + cut->target + 1);
-  const size_t joins = runs == 1 ? 0 : std::min(tiles, (size_t)cut->target + 1);
-  if (items * c.hkv >= kMaxGrid || joins * c.hkv * cut->rows >= kMaxGrid) return false;
-  cut->items = (int)items;
-  cut->joins = (int)joins;
-  cut->slots = runs == 1 ? 0 : (int)std::min(tiles * runs, (size_t)2 * cut->target + 2);
-  return true;
+// Workgroups that the chip holds at once: by the registers of their waves, or by their
+// LDS where one wave copies FP16 pages.
+constexpr int resident(int D, bool fp16, int waves) {
+  return waves > 1 ? (D == 64 ? 512 : 256) : fp16 ? (D == 64 ? 1024 : D == 128 ? 512 : 256) : D == 256 ? 1024 : 2048;
 }
+
 struct ChunkCuts {
-  int waves;                            // of a workgroup that takes many rows; 1: there are but few
+  int waves;                            // of a workgroup
   ChunkCut many, few;
-  int few_ws;                           // offset in the workspace
-  size_t blocks, joined, bytes;         // workgroups, rows that may be joined
+  size_t few_ws, blocks, joined, bytes; // offset in the workspace; workgroups; rows that may be joined
 };
+// Shares of a kind: those that `most` workgroups (or waves) of a head take, if there can be as many.
+static int most_shares(const PagedCache& c, const ChunkCut& cut, size_t tiles, size_t most) {
+  const size_t all = tiles * ((size_t)c.max_pages + cut.tile_cost) / (cut.least + cut.tile_cost) + 1;
+  return (int)std::min(all, most);
+}
 static bool chunk_cuts(const PagedCache& c, int hq, int total, int max_new, ChunkCuts* x) {
-  const size_t group = hq / c.hkv, most = max_new * group, all = (size_t)total * group;
+  const size_t group = hq / c.hkv, most = max_new * group, all = (size_t)total * group, batch = c.batch;
   if (most >= (size_t)1 << 30) return false;
-  const bool wide = most > kFewRows;
+  const bool wide = most > kFewRows, both = wide && !c.fp16;
   x->waves = wide ? wide_waves(c.D) : 1;
-  x->many = ChunkCut{wide ? 32 * x->waves : 0, 0, c.fp16 ? 0 : kFewRows, 1 << 30, 0, 0, 0};
-  x->few = ChunkCut{16, 0, 0, kFewRows, 0, 0, 0};
-  const int waves = 1024 * (c.D == 256 ? 1 : 2);            // that the chip holds
-  if (c.fp16) {
-    if (!wide) x->many.rows = most <= 16 ? 16 : 32;
-    x->many.target = std::max(1, waves / x->waves / c.hkv);
-    if (!cut_kind(c, all, most, c.batch, &x->many)) return false;
+  const size_t per_head = std::max<size_t>(both ? 2 : 1, resident(c.D, c.fp16, x->waves) / c.hkv);
+  x->many = ChunkCut{wide ? 32 * x->waves : most <= 16 ? 16 : 32, c.fp16 ? 0 : kFewRows, 1 << 30, 0, wide ? 3 : 1, wide ? 4 : 2, wide ? 6 : 1};
+  x->few = ChunkCut{!wide && most > 16 && c.D != 256 ? 32 : 16, 0, kFewRows, 0, 1, 2, 1};
+  const auto tiles = [&](const ChunkCut& cut, size_t seqs, size_t rows) {
+    return std::min(seqs * ((rows + cut.rows - 1) / cut.rows), all / cut.rows + seqs);
+  };
+  if (both) {                             // the few's waves come in the same workgroups
+    x->many.shares = (int)per_head;
+    x->few.shares = (int)per_head * x->waves;
+  } else if (c.fp16) {
+    x->many.shares = most_shares(c, x->many, tiles(x->many, batch, most), per_head);
   } else {
-    if (!wide && most > 16 && c.D != 256) x->few.rows = 32;
-    x->few.target = std::max(1, waves / (wide ? 2 : 1) / c.hkv);
-    if (!cut_kind(c, all, std::min(most, (size_t)kFewRows), c.batch, &x->few)) return false;
-    x->many.target = std::max(1, waves / x->waves / c.hkv);
-    if (wide && !cut_kind(c, all, most, std::min((size_t)c.batch, all / (kFewRows + 1)), &x->many)) return false;
+    x->few.shares = most_shares(c, x->few, tiles(x->few, batch, most), per_head);
   }
-  const size_t many = (chunk_ws_bytes(c, x->many) + 255) / 256 * 256;
-  x->few_ws = (int)many;
-  x->bytes = many + chunk_ws_bytes(c, x->few);
-  x->blocks = (x->many.items + ((size_t)x->few.items + x->waves - 1) / x->waves) * c.hkv;
-  x->joined = ((size_t)x->many.joins * x->many.rows + (size_t)x->few.joins * x->few.rows) * c.hkv;
-  return many < (size_t)1 << 31 && x->blocks < max_grid(64 * x->waves);
+  const size_t many = x->many.shares ? (chunk_ws_bytes(c, x->many) + 255) / 256 * 256 : 0;
+  x->few_ws = many;
+  x->bytes = many + chunk_ws_bytes(c, x->few) + 16;
+  x->blocks = (size_t)(x->many.shares ? x->many.shares : x->few.shares) * c.hkv;
+  x->joined = ((size_t)(x->many.shares > 1 ? x->many.shares : 0) * x->many.rows +
+               (size_t)(x->few.shares > 1 ? x->few.shares : 0) * x->few.rows) * c.hkv;
+  return x->blocks < max_grid(64 * x->waves) && x->joined < (size_t)1 << 26;
 }
 
 bool paged_chunk_fits(const PagedCache& c, int hq, int total, int max_new) {
@@ -940,7 +1025,7 @@ size_t paged_chunk_workspace(const PagedCache& c, int hq, int total, int max_new
 
 template <int G, bool kFp16, int kWaves, int NB>
 static hipError_t launch_wide(const PagedChunk& a, const ChunkCuts& x, hipStream_t st) {
-  constexpr size_t kLds = (size_t)2 * 16 * G * 1024;
+  constexpr size_t kLds = (size_t)2 * 16 * G * 1024 + (kFp16 ? kWaves * 4 * G * 64 * NB : 0);
   const auto kernel = k_chunk_wide<G, kFp16, kWaves, NB>;
   if (kLds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
@@ -953,23 +1038,25 @@ template <int G>
 static hipError_t launch_chunk(const PagedChunk& a, const ChunkCuts& x, hipStream_t st) {
   hipError_t e;
   if (a.c.fp16) {
-    e = x.waves > 1            ? launch_wide<G, true, wide_waves(64 * G), 2>(a, x, st)
+    e = x.waves > 1         ? launch_wide<G, true, wide_waves(64 * G), 2>(a, x, st)
         : x.many.rows == 16 ? launch_wide<G, true, 1, 1>(a, x, st)
                             : launch_wide<G, true, 1, 2>(a, x, st);
   } else if (x.waves > 1) {
     e = launch_wide<G, false, wide_waves(64 * G), 2>(a, x, st);
   } else {
     if (G == 4 || x.few.rows == 16)
-      k_chunk_rows<G, 1><<<dim3((unsigned)x.blocks), 64, 0, st>>>(a, x.few, x.few_ws);
+      k_chunk_rows<G, 1><<<dim3((unsigned)x.blocks), 64, 0, st>>>(a, x.few);
     else
-      k_chunk_rows<G == 4 ? 1 : G, 2><<<dim3((unsigned)x.blocks), 64, 0, st>>>(a, x.few, x.few_ws);
+      k_chunk_rows<G == 4 ? 1 : G, 2><<<dim3((unsigned)x.blocks), 64, 0, st>>>(a, x.few);
     e = hipGetLastError();
   }
   if (e != hipSuccess || x.joined == 0) return e;
-  if (x.joined <= 2048)
-    k_chunk_join<G, true><<<dim3((unsigned)(x.joined * (2 * G))), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
+  const bool few = x.joined <= 2048;
+  const dim3 grid((unsigned)(join_blocks(a.c, x.many, few) + join_blocks(a.c, x.few, few)));
+  if (few)
+    k_chunk_join<G, true><<<grid, kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   else
-    k_chunk_join<G, false><<<dim3((unsigned)std::min<size_t>(2048, x.joined / 4)), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
+    k_chunk_join<G, false><<<grid, kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   return hipGetLastError();
 }
 

@@ -20,6 +20,7 @@
 #include "hifa4_paged_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hifa4 {
 
@@ -324,47 +325,64 @@ __device__ __forceinline__ Row row_of(const PagedChunk& a, const ChunkSeq& s, in
   return Row{max(-1, s.base + token), (s.first + token) * a.hq + head * group + g};
 }
 
-// The query's operands: step c's channels of lane k, in the order of the keys'.
-template <int G, bool kFp16>
-__device__ __forceinline__ void load_query(h8v_t (&q)[2 * G], const PagedChunk& a, const Row& r, int head, int k) {
+// The queries' operands: step c's channels of lane k, in the order of the keys'.  All
+// loads are on their way before the first is used.
+template <int G, bool kFp16, int NB>
+__device__ __forceinline__ void load_queries(h8v_t (&q)[NB][2 * G], const PagedChunk& a, const Row (&r)[NB], int head, int k) {
+  const auto channel = [k](int c) { return kFp16 ? 32 * c + 8 * k : 64 * (c >> 1) + 16 * k + 8 * (c & 1); };
 #pragma unroll
-  for (int c = 0; c < 2 * G; ++c) {
-    const int ch = kFp16 ? 32 * c + 8 * k : 64 * (c >> 1) + 16 * k + 8 * (c & 1);
-    h8v_t x = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (r.limit > -2) {
-      x = *reinterpret_cast<const h8v_t*>(a.q + (size_t)r.at * (64 * G) + ch);
-      if (a.s) {
-        const f4v_t* s = reinterpret_cast<const f4v_t*>(a.s + (size_t)head * (64 * G) + ch);
-        const f4v_t s0 = s[0], s1 = s[1];
+  for (int i = 0; i < NB; ++i) {
+    const half_t* row = a.q + (size_t)r[i].at * (64 * G);      // (the first row where there is none)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = round_product(x[i], i < 4 ? s0[i & 3] : s1[i & 3]);
-      }
-    }
-    q[c] = kFp16 ? x : __builtin_shufflevector(x, x, 0, 4, 1, 5, 2, 6, 3, 7);
+    for (int c = 0; c < 2 * G; ++c) q[i][c] = *reinterpret_cast<const h8v_t*>(row + channel(c));
   }
+  if (a.s) {
+    f4v_t s[2 * G][2];
+#pragma unroll
+    for (int c = 0; c < 2 * G; ++c) {
+      const f4v_t* from = reinterpret_cast<const f4v_t*>(a.s + (size_t)head * (64 * G) + channel(c));
+      s[c][0] = from[0];
+      s[c][1] = from[1];
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int c = 0; c < 2 * G; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[i][c][e] = round_product(q[i][c][e], s[c][e >> 2][e & 3]);
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int c = 0; c < 2 * G; ++c) {
+      if (r[i].limit == -2) q[i][c] = h8v_t{0, 0, 0, 0, 0, 0, 0, 0};
+      if (!kFp16) q[i][c] = __builtin_shufflevector(q[i][c], q[i][c], 0, 4, 1, 5, 2, 6, 3, 7);
+    }
 }
 
 // The state of 16 rows' softmax, and their sums.
-template <int G>
+// The sum of p as it was rounded is a lane's share, by dot products; or, where the vector
+// instructions have more to do than the matrix instructions, the whole sum by a product.
+template <int G, bool kDot>
 struct Rows16 {
-  float ref, l;                         // p = 2^(score - ref), scores in log2 units; l: the lane's share
-  f4v_t sum;                            // of the rounded p
+  float ref, l;                         // p = 2^(score - ref), scores in log2 units; l: the lane's share of its sum
+  std::conditional_t<kDot, float, f4v_t> sum;
   f4v_t o[4 * G];                       // channels 16 ct + 4k + v
 };
-template <int G>
-__device__ __forceinline__ void start(Rows16<G>& x) {
+template <int G, bool kDot>
+__device__ __forceinline__ void start(Rows16<G, kDot>& x) {
   const f4v_t z = {0.0f, 0.0f, 0.0f, 0.0f};
   x.ref = kNoRef;
   x.l = 0.0f;
-  x.sum = z;
+  x.sum = {};
 #pragma unroll
   for (int c = 0; c < 4 * G; ++c) x.o[c] = z;
 }
 
 // A page's scores (s[t][v]: key 16k + 4t + v, before the scale) to the second product's
 // operands; keys behind `seen` (the row's limit in the page) do not count.
-template <int G, bool kFp16>
-__device__ __forceinline__ void soften(Rows16<G>& x, f4v_t (&s)[4], h8v_t (&p)[2], float scale, bool masked, int seen, int k) {
+template <int G, bool kFp16, bool kDot>
+__device__ __forceinline__ void soften(Rows16<G, kDot>& x, f4v_t (&s)[4], h8v_t (&p)[2], float scale, bool masked, int seen, int k) {
   if (masked) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -407,13 +425,15 @@ __device__ __forceinline__ void soften(Rows16<G>& x, f4v_t (&s)[4], h8v_t (&p)[2
   for (int c = 0; c < 2; ++c) {
     const h4v_t a = __builtin_convertvector(s[2 * c], h4v_t), b = __builtin_convertvector(s[2 * c + 1], h4v_t);
     p[c] = kFp16 ? __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7) : __builtin_shufflevector(a, b, 0, 4, 1, 5, 2, 6, 3, 7);
+    if constexpr (kDot)
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) x.sum = __builtin_amdgcn_fdot2(h2_t{p[c][i], p[c][i + 1]}, h2_t{1, 1}, x.sum, false);
   }
 }
 
 __device__ __forceinline__ f4v_t product(h8v_t a, h8v_t b, f4v_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ h8v_t ones() { return h8v_t{1, 1, 1, 1, 1, 1, 1, 1}; }
 
 // Values of FP16 pages that some rows of a tile must not see: 0 times them has to be 0
 // also where they are infinite or NaN.  Of the keys that no row sees they are cleared;
@@ -456,14 +476,19 @@ __device__ __forceinline__ int count_not_finite(const u4v_t (&v)[2], int seen, i
 
 // Leaves 16 rows of a tile: rounded and divided, or (`part` >= 0, a place of the
 // workspace) as a share's part.
-template <int G>
-__device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, long part, Rows16<G>& x, const Row& r, int head,
+template <int G, bool kDot>
+__device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, long part, Rows16<G, kDot>& x, const Row& r, int head,
                                        int tile_rows, int row_in_tile, int k) {
   constexpr int D = 64 * G;
   const float l = sum_across_rows(x.l);
+  float sum;
+  if constexpr (kDot)
+    sum = sum_across_rows(x.sum);
+  else
+    sum = x.sum[0];
   if (r.limit == -2) return;
   if (part < 0) {
-    const float by = x.sum[0] == 0.0f ? 0.0f : 1.0f / x.sum[0];
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int c = 0; c < 4 * G; ++c)
       *reinterpret_cast<h4v_t*>(a.o + (size_t)r.at * D + 16 * c + 4 * k) = __builtin_convertvector(x.o[c] * by, h4v_t);
@@ -477,7 +502,7 @@ __device__ __forceinline__ void finish(const PagedChunk& a, const ChunkWs& ws, l
   const size_t at = ((size_t)part * a.c.hkv + head) * tile_rows + row_in_tile;
 #pragma unroll
   for (int c = 0; c < 4 * G; ++c) *reinterpret_cast<f4v_t*>(ws.o + at * D + 16 * c + 4 * k) = x.o[c];
-  if (k == 0) ws.ml[at] = make_float4(l == 0.0f ? -INFINITY : x.ref, l, x.sum[0], 0.0f);
+  if (k == 0) ws.ml[at] = make_float4(l == 0.0f ? -INFINITY : x.ref, l, sum, 0.0f);
 }
 // The place of a share's part of its present tile; -1: the whole tile is the share's.
 __device__ __forceinline__ long part_of(const Share& s, int number) {
@@ -504,14 +529,14 @@ __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& 
     const uint8_t* rec = record_of<D, false>(tp, a, head);
     if (j < s.end) load_hif4<G>(k4, rec, lane);
     Row row[NB];
-    Rows16<G> x[NB];
+    Rows16<G, true> x[NB];
     h8v_t q[NB][2 * G];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       row[i] = row_of(a, s.seq, group, head, s.at.tile * kRows + 16 * i + n);
-      load_query<G, false>(q[i], a, row[i], head, k);
       start(x[i]);
     }
+    load_queries<G, false, NB>(q, a, row, head, k);
     const int all_see = s.seq.base + s.at.tile * kRows / group;     // every row of the tile sees the keys up to this one
     while (j < s.end) {
       const int key0 = j * kPage;
@@ -539,7 +564,7 @@ __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& 
       if (j < s.end) load_hif4<G>(k4, rec, lane);
       keep_order();
 #pragma unroll
-      for (int i = 0; i < NB; ++i) soften<G, false>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
+      for (int i = 0; i < NB; ++i) soften<G, false, true>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
       keep_order();
 #pragma unroll
       for (int u = 0; u < 4 * G; ++u)
@@ -549,14 +574,10 @@ __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& 
 #pragma unroll
           for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr, p[i][c], x[i].o[u]);
         }
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
     }
     const long part = part_of(s, number);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) finish<G>(a, ws, part, x[i], row[i], head, kRows, 16 * i + n, k);
+    for (int i = 0; i < NB; ++i) finish(a, ws, part, x[i], row[i], head, kRows, 16 * i + n, k);
   }
 }
 
@@ -634,24 +655,18 @@ struct HifShare {
 // A wave's share of an FP16 page, which is operands as it stands: copied to LDS past
 // the registers.  M0 and the copy that takes its LDS address from it are one statement:
 // the compiler keeps no value of its own in M0.
-template <int kBytes, int kStep>
-struct CopyPieces {
-  static __device__ __forceinline__ void run(uint64_t from, uint32_t to, uint32_t lane_bytes) {
-    if constexpr (kBytes > 0) {
-      CopyPieces<kBytes - kStep, kStep>::run(from, to, lane_bytes);
-      asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1"
-                   :
-                   : "v"(lane_bytes + (kBytes - kStep)), "s"(from), "s"(to), "n"(kBytes - kStep)
-                   : "memory", "m0", "scc");
-    }
-  }
-};
 template <int G, int kWaves>
 __device__ __forceinline__ void copy_share(h8v_t* page, const uint8_t* rec, int wave, int lane) {
   const uint64_t from = (uint64_t)(uintptr_t)(rec + 16384 * G / kWaves * wave);
-  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(page + 1024 * G / kWaves * wave);
-  CopyPieces<16384 * G / kWaves, 1024>::run((uint64_t)(uint32_t)scalar((int)from) | (uint64_t)(uint32_t)scalar((int)(from >> 32)) << 32, (uint32_t)scalar((int)to),
-                                            16 * lane);
+  const uint64_t at = (uint64_t)(uint32_t)scalar((int)from) | (uint64_t)(uint32_t)scalar((int)(from >> 32)) << 32;
+  uint32_t to = (uint32_t)scalar((int)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(page + 1024 * G / kWaves * wave));
+  uint32_t offset = 16 * lane;            // (goes along in one register: eight or more kept for the loop would be spilled)
+#pragma unroll
+  for (int i = 0; i < 16 * G / kWaves; ++i)
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2\n\tv_add_u32 %0, 0x400, %0\n\ts_add_u32 %1, %1, 0x400"
+                 : "+v"(offset), "+s"(to)
+                 : "s"(at)
+                 : "memory", "m0", "scc");
 }
 __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0)
 
@@ -710,14 +725,14 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
     }
     const int row0 = s.at.tile * kRows + wave * kMine;      // the wave's first row
     Row row[NB];
-    Rows16<G> x[NB];
+    Rows16<G, kFp16> x[NB];
     h8v_t q[NB][2 * G];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       row[i] = row_of(a, s.seq, group, head, row0 + 16 * i + n);
-      load_query<G, kFp16>(q[i], a, row[i], head, k);
       start(x[i]);
     }
+    load_queries<G, kFp16, NB>(q, a, row, head, k);
     // keys that every row of the wave sees, and that any of them sees: up to these
     const int first_token = row0 / group, last_token = min(s.seq.n - 1, (row0 + kMine - 1) / group);
     const int all_see = s.seq.base + first_token, some_see = first_token < s.seq.n ? s.seq.base + last_token : -1;
@@ -753,41 +768,47 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
         for (int i = 0; i < NB; ++i)
 #pragma unroll
           for (int t = 0; t < 4; ++t) sc[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-        // Operands come four units ahead of their products: a wave's own products have to
-        // cover LDS's latency, there are two waves a SIMD.
-        h8v_t next4[2][4];
+        // Operands come some units ahead of their products: a wave's own products have to
+        // cover LDS's latency, there are two waves a SIMD (one at D=256, out of registers).
+        constexpr int kAhead = G == 4 ? 2 : 4, kGroups = 8 * G / kAhead;
+        h8v_t next[2][kAhead];
+        const auto k_unit = [&](int e) { return page[64 * (e % 4 * 2 * G + e / 4)]; };
+        const auto v_unit = [&](int e) { return page[64 * (8 * G + e)]; };
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) next4[0][t] = page[64 * (t * 2 * G)];
+        for (int e = 0; e < kAhead; ++e) next[0][e] = k_unit(e);
 #pragma unroll
-        for (int c = 0; c < 2 * G; ++c) {
-          if (c + 1 < 2 * G)
+        for (int g = 0; g < kGroups; ++g) {
+          if (g + 1 < kGroups)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) next4[(c + 1) & 1][t] = page[64 * (t * 2 * G + c + 1)];
+            for (int e = 0; e < kAhead; ++e) next[(g + 1) & 1][e] = k_unit((g + 1) * kAhead + e);
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+          for (int e = 0; e < kAhead; ++e) {
+            const int at_unit = g * kAhead + e, c = at_unit / 4, t = at_unit % 4;
 #pragma unroll
-            for (int i = 0; i < NB; ++i) sc[i][t] = product(next4[c & 1][t], q[i][c], sc[i][t]);
+            for (int i = 0; i < NB; ++i) sc[i][t] = product(next[g & 1][e], q[i][c], sc[i][t]);
+          }
         }
-        __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
 #pragma unroll
-        for (int c = 0; c < 2 * G; ++c) {
-          if (c + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
-          __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
+        for (int g = 0; g < kGroups; ++g) {
+          if (g + 1 < kGroups) __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+          __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead * NB, 0);
         }
         keep_order();
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) next4[0][u] = page[64 * (8 * G + u)];
+        for (int e = 0; e < kAhead; ++e) next[0][e] = v_unit(e);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) soften<G, kFp16>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
+        for (int i = 0; i < NB; ++i) soften<G, kFp16, kFp16>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
         keep_order();
         const bool odd_values = kFp16 && masked;
         __builtin_amdgcn_s_setprio(1);
+        if constexpr (!kFp16)
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
+          for (int i = 0; i < NB; ++i)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) x[i].sum = product(ones(), p[i][c], x[i].sum);
+            for (int c = 0; c < 2; ++c) x[i].sum = product(h8v_t{1, 1, 1, 1, 1, 1, 1, 1}, p[i][c], x[i].sum);
         if (odd_values) {
           bool odd = false;
 #pragma unroll 1
@@ -820,19 +841,21 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
             }
         } else {
 #pragma unroll
-          for (int g = 0; g < 2 * G; ++g) {
-            if (g + 1 < 2 * G)
+          for (int g = 0; g < kGroups; ++g) {
+            if (g + 1 < kGroups)
 #pragma unroll
-              for (int u = 0; u < 4; ++u) next4[(g + 1) & 1][u] = page[64 * (8 * G + 4 * g + 4 + u)];
+              for (int e = 0; e < kAhead; ++e) next[(g + 1) & 1][e] = v_unit((g + 1) * kAhead + e);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int e = 0; e < kAhead; ++e) {
+              const int at_unit = g * kAhead + e, u = at_unit / 2, c = at_unit % 2;
 #pragma unroll
-              for (int i = 0; i < NB; ++i) x[i].o[2 * g + u / 2] = product(next4[g & 1][u], p[i][u & 1], x[i].o[2 * g + u / 2]);
+              for (int i = 0; i < NB; ++i) x[i].o[u] = product(next[g & 1][e], p[i][c], x[i].o[u]);
+            }
           }
 #pragma unroll
-          for (int g = 0; g < 2 * G; ++g) {
-            if (g + 1 < 2 * G) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
-            __builtin_amdgcn_sched_group_barrier(kMatrix, 4 * NB, 0);
+          for (int g = 0; g < kGroups; ++g) {
+            if (g + 1 < kGroups) __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead * NB, 0);
           }
           keep_order();
         }
@@ -857,7 +880,7 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
     }
     const long part = part_of(s, number);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) finish<G>(a, ws, part, x[i], row[i], head, kRows, wave * kMine + 16 * i + n, k);
+    for (int i = 0; i < NB; ++i) finish(a, ws, part, x[i], row[i], head, kRows, wave * kMine + 16 * i + n, k);
   }
 }
 

@@ -64,6 +64,10 @@ __device__ __forceinline__ ChunkSeq seq_of(const PagedChunk& a, int b) {
   const ChunkSeq s = chunk_seq(a, scalar(b));
   return ChunkSeq{scalar(s.first), scalar(s.n), scalar(s.len), scalar(s.base)};
 }
+__device__ __forceinline__ ChunkSeq lane_seq(const ChunkSeq& s, int lane) {
+  return ChunkSeq{__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.len, lane),
+                  __builtin_amdgcn_readlane(s.base, lane)};
+}
 __device__ __forceinline__ int tiles_of(const ChunkSeq& s, int group, const ChunkCut& cut) {
   const int rows = s.n * group;
   return rows > cut.above && rows <= cut.upto ? (rows + cut.rows - 1) / cut.rows : 0;
@@ -74,39 +78,52 @@ __device__ __forceinline__ int tile_pages(const ChunkSeq& s, int group, const Ch
   return max(0, s.base + last + kPage) / kPage;
 }
 // Cost of a sequence's first `tiles` tiles, counted in 1/group of a key: tile t's is
-// tile_cost pages and the keys that it sees, about base + (t + 1) rows / group.
-__device__ __forceinline__ long tiles_cost(const ChunkSeq& s, int group, const ChunkCut& cut, long tiles) {
-  return tiles * group * (kPage * cut.tile_cost + max(0, s.base)) + cut.rows * (tiles * (tiles + 1) / 2);
+// tile_cost pages and the keys that it sees, about base + (t + 1) rows / group.  Whole
+// numbers in fp64; where they are too large for it, every wave still rounds alike.
+__device__ __forceinline__ double tiles_cost(const ChunkSeq& s, int group, const ChunkCut& cut, int tiles) {
+#pragma clang fp contract(off)
+  const double t = tiles;
+  return t * ((double)group * (double)(kPage * cut.tile_cost + max(0, s.base))) + (double)cut.rows * (t * (t + 1.0) * 0.5);
 }
 
 // Sequences are in the order of the lanes that count them: b, b + 64, ..., then b + 1.
 struct ChunkPlan {
-  long before, upto, all;               // cost of the lanes before this one, up to it, of all
+  double before, upto, all;             // cost of the lanes before this one, up to it, of all
 };
 __device__ __forceinline__ int next_sequence(const PagedChunk& a, int b) {
   if (b + 64 < a.c.batch) return b + 64;
   b = (b & 63) + 1;
   return b < 64 && b < a.c.batch ? b : -1;
 }
-__device__ __forceinline__ long wave_last(long x) {
-  return (long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, 63) |
-                (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32);
+template <int kCtrl, int kRowMask, bool kBound>
+__device__ __forceinline__ double add_dpp(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, kCtrl, kRowMask, 0xF, kBound);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), kCtrl, kRowMask, 0xF, kBound);
+  return x + __builtin_bit_cast(double, (uint64_t)lo | (uint64_t)hi << 32);
+}
+__device__ __forceinline__ double lane_value(double x, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane) |
+                                        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane) << 32);
 }
 __device__ __forceinline__ void count_costs(ChunkPlan& p, const PagedChunk& a, const ChunkSeq& first, int group, const ChunkCut& cut, int lane) {
-  long mine = tiles_cost(first, group, cut, tiles_of(first, group, cut));
+#pragma clang fp contract(off)
+  double mine = tiles_cost(first, group, cut, tiles_of(first, group, cut));
   for (int b = lane + 64; b < a.c.batch; b += 64) {
     const ChunkSeq s = chunk_seq(a, b);
     mine += tiles_cost(s, group, cut, tiles_of(s, group, cut));
   }
-  long sum = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long x = __shfl_up(sum, d);
-    if (lane >= d) sum += x;
-  }
+  double sum = mine;
+  sum = add_dpp<0x111, 0xF, true>(sum);      // row_shr 1, 2, 4, 8
+  sum = add_dpp<0x112, 0xF, true>(sum);
+  sum = add_dpp<0x114, 0xF, true>(sum);
+  sum = add_dpp<0x118, 0xF, true>(sum);
+  sum = add_dpp<0x142, 0xA, false>(sum);     // lane 15 of each row to the next
+  sum = add_dpp<0x143, 0xC, false>(sum);
   p.before = sum - mine;
   p.upto = sum;
-  p.all = wave_last(sum);
+  p.all = lane_value(sum, 63);
 }
 
 // A place between two pages of the work: before page `page` of a tile, which is not
@@ -115,33 +132,36 @@ struct Place {
   int b, tile, page;
 };
 __device__ __forceinline__ bool same_tile(const Place& x, const Place& y) { return x.b == y.b && x.tile == y.tile; }
-__device__ __forceinline__ Place place_at(const ChunkPlan& p, const PagedChunk& a, int group, const ChunkCut& cut, long x) {
+// (`first`: lane l's sequence l)
+__device__ __forceinline__ Place place_at(const ChunkPlan& p, const PagedChunk& a, const ChunkSeq& first, int group, const ChunkCut& cut,
+                                          double x) {
+#pragma clang fp contract(off)
   const unsigned long long who = __builtin_amdgcn_ballot_w64(x < p.upto);
   if (!who) return Place{-1, 0, 0};
   const int src = __builtin_ctzll(who);
-  x -= (long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)p.before, src) |
-              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(p.before >> 32), src) << 32);
+  x -= lane_value(p.before, src);
   for (int b = src; b < a.c.batch; b += 64) {
-    const ChunkSeq s = seq_of(a, b);
+    const ChunkSeq s = b < 64 ? lane_seq(first, b) : seq_of(a, b);
     const int tiles = tiles_of(s, group, cut);
-    const long cost = tiles_cost(s, group, cut, tiles);
-    if (x >= cost) {
+    const double cost = tiles_cost(s, group, cut, tiles);
+    if (!(x < cost) && b + 64 < a.c.batch) {
       x -= cost;
       continue;
     }
+    if (tiles == 0) return Place{b, 0, 0};
     int t = 0, behind = tiles;           // the tile with cost(t) <= x < cost(t + 1)
     while (behind - t > 1) {
       const int mid = (t + behind) / 2;
-      if (tiles_cost(s, group, cut, mid) <= x)
+      if (scalar((int)(tiles_cost(s, group, cut, mid) <= x)))
         t = mid;
       else
         behind = mid;
     }
-    const long from = tiles_cost(s, group, cut, t), to = tiles_cost(s, group, cut, t + 1);
+    const double from = tiles_cost(s, group, cut, t), to = tiles_cost(s, group, cut, t + 1);
     const int pages = tile_pages(s, group, cut, t);
-    int page = scalar((int)((double)(x - from) / (double)(to - from) * (double)pages));
-    if (page < cut.whole) page = 0;
-    if (page && pages - page < cut.whole) return Place{b, t + 1, 0};
+    const int page = max(0, min(pages, scalar((int)((x - from) / (to - from) * (double)pages))));
+    if (page < cut.whole) return Place{b, t, 0};
+    if (pages - page < cut.whole) return Place{b, t + 1, 0};
     return Place{b, t, page};
   }
   return Place{-1, 0, 0};
@@ -154,18 +174,20 @@ struct Share {
   int tiles, end;                       // of the sequence; the tile's last page (behind it) in the share
   bool ends;                            // the tile ends in the share
 };
-__device__ __forceinline__ Share share_of(const ChunkPlan& p, const PagedChunk& a, int group, const ChunkCut& cut, int number, int shares) {
+__device__ __forceinline__ Share share_of(const ChunkPlan& p, const PagedChunk& a, const ChunkSeq& first, int group, const ChunkCut& cut,
+                                          int number, int shares) {
+#pragma clang fp contract(off)
   Share s;
   // equal parts: at least `least` pages and a tile's cost
-  const long least = (long)group * kPage * (cut.least + cut.tile_cost);
-  const int parts = scalar((int)max(1L, min((long)min(shares, cut.shares), p.all / least)));
+  const double least = (double)group * (double)(kPage * (cut.least + cut.tile_cost));
+  const int parts = scalar((int)fmax(1.0, fmin((double)min(shares, cut.shares), floor(p.all / least))));
   s.at = s.to = Place{-1, 0, 0};
-  if (number >= parts || p.all == 0) return s;
-  const long each = p.all / parts, rest = p.all % parts;
-  s.at = place_at(p, a, group, cut, each * number + rest * number / parts);
-  if (number + 1 < parts) s.to = place_at(p, a, group, cut, each * (number + 1) + rest * (number + 1) / parts);
+  if (number >= parts || p.all == 0.0) return s;
+  const double each = p.all / (double)parts;
+  s.at = place_at(p, a, first, group, cut, each * (double)number);
+  if (number + 1 < parts) s.to = place_at(p, a, first, group, cut, each * (double)(number + 1));
   if (s.at.b >= 0) {
-    s.seq = seq_of(a, s.at.b);
+    s.seq = s.at.b < 64 ? lane_seq(first, s.at.b) : seq_of(a, s.at.b);
     s.tiles = tiles_of(s.seq, group, cut);
   }
   return s;
@@ -515,12 +537,12 @@ __device__ __forceinline__ long part_of(const Share& s, int number) {
 // record in registers, one 16-byte load a lane for each KiB.  K of the next page is
 // fetched once this one's has been used, V while the scores are made.
 template <int G, int NB>
-__device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, const ChunkPlan& plan, int number,
-                                           int shares, int head, int lane) {
+__device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, const ChunkPlan& plan,
+                                           const ChunkSeq& first, int number, int shares, int head, int lane) {
   constexpr int D = 64 * G, kRows = 16 * NB;
   const int n = lane & 15, k = lane >> 4, group = a.hq / a.c.hkv;
   const ChunkWs ws = chunk_ws(ws_at, a.c, cut);
-  Share s = share_of(plan, a, group, cut, number, shares);
+  Share s = share_of(plan, a, first, group, cut, number, shares);
   if (head == 0 && lane == 0) ws.split[number] = split_of(a, s);
   HifPart<G> k4, v4;
   for (; enter_tile(s, a, group, cut); leave_tile(s)) {
@@ -584,8 +606,9 @@ __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& 
 template <int G, int NB>
 __global__ void __launch_bounds__(64, G == 4 ? 1 : 2) k_chunk_rows(PagedChunk a, ChunkCut cut) {
   ChunkPlan plan;
-  count_costs(plan, a, chunk_seq(a, threadIdx.x), a.hq / a.c.hkv, cut, threadIdx.x);
-  chunk_rows<G, NB>(a, cut, a.ws, plan, blockIdx.x / a.c.hkv, cut.shares, blockIdx.x % a.c.hkv, threadIdx.x);
+  const ChunkSeq first = chunk_seq(a, threadIdx.x);         // the first 64 sequences are read once
+  count_costs(plan, a, first, a.hq / a.c.hkv, cut, threadIdx.x);
+  chunk_rows<G, NB>(a, cut, a.ws, plan, first, blockIdx.x / a.c.hkv, cut.shares, blockIdx.x % a.c.hkv, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -674,9 +697,9 @@ __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F7
 // kinds: by the time that their pages take.  A page of 16 rows on one of a workgroup's
 // waves counts kFewTime of one of 256 rows on all of them.
 constexpr float kFewTime = 0.2f;
-__device__ __forceinline__ int many_shares(long many, long few, int shares) {
-  if (few == 0) return shares;
-  if (many == 0) return 0;
+__device__ __forceinline__ int many_shares(double many, double few, int shares) {
+  if (few == 0.0) return shares;
+  if (many == 0.0) return 0;
   const float m = (float)many, f = kFewTime * (float)few;
   return max(1, min(shares - 1, (int)((float)shares * m / (m + f) + 0.5f)));
 }
@@ -703,12 +726,12 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
     Split* const split = chunk_ws(a.ws + few_ws, a.c, few).split;
     if (number >= shares) {               // the rest of the workgroups: a share a wave
       if (head == 0 && threadIdx.x == 0) ws.split[number] = Split{};
-      chunk_rows<G, 1>(a, few, a.ws + few_ws, other, wave * rest + number - shares, rest * kWaves, head, lane);
+      chunk_rows<G, 1>(a, few, a.ws + few_ws, other, first, wave * rest + number - shares, rest * kWaves, head, lane);
       return;
     }
     if (head == 0 && lane == 0) split[rest * kWaves + number * kWaves + wave] = Split{};
   }
-  Share s = share_of(plan, a, group, cut, number, shares);
+  Share s = share_of(plan, a, first, group, cut, number, shares);
   if (head == 0 && threadIdx.x == 0) ws.split[number] = split_of(a, s);
   HifShare<G, kWaves> share;
   // what is not finite and comes to the lane's sums: [channels / 16][lane][16 rows]
@@ -888,8 +911,9 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(Page
 // Joining the parts of a row that several shares hold: with m the largest of their
 // references, o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in
 // the shares' order.  kFew: a workgroup takes 32 channels of a row, its threads share out
-// the parts (many, where there are few rows); else a wave takes a row.
-constexpr int kChunkJoin = 256;
+// the parts (many, where there are few rows); else a wave takes a row.  A workgroup reads
+// once what the shares have cut and goes through its part of it.
+constexpr int kChunkJoin = 256, kMostShares = 2048;
 
 struct Joined {
   float m, l, sum;
@@ -907,85 +931,101 @@ __device__ __forceinline__ void join_pair(Joined& x, const Joined& y) {
 constexpr int kJoinRows = 16;           // of a workgroup where a wave takes a row
 
 template <int G, bool kFew>
-__device__ __forceinline__ void join_tile(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, int block, Joined* part) {
+__device__ __forceinline__ void join_tiles(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, Joined* part, uint8_t* how,
+                                           short* cuts, int* counts) {
   constexpr int D = 64 * G, kCols = kFew ? 8 : D / 4, kSets = (kFew ? kChunkJoin : 64) / kCols, kAhead = 4;
-  const int lane = threadIdx.x & 63, at_set = kFew ? threadIdx.x : lane, col = at_set % kCols, set = at_set / kCols;
+  const int tid = threadIdx.x, lane = tid & 63, at_set = kFew ? tid : lane, col = at_set % kCols, set = at_set / kCols;
   const ChunkWs ws = chunk_ws(ws_at, a.c, cut);
   const int group = a.hq / a.c.hkv;
-  // workgroups of a share and head: kFew rows times slices of 32 channels, else sets of kJoinRows rows
+  // the shares behind which a tile goes on, in order
+  int found = 0;
+  for (int i0 = 0; i0 < cut.shares; i0 += kChunkJoin) {
+    const int i = i0 + tid, h = i < cut.shares ? ws.split[i].how : 0;
+    if (i < cut.shares) how[i] = (uint8_t)h;
+    const unsigned long long who = __builtin_amdgcn_ballot_w64(h & kCutAfter);
+    if (lane == 0) counts[tid >> 6] = __popcll(who);
+    __syncthreads();
+    int to = found + __popcll(who & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < kChunkJoin / 64; ++w) {
+      if (w < tid >> 6) to += counts[w];
+      found += counts[w];
+    }
+    if (h & kCutAfter) cuts[to] = (short)i;
+    __syncthreads();
+  }
+  // of such a share and a head: kFew rows times slices of 32 channels, else sets of kJoinRows rows
   const int per = kFew ? cut.rows * (D / 32) : cut.rows / kJoinRows;
-  const int first = block / per / a.c.hkv, head = block / per % a.c.hkv;
-  const Split sp = ws.split[first];
-  if (!(sp.how & kCutAfter)) return;
-  // the shares that lie within the tile, then the one that it ends in
-  int parts = 2;
-  for (int from = first + 1; from < cut.shares; from += 64) {
-    const bool goes_on = from + lane < cut.shares && (ws.split[from + lane].how & kWithin);
-    const unsigned long long stops = ~__builtin_amdgcn_ballot_w64(goes_on);
-    parts += stops ? __builtin_ctzll(stops) : 64;
-    if (stops) break;
-  }
-  const int ch = (kFew ? block % per % (D / 32) * 32 : 0) + 4 * col;
-#pragma unroll
-  for (int r = 0; r < (kFew ? 1 : kJoinRows / 4); ++r) {
-    const int row_in_tile = kFew ? block % per / (D / 32) : block % per * kJoinRows + 4 * r + (int)(threadIdx.x >> 6);
-    const Row row = row_of(a, sp.seq, group, head, sp.tile * cut.rows + row_in_tile);
-    if (row.limit == -2) continue;
-    Joined x = {-INFINITY, 0.0f, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int i = set; i < parts; i += kAhead * kSets) {
-      float4 ml[kAhead];
-      f4v_t y[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int share = first + min(i + u * kSets, parts - 1);
-        const size_t from = (((size_t)2 * share + (share == first)) * a.c.hkv + head) * cut.rows + row_in_tile;
-        ml[u] = ws.ml[from];
-        y[u] = *reinterpret_cast<const f4v_t*>(ws.o + from * D + ch);
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (i + u * kSets < parts) join_pair(x, Joined{ml[u].x, ml[u].y, ml[u].z, y[u]});
+  for (int block = blockIdx.x; block < found * a.c.hkv * per; block += gridDim.x) {
+    const int first = cuts[block / per / a.c.hkv], head = block / per % a.c.hkv;
+    const Split sp = ws.split[first];
+    int parts = 2;                       // the shares that lie within the tile, then the one that it ends in
+    for (int from = first + 1; from < cut.shares; from += 64) {
+      const bool goes_on = from + lane < cut.shares && (how[from + lane] & kWithin);
+      const unsigned long long stops = ~__builtin_amdgcn_ballot_w64(goes_on);
+      parts += stops ? __builtin_ctzll(stops) : 64;
+      if (stops) break;
     }
-    if constexpr (kFew) {
-      part[threadIdx.x] = x;
-      __syncthreads();
-      if (set == 0) {
+    const int ch = (kFew ? block % per % (D / 32) * 32 : 0) + 4 * col;
+#pragma unroll
+    for (int r = 0; r < (kFew ? 1 : kJoinRows / 4); ++r) {
+      const int row_in_tile = kFew ? block % per / (D / 32) : block % per * kJoinRows + 4 * r + (int)(threadIdx.x >> 6);
+      const Row row = row_of(a, sp.seq, group, head, sp.tile * cut.rows + row_in_tile);
+      if (row.limit == -2) continue;
+      Joined x = {-INFINITY, 0.0f, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+      for (int i = set; i < parts; i += kAhead * kSets) {
+        float4 ml[kAhead];
+        f4v_t y[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int share = first + min(i + u * kSets, parts - 1);
+          const size_t from = (((size_t)2 * share + (share == first)) * a.c.hkv + head) * cut.rows + row_in_tile;
+          ml[u] = ws.ml[from];
+          y[u] = *reinterpret_cast<const f4v_t*>(ws.o + from * D + ch);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (i + u * kSets < parts) join_pair(x, Joined{ml[u].x, ml[u].y, ml[u].z, y[u]});
+      }
+      if constexpr (kFew) {
+        part[threadIdx.x] = x;
+        __syncthreads();
+        if (set == 0) {
 #pragma unroll 4
-        for (int i = 1; i < kSets; ++i) join_pair(x, part[i * kCols + col]);
-      }
-      __syncthreads();
-    } else {
+          for (int i = 1; i < kSets; ++i) join_pair(x, part[i * kCols + col]);
+        }
+        __syncthreads();
+      } else {
 #pragma unroll
-      for (int d = kCols; d < 64; d <<= 1) {
-        Joined y;
-        y.m = __shfl_xor(x.m, d);
-        y.l = __shfl_xor(x.l, d);
-        y.sum = __shfl_xor(x.sum, d);
+        for (int d = kCols; d < 64; d <<= 1) {
+          Joined y;
+          y.m = __shfl_xor(x.m, d);
+          y.l = __shfl_xor(x.l, d);
+          y.sum = __shfl_xor(x.sum, d);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) y.o[v] = __shfl_xor(x.o[v], d);
-        join_pair(x, y);
+          for (int v = 0; v < 4; ++v) y.o[v] = __shfl_xor(x.o[v], d);
+          join_pair(x, y);
+        }
       }
-    }
-    if (set) continue;
-    *reinterpret_cast<h4v_t*>(a.o + (size_t)row.at * D + ch) = __builtin_convertvector(x.o * (x.sum == 0.0f ? 0.0f : 1.0f / x.sum), h4v_t);
-    if (ch == 0) {
-      const int token = row.at / a.hq;
-      a.lse[(size_t)(row.at - token * a.hq) * a.total + token] =
-          x.l == 0.0f ? -INFINITY : (float)(((double)x.m + (double)__log2f(x.l)) * 0.6931471805599453);
+      if (set) continue;
+      *reinterpret_cast<h4v_t*>(a.o + (size_t)row.at * D + ch) = __builtin_convertvector(x.o * (x.sum == 0.0f ? 0.0f : 1.0f / x.sum), h4v_t);
+      if (ch == 0) {
+        const int token = row.at / a.hq;
+        a.lse[(size_t)(row.at - token * a.hq) * a.total + token] =
+            x.l == 0.0f ? -INFINITY : (float)(((double)x.m + (double)__log2f(x.l)) * 0.6931471805599453);
+      }
     }
   }
-}
-__host__ __device__ __forceinline__ size_t join_blocks(const PagedCache& c, const ChunkCut& cut, bool few) {
-  return cut.shares < 2 ? 0 : (size_t)cut.shares * c.hkv * (few ? cut.rows * (c.D / 32) : cut.rows / kJoinRows);
 }
 template <int G, bool kFew>
 __global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCut cut, ChunkCut few, size_t few_ws) {
   __shared__ Joined part[kFew ? kChunkJoin : 1];
-  const int many = (int)join_blocks(a.c, cut, kFew), block = blockIdx.x;
-  if (block < many)
-    join_tile<G, kFew>(a, cut, a.ws, block, part);
-  else
-    join_tile<G, kFew>(a, few, a.ws + few_ws, block - many, part);
+  __shared__ uint8_t how[kMostShares];
+  __shared__ short cuts[kMostShares];
+  __shared__ int counts[kChunkJoin / 64];
+  if (cut.shares > 1) join_tiles<G, kFew>(a, cut, a.ws, part, how, cuts, counts);
+  __syncthreads();
+  if (few.shares > 1) join_tiles<G, kFew>(a, few, a.ws + few_ws, part, how, cuts, counts);
 }
 
 // ---------------------------------------------------------------------------
@@ -1034,7 +1074,7 @@ static bool chunk_cuts(const PagedCache& c, int hq, int total, int max_new, Chun
   x->blocks = (size_t)(x->many.shares ? x->many.shares : x->few.shares) * c.hkv;
   x->joined = ((size_t)(x->many.shares > 1 ? x->many.shares : 0) * x->many.rows +
                (size_t)(x->few.shares > 1 ? x->few.shares : 0) * x->few.rows) * c.hkv;
-  return x->blocks < max_grid(64 * x->waves) && x->joined < (size_t)1 << 26;
+  return std::max(x->many.shares, x->few.shares) <= kMostShares && x->blocks < max_grid(64 * x->waves) && x->joined < (size_t)1 << 26;
 }
 
 bool paged_chunk_fits(const PagedCache& c, int hq, int total, int max_new) {
@@ -1074,12 +1114,10 @@ static hipError_t launch_chunk(const PagedChunk& a, const ChunkCuts& x, hipStrea
     e = hipGetLastError();
   }
   if (e != hipSuccess || x.joined == 0) return e;
-  const bool few = x.joined <= 2048;
-  const dim3 grid((unsigned)(join_blocks(a.c, x.many, few) + join_blocks(a.c, x.few, few)));
-  if (few)
-    k_chunk_join<G, true><<<grid, kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
+  if (x.joined <= 2048)
+    k_chunk_join<G, true><<<dim3((unsigned)(x.joined * (2 * G))), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   else
-    k_chunk_join<G, false><<<grid, kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
+    k_chunk_join<G, false><<<dim3(1024), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   return hipGetLastError();
 }
 

@@ -928,7 +928,7 @@ __device__ __forceinline__ void join_pair(Joined& x, const Joined& y) {
   x.o = x.o * f + y.o * g;
 }
 
-constexpr int kJoinRows = 16;           // of a workgroup where a wave takes a row
+constexpr int kJoinRows = 4;           // of a workgroup where a wave takes a row
 
 template <int G, bool kFew>
 __device__ __forceinline__ void join_tiles(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, Joined* part, uint8_t* how,
@@ -1117,7 +1117,7 @@ static hipError_t launch_chunk(const PagedChunk& a, const ChunkCuts& x, hipStrea
   if (x.joined <= 2048)
     k_chunk_join<G, true><<<dim3((unsigned)(x.joined * (2 * G))), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   else
-    k_chunk_join<G, false><<<dim3(1024), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
+    k_chunk_join<G, false><<<dim3(2048), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   return hipGetLastError();
 }
 

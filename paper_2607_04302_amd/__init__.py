@@ -516,6 +516,13 @@ def _shaped(t, dtype, shape, device, name):
         raise ValueError(f"{name} must be on {device}, got {t.device}")
 
 
+def _row(t, dtype, n, device, name):
+    """_shaped for one dimension of n."""
+    if t.numel() == n and t.dtype is dtype and t.dim() == 1 and t.get_device() == device.index and t.is_contiguous():
+        return
+    _shaped(t, dtype, (n,), device, name)
+
+
 def _count(x, name):
     """`x` where a 32-bit count goes (ctypes would cut a larger one without a word)."""
     if not -2 ** 31 <= x < 2 ** 31:
@@ -525,8 +532,8 @@ def _count(x, name):
 
 def _paged_call(name, device, *args):
     """Calls an entry point of the library with `device` current."""
-    fn = getattr(load_library(), name)
-    cuda = _torch()._C
+    fn = getattr(_lib or load_library(), name)
+    cuda = _torch_module._C
     back = cuda._cuda_getDevice()
     if back == device.index:
         status = fn(*args)
@@ -818,43 +825,41 @@ def hifa4_paged_extend(block_table, seq_lens, counts, free_pages, num_free, max_
     if free_pages.dim() != 1:
         raise ValueError("free_pages is [capacity]")
     i32 = torch.int32
-    shape = block_table.shape
-    rows, one = shape[:1], (1,)
-    total = (_count(max_total, "max_total"),)
-    max_new = max_total if max_new is None else _count(max_new, "max_new")
-    if max_total < 0:
+    batch, max_pages = shape = block_table.shape
+    capacity = _count(free_pages.shape[0], "the free pages")
+    if _count(max_total, "max_total") < 0:
         raise ValueError("max_total must be >= 0")
+    max_new = max_total if max_new is None else _count(max_new, "max_new")
     _shaped(block_table, i32, shape, dev, "block_table")
-    _shaped(seq_lens, i32, rows, dev, "seq_lens")
-    _shaped(counts, i32, rows, dev, "counts")
-    _shaped(free_pages, i32, free_pages.shape, dev, "free_pages")
-    _shaped(num_free, i32, one, dev, "num_free")
+    _row(seq_lens, i32, batch, dev, "seq_lens")
+    _row(counts, i32, batch, dev, "counts")
+    _row(free_pages, i32, capacity, dev, "free_pages")
+    _row(num_free, i32, 1, dev, "num_free")
     if shift is not None:
-        _shaped(shift, i32, rows, dev, "shift")
+        _row(shift, i32, batch, dev, "shift")
     if out_lens is None:
         out_lens = seq_lens
     else:
-        _shaped(out_lens, i32, rows, dev, "out_lens")
+        _row(out_lens, i32, batch, dev, "out_lens")
     if out_free is None:
         out_free = num_free
     else:
-        _shaped(out_free, i32, one, dev, "out_free")
+        _row(out_free, i32, 1, dev, "out_free")
     if cu_new is None:
-        cu_new = torch.empty(shape[0] + 1, dtype=i32, device=dev)
+        cu_new = torch.empty(batch + 1, dtype=i32, device=dev)
     else:
-        _shaped(cu_new, i32, (shape[0] + 1,), dev, "cu_new")
+        _row(cu_new, i32, batch + 1, dev, "cu_new")
     if positions is None:
-        positions = torch.empty(total, dtype=i32, device=dev)
+        positions = torch.empty(max_total, dtype=i32, device=dev)
     else:
-        _shaped(positions, i32, total, dev, "positions")
+        _row(positions, i32, max_total, dev, "positions")
     if slots is None:
-        slots = torch.empty(total, dtype=torch.int64, device=dev)
+        slots = torch.empty(max_total, dtype=torch.int64, device=dev)
     else:
-        _shaped(slots, torch.int64, total, dev, "slots")
-    _paged_call("hifa4_paged_extend", dev, shape[0], shape[1], block_table.data_ptr(), seq_lens.data_ptr(), counts.data_ptr(),
-                free_pages.data_ptr(), _count(free_pages.shape[0], "the free pages"), num_free.data_ptr(), _ptr(shift), max_total,
-                max_new, out_lens.data_ptr(), out_free.data_ptr(), cu_new.data_ptr(), positions.data_ptr(), slots.data_ptr(),
-                _stream(dev))
+        _row(slots, torch.int64, max_total, dev, "slots")
+    _paged_call("hifa4_paged_extend", dev, batch, max_pages, block_table.data_ptr(), seq_lens.data_ptr(), counts.data_ptr(),
+                free_pages.data_ptr(), capacity, num_free.data_ptr(), None if shift is None else shift.data_ptr(), max_total, max_new,
+                out_lens.data_ptr(), out_free.data_ptr(), cu_new.data_ptr(), positions.data_ptr(), slots.data_ptr(), _stream(dev))
     return cu_new, positions, slots
 
 
@@ -870,24 +875,23 @@ def hifa4_paged_release(table, to, free_pages, num_free, first=None, out_free=No
     if free_pages.dim() != 1:
         raise ValueError("free_pages is [capacity]")
     i32 = torch.int32
-    shape = table.shape
-    rows, one = shape[:1], (1,)
+    batch, max_pages = shape = table.shape
+    capacity = _count(free_pages.shape[0], "the free pages")
     _shaped(table, i32, shape, dev, "table")
-    _shaped(to, i32, rows, dev, "to")
+    _row(to, i32, batch, dev, "to")
     if first is not None:
-        _shaped(first, i32, rows, dev, "first")
-    _shaped(free_pages, i32, free_pages.shape, dev, "free_pages")
-    _shaped(num_free, i32, one, dev, "num_free")
+        _row(first, i32, batch, dev, "first")
+    _row(free_pages, i32, capacity, dev, "free_pages")
+    _row(num_free, i32, 1, dev, "num_free")
     if out_free is None:
         out_free = num_free
     else:
-        _shaped(out_free, i32, one, dev, "out_free")
-    need = 4 * (shape[0] + 1)
+        _row(out_free, i32, 1, dev, "out_free")
+    need = 4 * (batch + 1)
     stream = _stream(dev)
     ws = _scratch(need, dev, stream) if workspace is None else workspace.get(need, dev)
-    _paged_call("hifa4_paged_release", dev, shape[0], shape[1], table.data_ptr(), _ptr(first), to.data_ptr(),
-                free_pages.data_ptr(), _count(free_pages.shape[0], "the free pages"), num_free.data_ptr(), out_free.data_ptr(),
-                ws.data_ptr(), ws.numel(), stream)
+    _paged_call("hifa4_paged_release", dev, batch, max_pages, table.data_ptr(), None if first is None else first.data_ptr(), to.data_ptr(),
+                free_pages.data_ptr(), capacity, num_free.data_ptr(), out_free.data_ptr(), ws.data_ptr(), ws.numel(), stream)
     return out_free
 
 
@@ -927,6 +931,7 @@ class Rope:
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
         self.device = self.turns.device
         self.head_dim, self.rot_dim, self.interleaved, self.magnitude = head_dim, rot_dim, bool(interleaved), float(magnitude)
+        self._interleaved, self._turns = int(self.interleaved), self.turns.data_ptr()
 
 
 def _rope_rows(t, tokens, head_dim, device, name):
@@ -934,19 +939,37 @@ def _rope_rows(t, tokens, head_dim, device, name):
     torch = _torch()
     if t is None:
         return 0, None, 0
+    if t.dim() == 3 and t.dtype is torch.float16 and t.get_device() == device.index:
+        rows, heads, d = t.shape
+        if rows == tokens and d == head_dim:
+            a, b, c = t.stride()
+            if tokens <= 1:
+                a = max(a, heads * d)
+            if c == 1 and (b == d or heads <= 1) or not tokens:
+                return _count(heads, "heads"), t.data_ptr(), a
+            raise ValueError(f"{name}: a token's heads must be contiguous")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype is not torch.float16:
         raise ValueError(f"{name} must be {torch.float16}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}, got {t.device}")
-    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != head_dim:
-        raise ValueError(f"{name} must be [{tokens}, heads, {head_dim}], got {list(t.shape)}")
-    heads = t.shape[1]
-    a, b, c = t.stride()
-    if tokens and (c != 1 or (heads > 1 and b != head_dim)):
-        raise ValueError(f"{name}: a token's heads must be contiguous")
-    return _count(heads, "heads"), t.data_ptr(), max(a, heads * head_dim) if tokens <= 1 else a
+    raise ValueError(f"{name} must be [{tokens}, heads, {head_dim}], got {list(t.shape)}")
+
+
+def _rope_out(x, y, heads, tokens, head_dim, device, name):
+    """The output for x (y, or a new tensor): (it, pointer, elements from token to token)."""
+    if x is None:
+        if y is not None:
+            raise ValueError(f"{name}_out needs a {name} of its shape")
+        return None, None, 0
+    if y is None:
+        y = _torch().empty((tokens, heads, head_dim), dtype=x.dtype, device=device)
+        return y, y.data_ptr(), heads * head_dim
+    if y.shape != x.shape:
+        raise ValueError(f"{name}_out needs a {name} of its shape")
+    _, at, stride = _rope_rows(y, tokens, head_dim, device, name + "_out")
+    return y, at, stride
 
 
 def hifa4_rope(rope: Rope, positions, q=None, k=None, q_out=None, k_out=None, transposed: bool = False):
@@ -961,21 +984,14 @@ def hifa4_rope(rope: Rope, positions, q=None, k=None, q_out=None, k_out=None, tr
     if positions.dim() != 1:
         raise ValueError("positions is [tokens]")
     tokens = _count(positions.shape[0], "the tokens")
-    _shaped(positions, torch.int32, (tokens,), dev, "positions")
+    _row(positions, torch.int32, tokens, dev, "positions")
     d = rope.head_dim
     hq, qp, qs = _rope_rows(q, tokens, d, dev, "q")
     hk, kp, ks = _rope_rows(k, tokens, d, dev, "k")
-    for x, y, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if y is not None and (x is None or x.shape != y.shape):
-            raise ValueError(f"{name}_out needs a {name} of its shape")
-    if q is not None and q_out is None:
-        q_out = torch.empty((tokens, hq, d), dtype=torch.float16, device=dev)
-    if k is not None and k_out is None:
-        k_out = torch.empty((tokens, hk, d), dtype=torch.float16, device=dev)
-    _, qo, qos = _rope_rows(q_out, tokens, d, dev, "q_out")
-    _, ko, kos = _rope_rows(k_out, tokens, d, dev, "k_out")
-    _paged_call("hifa4_rope", dev, d, rope.rot_dim, int(rope.interleaved), int(bool(transposed)), rope.magnitude,
-                rope.turns.data_ptr(), tokens, positions.data_ptr(), hq, qp, qs, qo, qos, hk, kp, ks, ko, kos, _stream(dev))
+    q_out, qo, qos = _rope_out(q, q_out, hq, tokens, d, dev, "q")
+    k_out, ko, kos = _rope_out(k, k_out, hk, tokens, d, dev, "k")
+    _paged_call("hifa4_rope", dev, d, rope.rot_dim, rope._interleaved, 1 if transposed else 0, rope.magnitude, rope._turns, tokens,
+                positions.data_ptr(), hq, qp, qs, qo, qos, hk, kp, ks, ko, kos, _stream(dev))
     return q_out, k_out
 
 

@@ -696,7 +696,7 @@ __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F7
 // How many of a head's workgroups take the sequences of many rows where there are both
 // kinds: by the time that their pages take.  A page of 16 rows on one of a workgroup's
 // waves counts kFewTime of one of 256 rows on all of them.
-constexpr float kFewTime = 0.2f;
+constexpr float kFewTime = 0.22f;
 __device__ __forceinline__ int many_shares(double many, double few, int shares) {
   if (few == 0.0) return shares;
   if (many == 0.0) return 0;
@@ -1055,7 +1055,7 @@ static bool chunk_cuts(const PagedCache& c, int hq, int total, int max_new, Chun
   const bool wide = most > kFewRows, both = wide && !c.fp16;
   x->waves = wide ? wide_waves(c.D) : 1;
   const size_t per_head = std::max<size_t>(both ? 2 : 1, resident(c.D, c.fp16, x->waves) / c.hkv);
-  x->many = ChunkCut{wide ? 32 * x->waves : most <= 16 ? 16 : 32, c.fp16 ? 0 : kFewRows, 1 << 30, 0, wide ? 3 : 1, wide ? 4 : 2, wide ? 6 : 1};
+  x->many = ChunkCut{wide ? 32 * x->waves : most <= 16 ? 16 : 32, c.fp16 ? 0 : kFewRows, 1 << 30, 0, wide ? 4 : 1, wide ? 4 : 2, wide ? 10 : 1};
   x->few = ChunkCut{!wide && most > 16 && c.D != 256 ? 32 : 16, 0, kFewRows, 0, 1, 2, 1};
   const auto tiles = [&](const ChunkCut& cut, size_t seqs, size_t rows) {
     return std::min(seqs * ((rows + cut.rows - 1) / cut.rows), all / cut.rows + seqs);

@@ -27,14 +27,21 @@ __device__ __forceinline__ int extend_asked(const PagedExtend& a, int b, int len
 }
 __device__ __forceinline__ int pages_in(int tokens) { return (tokens + kPage - 1) / kPage; }
 
-// One new token of row b: i-th of the row, t-th of all, `len` tokens before them;
-// the row's first new page is the one below stack place `top`.
-__device__ __forceinline__ void place_token(const PagedExtend& a, int b, int len, int i, int t, int top) {
-  const int at = len + i, place = at / kPage, have = pages_in(len);
-  int* entry = a.table + (size_t)b * a.max_pages + place;
-  const int page = place < have ? *entry : a.free[top - 1 - (place - have)];
-  if (place >= have && (i == 0 || at % kPage == 0)) *entry = page;
-  a.positions[t] = at + (a.shift ? a.shift[b] : 0);
+// New tokens of row b, `len` tokens before them; the row's first new page is the one
+// below stack place `top`.
+struct RowPlan {
+  int b, len, top;
+};
+// Page of the row's i-th new token.
+__device__ __forceinline__ int page_of(const PagedExtend& a, const RowPlan& r, int i) {
+  const int place = (r.len + i) / kPage, have = pages_in(r.len);
+  return place < have ? a.table[(size_t)r.b * a.max_pages + place] : a.free[r.top - 1 - (place - have)];
+}
+// The token, t-th of all, is put down; the first of a new page puts down the page.
+__device__ __forceinline__ void place_token(const PagedExtend& a, const RowPlan& r, int i, int t, int page, int shift) {
+  const int at = r.len + i, place = at / kPage;
+  if (place >= pages_in(r.len) && (i == 0 || at % kPage == 0)) a.table[(size_t)r.b * a.max_pages + place] = page;
+  a.positions[t] = at + shift;
   a.slots[t] = page < 0 ? -1 : (int64_t)page * kPage + at % kPage;
 }
 
@@ -43,17 +50,23 @@ __device__ __forceinline__ void place_token(const PagedExtend& a, int b, int len
 struct Sums {
   long tokens, pages;
 };
+template <int kCtrl, int kRowMask, bool kBound>
+__device__ __forceinline__ long add_dpp(long x) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, kCtrl, kRowMask, 0xF, kBound);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), kCtrl, kRowMask, 0xF, kBound);
+  return x + (long)((uint64_t)lo | (uint64_t)hi << 32);
+}
+__device__ __forceinline__ long wave_scan(long x) {
+  x = add_dpp<0x111, 0xF, true>(x);      // row_shr 1, 2, 4, 8
+  x = add_dpp<0x112, 0xF, true>(x);
+  x = add_dpp<0x114, 0xF, true>(x);
+  x = add_dpp<0x118, 0xF, true>(x);
+  x = add_dpp<0x142, 0xA, false>(x);     // lane 15 of each row to the next
+  return add_dpp<0x143, 0xC, false>(x);
+}
 __device__ __forceinline__ Sums scan_sums(Sums x, Sums* waves, Sums& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Sums s = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long t = __shfl_up(s.tokens, d), p = __shfl_up(s.pages, d);
-    if (lane >= d) {
-      s.tokens += t;
-      s.pages += p;
-    }
-  }
+  const Sums s = {wave_scan(x.tokens), wave_scan(x.pages)};
   if (lane == 63) waves[wave] = s;
   __syncthreads();
   all = Sums{0, 0};
@@ -83,7 +96,7 @@ __global__ void __launch_bounds__(kExtendThreads) k_paged_extend(PagedExtend a) 
   Sums upto = {0, 0};                    // asked for by the rows before
   long given = 0;
   int taken = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kExtendThreads) {
+  for (int b0 = 0; b0 < a.batch; b0 += blockDim.x) {
     const int b = b0 + tid;
     const bool there = b < a.batch;
     const int len = there ? extend_len(a, b) : 0, asked = there ? extend_asked(a, b, len) : 0;
@@ -93,8 +106,8 @@ __global__ void __launch_bounds__(kExtendThreads) k_paged_extend(PagedExtend a) 
     const bool fits = upto.tokens + before.tokens + asked <= a.max_total &&
                       (need == 0 || upto.pages + before.pages + need <= top);
     const int n = fits ? asked : 0, pages = fits ? need : 0;
-    Sums got;
-    const Sums mine = scan_sums(Sums{n, pages}, waves, got);
+    Sums got = all, mine = before;
+    if (upto.tokens + all.tokens > a.max_total || upto.pages + all.pages > top) mine = scan_sums(Sums{n, pages}, waves, got);
     const int t0 = (int)(given + mine.tokens), stack = top - taken - (int)mine.pages;
     if (there) {
       a.cu[b] = t0;
@@ -117,7 +130,7 @@ __global__ void __launch_bounds__(kExtendThreads) k_paged_extend(PagedExtend a) 
   if (!kAlone) return;
   if (tid == 0) first[a.batch] = (int)given;
   __syncthreads();
-  for (int t = tid; t < a.max_total; t += kExtendThreads) {
+  for (int t = tid; t < a.max_total; t += blockDim.x) {
     if (t >= (int)given) {
       a.positions[t] = -1;
       a.slots[t] = -1;
@@ -131,7 +144,8 @@ __global__ void __launch_bounds__(kExtendThreads) k_paged_extend(PagedExtend a) 
       else
         behind = mid;
     }
-    place_token(a, b, lens[b], t - first[b], t, stacks[b]);
+    const RowPlan r = {b, lens[b], stacks[b]};
+    place_token(a, r, t - first[b], t, page_of(a, r, t - first[b]), a.shift ? a.shift[b] : 0);
   }
 }
 
@@ -139,20 +153,21 @@ __global__ void __launch_bounds__(kExtendThreads) k_paged_extend(PagedExtend a) 
 __global__ void __launch_bounds__(kFillThreads) k_paged_extend_fill(PagedExtend a, int chunks) {
   __shared__ int sums[2][kFillThreads / 64];
   const int b = blockIdx.x / chunks, i0 = blockIdx.x % chunks * kFillTokens, tid = threadIdx.x;
-  const int total = a.cu[a.batch];
-  for (int t = total + blockIdx.x * kFillThreads + tid; t < a.max_total; t += gridDim.x * kFillThreads) {
-    a.positions[t] = -1;
-    a.slots[t] = -1;
-  }
-  const int t0 = a.cu[b], n = a.cu[b + 1] - t0;
-  if (i0 >= n) return;
-  // pages that the rows before this one took, and all rows: what is left says where the stack began
+  // (all loads that hang on nothing first)
+  const int total = a.cu[a.batch], t0 = a.cu[b], n = a.cu[b + 1] - t0, has = a.out_lens[b], left = a.out_free[0];
+  const int shift = a.shift ? a.shift[b] : 0;
   int before = 0, all = 0;
   for (int r = tid; r < a.batch; r += kFillThreads) {
     const int len = a.out_lens[r], pages = pages_in(len) - pages_in(len - (a.cu[r + 1] - a.cu[r]));
     all += pages;
     if (r < b) before += pages;
   }
+  for (int t = total + blockIdx.x * kFillThreads + tid; t < a.max_total; t += gridDim.x * kFillThreads) {
+    a.positions[t] = -1;
+    a.slots[t] = -1;
+  }
+  if (i0 >= n) return;
+  // pages that the rows before this one took, and all rows: what is left says where the stack began
   before = wave_scan(before);
   all = wave_scan(all);
   if ((tid & 63) == 63) {
@@ -166,14 +181,27 @@ __global__ void __launch_bounds__(kFillThreads) k_paged_extend_fill(PagedExtend 
     before += sums[0][w];
     all += sums[1][w];
   }
-  const int len = a.out_lens[b] - n, stack = a.out_free[0] + all - before;
+  const RowPlan row = {b, has - n, left + all - before};
   const int end = min(n, i0 + kFillTokens);
-  for (int i = i0 + tid; i < end; i += kFillThreads) place_token(a, b, len, i, t0 + i, stack);
+  constexpr int kMine = kFillTokens / kFillThreads;
+  int page[kMine];
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) {
+    const int i = i0 + tid + u * kFillThreads;
+    page[u] = i < end ? page_of(a, row, i) : 0;
+  }
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) {
+    const int i = i0 + tid + u * kFillThreads;
+    if (i < end) place_token(a, row, i, t0 + i, page[u], shift);
+  }
 }
 
 hipError_t launch_paged_extend(const PagedExtend& a, hipStream_t st) {
   if (a.max_total <= kExtendAlone && a.batch <= kExtendThreads) {
-    k_paged_extend<true><<<dim3(1), kExtendThreads, 0, st>>>(a);
+    // a thread for each row and, up to a point, for each token: fewer waves meet sooner
+    const int threads = std::max(a.batch, std::min(a.max_total, kExtendThreads));
+    k_paged_extend<true><<<dim3(1), (threads + 63) / 64 * 64, 0, st>>>(a);
     return hipGetLastError();
   }
   k_paged_extend<false><<<dim3(1), kExtendThreads, 0, st>>>(a);
@@ -254,7 +282,47 @@ __global__ void __launch_bounds__(kReleaseThreads) k_paged_release(PagedRelease 
   if (b == 0 && tid == 0) a.out_free[0] = (int)min((long)a.capacity, (long)top + all);
 }
 
+// Few places in all: one workgroup reads them once, the entries in registers.
+constexpr int kReleaseFew = 4096, kFewThreads = 1024, kFewHeld = kReleaseFew / kFewThreads;
+
+__global__ void __launch_bounds__(kFewThreads) k_paged_release_few(PagedRelease a) {
+  constexpr int kWaves = kFewThreads / 64;
+  __shared__ int counts[kFewHeld * kWaves];
+  static_assert(kFewHeld * kWaves == 64, "a count a lane");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, places = a.batch * a.max_pages;
+  const int top = max(0, min(a.num_free[0], a.capacity));
+  int page[kFewHeld];
+  unsigned long long who[kFewHeld];
+#pragma unroll
+  for (int u = 0; u < kFewHeld; ++u) {
+    const int i = u * kFewThreads + tid, b = i / a.max_pages, place = i - b * a.max_pages;
+    page[u] = -1;
+    if (i < places) {
+      const int2 r = released(a, b);
+      const int x = a.table[i];
+      if (place >= r.x && place < r.y) page[u] = x;
+    }
+    who[u] = __builtin_amdgcn_ballot_w64(page[u] >= 0);
+    if (lane == 0) counts[u * kWaves + wave] = __popcll(who[u]);
+  }
+  __syncthreads();
+  const int mine = counts[lane], upto = wave_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+#pragma unroll
+  for (int u = 0; u < kFewHeld; ++u) {
+    const int rank = __builtin_amdgcn_readlane(upto - mine, u * kWaves + __builtin_amdgcn_readfirstlane(wave)) +
+                     __popcll(who[u] & ((1ull << lane) - 1));
+    const long to = (long)top + all - 1 - rank;
+    if (page[u] >= 0 && to < a.capacity) a.free[to] = page[u];
+  }
+  __syncthreads();
+  if (tid == 0) a.out_free[0] = (int)min((long)a.capacity, (long)top + all);
+}
+
 hipError_t launch_paged_release(const PagedRelease& a, hipStream_t st) {
+  if ((long)a.batch * a.max_pages <= kReleaseFew) {
+    k_paged_release_few<<<dim3(1), kFewThreads, 0, st>>>(a);
+    return hipGetLastError();
+  }
   k_paged_release_count<<<dim3((unsigned)a.batch), kReleaseThreads, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

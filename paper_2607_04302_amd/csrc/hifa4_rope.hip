@@ -58,32 +58,51 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int units, int slices)
       w[i].y *= a.transposed ? -a.magnitude : a.magnitude;
     }
   }
-  for (int h = slice * per + lane / units; h < heads; h += slices * per) {
+  const auto head_rows = [&](int h, const half_t*& x, half_t*& y) {
     const bool is_q = h < a.q.heads;
     const RopeRows& r = is_q ? a.q : a.k;
     const int head = is_q ? h : h - a.q.heads;
-    const half_t* x = r.x + token * r.x_stride + (long)head * a.D;
-    half_t* y = r.y + token * r.y_stride + (long)head * a.D;
-    const vec_t x0 = *reinterpret_cast<const vec_t*>(x + at0), x1 = *reinterpret_cast<const vec_t*>(x + at1);
-    vec_t y0 = x0, y1 = x1;
-    if (rotates) {
+    x = r.x + token * r.x_stride + (long)head * a.D;
+    y = r.y + token * r.y_stride + (long)head * a.D;
+  };
+  // kHeads of the lane's heads at a time, all fetched before the first is used
+  constexpr int kHeads = 4;
+  const int step = slices * per;
+  for (int h0 = slice * per + lane / units; h0 < heads; h0 += kHeads * step) {
+    vec_t x0[kHeads], x1[kHeads];
+    half_t* y[kHeads];
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (kInterleaved) {
-          const vec_t& in = i < V / 2 ? x0 : x1;
-          const float p = (float)in[2 * i % V], q = (float)in[2 * i % V + 1];
-          vec_t& out = i < V / 2 ? y0 : y1;
-          out[2 * i % V] = (half_t)(p * w[i].x - q * w[i].y);
-          out[2 * i % V + 1] = (half_t)(p * w[i].y + q * w[i].x);
-        } else {
-          const float p = (float)x0[i], q = (float)x1[i];
-          y0[i] = (half_t)(p * w[i].x - q * w[i].y);
-          y1[i] = (half_t)(p * w[i].y + q * w[i].x);
-        }
+    for (int u = 0; u < kHeads; ++u) {
+      const half_t* x;
+      head_rows(min(h0 + u * step, heads - 1), x, y[u]);
+      if (h0 + u * step < heads) {
+        x0[u] = *reinterpret_cast<const vec_t*>(x + at0);
+        x1[u] = *reinterpret_cast<const vec_t*>(x + at1);
       }
     }
-    *reinterpret_cast<vec_t*>(y + at0) = y0;
-    *reinterpret_cast<vec_t*>(y + at1) = y1;
+#pragma unroll
+    for (int u = 0; u < kHeads; ++u) {
+      if (h0 + u * step >= heads) break;
+      vec_t y0 = x0[u], y1 = x1[u];
+      if (rotates) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          if (kInterleaved) {
+            const vec_t& in = i < V / 2 ? x0[u] : x1[u];
+            const float p = (float)in[2 * i % V], q = (float)in[2 * i % V + 1];
+            vec_t& out = i < V / 2 ? y0 : y1;
+            out[2 * i % V] = (half_t)(p * w[i].x - q * w[i].y);
+            out[2 * i % V + 1] = (half_t)(p * w[i].y + q * w[i].x);
+          } else {
+            const float p = (float)x0[u][i], q = (float)x1[u][i];
+            y0[i] = (half_t)(p * w[i].x - q * w[i].y);
+            y1[i] = (half_t)(p * w[i].y + q * w[i].x);
+          }
+        }
+      }
+      *reinterpret_cast<vec_t*>(y[u] + at0) = y0;
+      *reinterpret_cast<vec_t*>(y[u] + at1) = y1;
+    }
   }
 }
 

@@ -696,7 +696,7 @@ __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F7
 // How many of a head's workgroups take the sequences of many rows where there are both
 // kinds: by the time that their pages take.  A page of 16 rows on one of a workgroup's
 // waves counts kFewTime of one of 256 rows on all of them.
-constexpr float kFewTime = 0.22f;
+constexpr float kFewTime = 0.2f;
 __device__ __forceinline__ int many_shares(double many, double few, int shares) {
   if (few == 0.0) return shares;
   if (many == 0.0) return 0;

@@ -318,21 +318,32 @@ __device__ __forceinline__ void load_hif4(HifPart<G>& p, const uint8_t* part, in
   for (int g = 0; g < G; ++g)
     p.base[g] = __builtin_bit_cast(uint4, load_at<u4v_t>(meta, 192 * G + 16 * G * ((lane & 15) >> 2) + 16 * g));
 }
-// Bit `bit` of both halves of x at the place of fp16's exponent.
-__device__ __forceinline__ uint32_t exponent_bit(uint32_t x, int bit) {
-  return (bit <= 10 ? x << (10 - bit) : x >> (bit - 10)) & 0x04000400u;
+// E2 + E3 of words in both halves of a register, two bits each: of the words (t, 0) in
+// `even`, of the words (t, 1) in `odd`, from bits 2t on (of E2's and E3's own 2t + c).
+struct Exponents {
+  uint32_t even, odd;
+};
+__device__ __forceinline__ Exponents add_exponents(uint32_t e3, uint32_t e2) {
+  constexpr uint32_t kEven = 0x55555555u;
+  return Exponents{(e3 & kEven) + (e2 & kEven), (e3 >> 1 & kEven) + (e2 >> 1 & kEven)};
 }
-// The operand of word (t, c) of a tile.
+// 2^-(E2 + E3) in both halves, from bit `bit` on.
+__device__ __forceinline__ h2_t powers(uint32_t x, int bit) {
+  return __builtin_bit_cast(h2_t, 0x3C003C00u - ((bit <= 10 ? x << (10 - bit) : x >> (bit - 10)) & 0x0C000C00u));
+}
+// The exponents of tile and tile ^ 1, and the operand of word (t, c) of a tile.
 template <int G>
-__device__ __forceinline__ h8v_t part_operand(const HifPart<G>& p, int tile, int t, int c, int lane) {
+__device__ __forceinline__ Exponents exponents_of(const HifPart<G>& p, int tile) {
+  const uint32_t e3 = G == 1 ? (p.e3[0] & 0xFFu) | ((p.e3[0] & 0xFF00u) << 8) : p.e3[tile / 2];
+  return add_exponents(e3, (p.e2 >> (16 * (tile / 2)) & 0xFFFFu) * 0x10001u);
+}
+template <int G>
+__device__ __forceinline__ h8v_t part_operand(const HifPart<G>& p, const Exponents& x, int tile, int t, int c, int lane) {
   const uint4 w = p.code[2 * tile + (t >> 1)];
   const uint32_t word = t & 1 ? (c ? w.w : w.z) : (c ? w.y : w.x);
-  const uint32_t e3 = G == 1 ? (p.e3[0] & 0xFFu) | ((p.e3[0] & 0xFF00u) << 8) : p.e3[tile / 2];
-  const uint32_t e2 = (p.e2 >> (8 * tile) & 0xFFu) * 0x10001u;
-  const uint32_t two = 0x3C003C00u - exponent_bit(e3, 8 * (tile & 1) + 2 * t + c) - exponent_bit(e2, 2 * t + c);
   const uint32_t bases = t == 0 ? p.base[tile].x : t == 1 ? p.base[tile].y : t == 2 ? p.base[tile].z : p.base[tile].w;
   const half_t b = (half_t)__uint_as_float(((bases >> (8 * (lane & 3)) & 0xFFu) << 21) + 0x30000000u);
-  return hif4_operand(word, h2_t{b, b} * __builtin_bit_cast(h2_t, two));
+  return hif4_operand(word, h2_t{b, b} * powers(c ? x.odd : x.even, 8 * (tile & 1) + 2 * t));
 }
 
 // ---------------------------------------------------------------------------
@@ -410,7 +421,7 @@ __device__ __forceinline__ void soften(Rows16<G, kDot>& x, f4v_t (&s)[4], h8v_t 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
-        if (16 * k + 4 * t + v > seen) s[t][v] = -INFINITY;
+        if (4 * t + v > seen - 16 * k) s[t][v] = -INFINITY;
   }
   float top = s[0][0];
 #pragma unroll
@@ -573,13 +584,15 @@ __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& 
 #pragma unroll
         for (int t = 0; t < 4; ++t) sc[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int c = 0; c < 2 * G; ++c)
+      for (int c = 0; c < 2 * G; ++c) {
+        const Exponents e = exponents_of(k4, c >> 1);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const h8v_t kr = part_operand<G>(k4, c >> 1, t, c & 1, lane);
+          const h8v_t kr = part_operand<G>(k4, e, c >> 1, t, c & 1, lane);
 #pragma unroll
           for (int i = 0; i < NB; ++i) sc[i][t] = product(kr, q[i][c], sc[i][t]);
         }
+      }
       keep_order();
       j = next_page(tp, a, j + 1, lane);
       rec = record_of<D, false>(tp, a, head);
@@ -589,13 +602,15 @@ __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& 
       for (int i = 0; i < NB; ++i) soften<G, false, true>(x[i], sc[i], p[i], a.scale, masked, row[i].limit - key0, k);
       keep_order();
 #pragma unroll
-      for (int u = 0; u < 4 * G; ++u)
+      for (int u = 0; u < 4 * G; ++u) {
+        const Exponents e = exponents_of(v4, u >> 2);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const h8v_t vr = part_operand<G>(v4, u >> 2, u & 3, c, lane);
+          const h8v_t vr = part_operand<G>(v4, e, u >> 2, u & 3, c, lane);
 #pragma unroll
           for (int i = 0; i < NB; ++i) x[i].o[u] = product(vr, p[i][c], x[i].o[u]);
         }
+      }
     }
     const long part = part_of(s, number);
 #pragma unroll
@@ -646,17 +661,16 @@ template <int G>
 __device__ __forceinline__ void store_quad(h8v_t* page, const HifQuad& q, int at, int lane) {
   const int tile = at / 2 % G, half = at & 1;
   const bool is_v = at >= 2 * G;
-  const uint32_t e3 = (G == 1 ? (q.e3 & 0xFFu) | ((q.e3 & 0xFF00u) << 8) : q.e3) >> (8 * (tile & 1) + 4 * half);
-  const uint32_t e2 = (q.e2 * 0x10001u) >> (4 * half);
+  const Exponents x = add_exponents((G == 1 ? (q.e3 & 0xFFu) | ((q.e3 & 0xFF00u) << 8) : q.e3) >> (8 * (tile & 1) + 4 * half),
+                                    (q.e2 * 0x10001u) >> (4 * half));
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const half_t b = (half_t)__uint_as_float((((u ? q.base.y : q.base.x) >> (8 * (lane & 3)) & 0xFFu) << 21) + 0x30000000u);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const uint32_t word = u ? (c ? q.code.w : q.code.z) : (c ? q.code.y : q.code.x);
-      const uint32_t two = 0x3C003C00u - exponent_bit(e3, 2 * u + c) - exponent_bit(e2, 2 * u + c);
       const int t = 2 * half + u, unit = is_v ? 8 * G + (4 * tile + t) * 2 + c : t * 2 * G + 2 * tile + c;
-      page[64 * unit + lane] = hif4_operand(word, h2_t{b, b} * __builtin_bit_cast(h2_t, two));
+      page[64 * unit + lane] = hif4_operand(word, h2_t{b, b} * powers(c ? x.odd : x.even, 2 * u));
     }
   }
 }
@@ -705,7 +719,7 @@ __device__ __forceinline__ int many_shares(double many, double few, int shares) 
 }
 
 template <int G, bool kFp16, int kWaves, int NB>
-__global__ void __launch_bounds__(64 * kWaves, G == 4 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut, ChunkCut few, size_t few_ws) {
+__global__ void __launch_bounds__(64 * kWaves, G == 4 || kWaves == 1 ? 1 : 2) k_chunk_wide(PagedChunk a, ChunkCut cut, ChunkCut few, size_t few_ws) {
   constexpr int D = 64 * G, kMine = 16 * NB, kRows = kMine * kWaves, kUnits = 16 * G;
   static_assert(16 * G % kWaves == 0 && 4 * G % kWaves == 0, "equal shares");
   extern __shared__ __align__(16) uint8_t smem[];

@@ -219,6 +219,61 @@ def test_chunk_values_that_are_not_finite(bad, d, new):
 
 
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+def test_chunk_rounds_smoothed_queries_once(fmt):
+    """q s lies half way between fp16 numbers in fp32 but not exactly, or below their normal range.  A row that sees one
+    key has its score as LSE: with one channel c of the key at 2^14 (on HIF4 pages what they hold for that: more than
+    2^13, a few bits) that is q~_c k_c / 8, and another q~_c would be off by 2^-24 2^10 = 2^-14 and more, relatively by
+    2^-11.  The score's product is exact; its scale, the reference, the
+    exponent and the result are rounded, by less than 8 times 2^-24 of it, and log2 of the one p (2^7) by 2^-19."""
+    rng = np.random.default_rng(40)
+    d, heads, batch, at = 64, 64, 6, 5
+    q = (rng.uniform(0.5, 2.0, (batch, heads, d)) * rng.choice([-1, 1], (batch, heads, d))).astype(np.float16)
+    s = rng.uniform(0.5, 2.0, (heads, d)).astype(np.float32)
+    half_way = rng.integers(1025, 2047, 32) / 1024 + 2.0 ** -11
+    s[:32, at] = (half_way / np.abs(q[0, :32, at].astype(np.float64))).astype(np.float32)
+    s[32:48, at] = (2.0 ** -16 * rng.uniform(0.5, 2.0, 16)).astype(np.float32)
+    exact = q[:, :, at].astype(np.float64) * s[:, at].astype(np.float64)          # (35 bits)
+    want = exact.astype(np.float16).astype(np.float64)
+    twice = exact.astype(np.float32).astype(np.float16).astype(np.float64)
+    assert (want != twice).sum() >= 4
+    k = np.zeros((1, heads, d), np.float16)
+    k[:, :, at] = 2.0 ** 14
+    table = np.zeros((batch, 1), np.int32)
+    pool = P.fill_pool([k], [np.ones_like(k)], table[:1], [1], 1, FMT[fmt])
+    held = P.cached(pool, table[0], 1, heads, d, FMT[fmt])[0][0]
+    assert np.array_equal(held != 0, k[0] != 0) and (held[:, at] > 2.0 ** 13).all()
+    _, lse = _run(q, pool, table, [1] * batch, np.arange(batch + 1), d, FMT[fmt], s, 1)
+    score = want * held[:, at] / 8
+    assert (np.abs(to_np(lse).T - score) <= 2.0 ** -19 + 8 * 2.0 ** -24 * np.abs(score)).all()
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [[16, 1], [17, 9], [32, 2], [33, 32]])
+def test_chunk_rows_where_the_kinds_change(fmt, d, new):
+    """16, 17, 32 and 33 rows of a sequence; the last page ends inside it."""
+    _case(d + sum(new), [1300, 77], new, 2, 2, d, FMT[fmt], smooth=True)
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 256])
+def test_chunk_of_more_heads_than_workgroups(fmt, d):
+    """As many kv heads as the chip holds workgroups, or more: one or two shares a head."""
+    _case(d, [70, 130], [3, 40], 600, 600, d, FMT[fmt])
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+def test_chunk_cuts_sequences_behind_the_64th(fmt):
+    """Long sequences among more than a wave has lanes: their tiles are cut, the plan walks on from one to the next."""
+    rng = np.random.default_rng(41)
+    lens = [int(x) for x in rng.integers(1, 30, 140)]
+    for b in (0, 63, 64, 65, 127, 128, 139):
+        lens[b] = 2000 + b
+    new = [min(n, 3 if b % 2 else 50) for b, n in enumerate(lens)]
+    _case(42, lens, new, 2, 1, 64, FMT[fmt])
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 def test_chunk_leaves_other_rows(fmt):
     """Rows behind the last sequence, and tokens beyond max_new, are left as they were."""
     rng = np.random.default_rng(20)

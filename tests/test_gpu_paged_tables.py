@@ -113,6 +113,19 @@ def test_release(seed):
         assert int(o2) == n and int(c2) == num and torch.equal(f, f2)
 
 
+@pytest.mark.parametrize("batch,mp", [(64, 64), (1, 4096), (4096, 1), (1, 4097), (17, 241)])
+def test_release_where_one_launch_ends(batch, mp):
+    """4096 places and one more; every second entry is none."""
+    rng = np.random.default_rng(batch)
+    table = rng.permutation(batch * mp).astype(np.int32).reshape(batch, mp)
+    table.reshape(-1)[::2] *= -1
+    free = rng.integers(10 ** 6, 2 * 10 ** 6, batch * mp + 3).astype(np.int32)
+    want, n = C.release(table, np.full(batch, mp, np.int32), free, 3)
+    f, c = to_gpu(free), to_gpu(np.array([3], np.int32))
+    h.hifa4_paged_release(to_gpu(table), to_gpu(np.full(batch, mp, np.int32)), f, c)
+    assert int(c) == n and np.array_equal(to_np(f), want)
+
+
 def test_release_undoes_extend():
     rng = np.random.default_rng(5)
     lens = [int(x) for x in rng.integers(0, 300, 40)]

@@ -477,8 +477,8 @@ hifa4_status hifa4_paged_evict(int32_t batch, int32_t max_pages, const int32_t* 
                                float* out_weights, int32_t* freed, int32_t* num_freed, void* stream);
 
 /* Bytes of device workspace hifa4_paged_chunk_fwd needs (0 on invalid
- * arguments).  It is bounded by the number of runs that fill the GPU and does
- * not depend on the lengths. */
+ * arguments): the parts of rows that two shares of the work cut, for the shares
+ * that fill the GPU.  It does not depend on the lengths. */
 size_t hifa4_paged_chunk_workspace_bytes(const hifa4_paged_cache* c, int32_t num_heads_q,
                                          int32_t total_new, int32_t max_new);
 
@@ -489,7 +489,7 @@ size_t hifa4_paged_chunk_workspace_bytes(const hifa4_paged_cache* c, int32_t num
  * and the last ones of its seq_lens[b] tokens, appended before; the i-th of n
  * stands at position seq_lens[b] - n + i and sees the cached tokens up to its
  * own.  cu_new: DEVICE int32 [batch+1], prefix sums from 0 to at most total_new
- * (where they grow beyond that nothing is written).  q is smoothed with s when s
+ * (others are cut so that no access leaves q, o and lse).  q is smoothed with s when s
  * is not NULL (q~ = fp16(q*s)); query head h reads kv head h / (num_heads_q /
  * num_heads_kv).  With S_j = q~ k_j / sqrt(D) over the cached values that the
  * token sees: p = softmax(S), o = sum_j p_j v_j (DEVICE fp16, like q), lse = log

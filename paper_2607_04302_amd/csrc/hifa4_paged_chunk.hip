@@ -17,6 +17,16 @@
 // workgroup that the chip holds: a share ends where it ends, inside a tile too, and
 // a second kernel joins the parts of the tiles that were cut.  Lengths and counts
 // are read on the device, so a captured call follows them.
+//
+// Bounds and times (MI355X, Hq=32, Hkv=8, D=128, HIF4 pages unless stated).  Few rows
+// read each page once and are bound by making its values in registers (VALU busy 58% of
+// all cycles): 32 sequences of 300 to 8192 tokens, 5 new ones each, 68 us, of which the
+// bytes take 33.  Many rows are bound by the matrix instructions with the VALU beside
+// them: 2048 tokens over 32768 in 1010 us, 1.05 PFLOP/s, where a matrix product of this
+// library's speed (1.3) takes 819; without the softmax's exponentials and the making of
+// operands it took 811.  16 prompts of 512 to 2048 tokens: 379 us, 7 us of each tile's
+// beginning and end among 21 of its pages (a wave a tile, runs of pages of one length
+// instead of equal shares: 712).
 #include "hifa4_paged_device.h"
 
 #include <algorithm>
@@ -569,7 +579,9 @@ __device__ __forceinline__ long part_of(const Share& s, int number) {
 // ---------------------------------------------------------------------------
 // Few rows over HIF4 pages.
 // One wave per (share, kv head): tiles of 16 NB rows; the operands are made of a page's
-// record in registers, one 16-byte load a lane for each KiB.  K of the next page is
+// record in registers, one 16-byte load a lane for each KiB: no barrier, and 8 waves a CU
+// hide each other's loads.  About 21 vector instructions make the eight values of a word
+// (E2 + E3 as one field: 2.5 fewer, 74 to 72 us for the 32 sequences above).  K of the next page is
 // fetched once this one's has been used, V while the scores are made.
 template <int G, int NB>
 __device__ __forceinline__ void chunk_rows(const PagedChunk& a, const ChunkCut& cut, uint8_t* ws_at, const ChunkPlan& plan,
@@ -655,7 +667,11 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 2) k_chunk_rows(PagedChunk a,
 // LDS (two pages' room: the next one is made while this one is used).  A record's KiB
 // unit of fp16 operands is what a wave reads for one operand of a product, 16 bytes a
 // lane in lane order, so neither reads nor writes have bank conflicts.  Over FP16 pages
-// a few rows are a workgroup of one wave.
+// a few rows are a workgroup of one wave.  A page of HIF4 operands takes a workgroup 4700
+// cycles, of which the matrix instructions are 2180: making the operands costs the eight
+// waves 15% (1038 to 889 us without, 2048 tokens over 32768), the exponentials 8%.  FP16
+// pages are copied past the registers; D=256 has one wave a SIMD and no other to fill
+// its waits: 4 x 201 tokens over 1000 to 8192, Hq=16, 178 us (floor 50).
 // Units of a page: K [t][c], then V [channels / 16][c].
 constexpr int kMatrix = 0x008, kDsRead = 0x100;      // kinds of instructions to the scheduler
 
@@ -733,7 +749,8 @@ __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F7
 
 // How many of a head's workgroups take the sequences of many rows where there are both
 // kinds: by the time that their pages take.  A page of 16 rows on one of a workgroup's
-// waves counts kFewTime of one of 256 rows on all of them.
+// waves counts kFewTime of one of 256 rows on all of them (prompts and single tokens in
+// one batch of 35: 177 us; 0.14 232, 0.28 176).
 constexpr float kFewTime = 0.2f;
 __device__ __forceinline__ int many_shares(double many, double few, int shares) {
   if (few == 0.0) return shares;
@@ -830,7 +847,8 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 || kWaves == 1 ? 1 : 2) k_
 #pragma unroll
           for (int t = 0; t < 4; ++t) sc[i][t] = f4v_t{0.0f, 0.0f, 0.0f, 0.0f};
         // Operands come some units ahead of their products: a wave's own products have to
-        // cover LDS's latency, there are two waves a SIMD (one at D=256, out of registers).
+        // cover LDS's latency, there are two waves a SIMD (one at D=256, where four units
+        // ahead spill: 769 us for 2 x 1000 tokens over 8000, with two 757).
         constexpr int kAhead = G == 4 ? 2 : 4, kGroups = 8 * G / kAhead;
         h8v_t next[2][kAhead];
         const auto k_unit = [&](int e) { return page[64 * (e % 4 * 2 * G + e / 4)]; };
@@ -950,7 +968,8 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 || kWaves == 1 ? 1 : 2) k_
 // references, o = sum o_i 2^(m_i - m) / sum l^_i 2^(m_i - m), l = sum l_i 2^(m_i - m), in
 // the shares' order.  kFew: a workgroup takes 32 channels of a row, its threads share out
 // the parts (many, where there are few rows); else a wave takes a row.  A workgroup reads
-// once what the shares have cut and goes through its part of it.
+// once what the shares have cut and goes through its part of it.  Bound by the latency of
+// dependent loads: 7 to 14 us, 29 after 2048 tokens over 32768 (270 MB of parts at most).
 constexpr int kChunkJoin = 256, kMostShares = 2048;
 
 struct Joined {
@@ -1067,9 +1086,12 @@ __global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCu
 }
 
 // ---------------------------------------------------------------------------
-// Rows (of one sequence and kv head) up to which a wave of its own takes them.
+// Rows (of one sequence and kv head) up to which a wave of its own takes them.  20 rows
+// each of 32 sequences: 68 us, by the workgroups of 256 rows 146.
 constexpr int kFewRows = 32;
-// Waves of a workgroup that share a page.
+// Waves of a workgroup that share a page.  At D=128 eight, two a SIMD: 16 prompts 379 us,
+// with four 605.  D=64 has four shares of a page and two workgroups a CU; at D=256 two
+// waves a SIMD do not hold 32 rows' sums.
 constexpr int wide_waves(int D) { return D == 128 ? 8 : 4; }
 // Workgroups that the chip holds at once: by the registers of their waves, or by their
 // LDS where one wave copies FP16 pages.
@@ -1082,6 +1104,9 @@ struct ChunkCuts {
   ChunkCut many, few;
   size_t few_ws, blocks, joined, bytes; // offset in the workspace; workgroups; rows that may be joined
 };
+// tile_cost, least, whole of many rows over HIF4: 4, 4 and 10 pages.  16 prompts: 379 us,
+// with a tile's cost at 1 427, with parts of six pages kept apart 10 us more; `least` says
+// only how small a share of small calls may be (16: no difference there).
 // Shares of a kind: those that `most` workgroups (or waves) of a head take, if there can be as many.
 static int most_shares(const PagedCache& c, const ChunkCut& cut, size_t tiles, size_t most) {
   const size_t all = tiles * ((size_t)c.max_pages + cut.tile_cost) / (cut.least + cut.tile_cost) + 1;
@@ -1152,7 +1177,10 @@ static hipError_t launch_chunk(const PagedChunk& a, const ChunkCuts& x, hipStrea
     e = hipGetLastError();
   }
   if (e != hipSuccess || x.joined == 0) return e;
-  if (x.joined <= 2048)
+  // few rows in many parts: their parts shared out among a workgroup's threads.  One token,
+  // one kv head: over 16384 cached ones (86 shares) 18.0 us, a wave a row 25.2; over 4096
+  // (22 shares) 17.6 by either; over 2048 (11) 16.5 and 15.0.
+  if (x.joined <= 2048 && std::max(x.many.shares, x.few.shares) > 24)
     k_chunk_join<G, true><<<dim3((unsigned)(x.joined * (2 * G))), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);
   else
     k_chunk_join<G, false><<<dim3(2048), kChunkJoin, 0, st>>>(a, x.many, x.few, x.few_ws);

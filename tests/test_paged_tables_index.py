@@ -11,6 +11,7 @@ extern "C" {
 int64_t tail_first(int total, uint32_t block, int thread) { return hifa4::tail_first(total, block, thread); }
 int64_t tail_step(uint32_t blocks) { return hifa4::tail_step(blocks); }
 int fill_end(int n, int i0) { return hifa4::fill_end(n, i0); }
+int extend_chunks(int max_new) { return hifa4::extend_chunks(max_new); }
 int fill_threads() { return hifa4::kFillThreads; }
 int fill_tokens() { return hifa4::kFillTokens; }
 }
@@ -48,3 +49,8 @@ def test_the_parts_of_a_row_end_where_the_next_begin(index, n):
     assert index.fill_end(n, last) == n
     for i0 in {0, last // 2 // part * part, last - part} & set(range(0, last, part)):
         assert index.fill_end(n, i0) == i0 + part
+
+
+@pytest.mark.parametrize("max_new", [0, 1, 2047, 2048, 2049, 2 ** 31 - 1])
+def test_every_row_has_a_workgroup(index, max_new):
+    assert index.extend_chunks(max_new) == max(1, -(-max_new // index.fill_tokens()))

@@ -31,4 +31,9 @@ HIFA4_HD int64_t tail_step(uint32_t blocks) { return (int64_t)blocks * kFillThre
 // i0 + kFillTokens may pass 31 bits).
 HIFA4_HD int fill_end(int n, int i0) { return n - i0 < kFillTokens ? n : i0 + kFillTokens; }
 
+// The places [first, to) of a row that a release takes, cut to the row: both at most
+// max_pages (below 2^25), so that a thread's steps from there stay within 31 bits.
+HIFA4_HD int release_first(int first, int max_pages) { return first < 0 ? 0 : first < max_pages ? first : max_pages; }
+HIFA4_HD int release_end(int to, int max_pages) { return to < max_pages ? to : max_pages; }
+
 }  // namespace hifa4

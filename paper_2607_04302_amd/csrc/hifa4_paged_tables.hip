@@ -221,8 +221,7 @@ hipError_t launch_paged_extend(const PagedExtend& a, hipStream_t st) {
 constexpr int kReleaseThreads = 256;
 
 __device__ __forceinline__ int2 released(const PagedRelease& a, int b) {
-  const int from = a.first ? max(0, a.first[b]) : 0;
-  return make_int2(from, min(a.to[b], a.max_pages));
+  return make_int2(a.first ? release_first(a.first[b], a.max_pages) : 0, release_end(a.to[b], a.max_pages));
 }
 
 __global__ void __launch_bounds__(kReleaseThreads) k_paged_release_count(PagedRelease a) {

@@ -2,6 +2,9 @@
 import numpy as np
 import pytest
 
+import _paged_chunk as C
+import paper_2607_04302_amd as h
+from _gpu_util import to_gpu, to_np
 from test_gpu_paged_tables import _extend, _state
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +32,19 @@ def test_extend_of_no_tokens(batch, max_total, max_new):
     _, (_, new_lens, left, cu, pos, slots) = _extend(table, lens, counts, free, num, max_total, max_new)
     assert int(cu.abs().max()) == 0 and int(left) == num and new_lens.tolist() == lens
     assert bool((pos == -1).all()) and bool((slots == -1).all())
+
+
+@pytest.mark.parametrize("batch,mp", [(3, 40), (3, 3000)])
+def test_release_cuts_places_to_the_row(batch, mp):
+    """First and last places up to the ends of 32 bits, in one launch and in two."""
+    rng = np.random.default_rng(11)
+    table = rng.permutation(batch * mp).astype(np.int32).reshape(batch, mp)
+    ends = [-2 ** 31, -1, 0, mp - 1, mp, 2 ** 31 - 256, 2 ** 31 - 255, 2 ** 31 - 1]
+    for first in ends:
+        for to in ends:
+            firsts, tos = np.array([0, first, mp // 2], np.int32), np.array([mp // 3, to, mp], np.int32)
+            free = rng.integers(10 ** 6, 2 * 10 ** 6, batch * mp + 3).astype(np.int32)
+            want, n = C.release(table, tos, free, 3, firsts)
+            f, c = to_gpu(free), to_gpu(np.array([3], np.int32))
+            h.hifa4_paged_release(to_gpu(table), to_gpu(tos), f, c, first=to_gpu(firsts))
+            assert int(c) == n and np.array_equal(to_np(f), want), (first, to)

@@ -12,6 +12,8 @@ int64_t tail_first(int total, uint32_t block, int thread) { return hifa4::tail_f
 int64_t tail_step(uint32_t blocks) { return hifa4::tail_step(blocks); }
 int fill_end(int n, int i0) { return hifa4::fill_end(n, i0); }
 int extend_chunks(int max_new) { return hifa4::extend_chunks(max_new); }
+int release_first(int first, int max_pages) { return hifa4::release_first(first, max_pages); }
+int release_end(int to, int max_pages) { return hifa4::release_end(to, max_pages); }
 int fill_threads() { return hifa4::kFillThreads; }
 int fill_tokens() { return hifa4::kFillTokens; }
 }
@@ -54,3 +56,10 @@ def test_the_parts_of_a_row_end_where_the_next_begin(index, n):
 @pytest.mark.parametrize("max_new", [0, 1, 2047, 2048, 2049, 2 ** 31 - 1])
 def test_every_row_has_a_workgroup(index, max_new):
     assert index.extend_chunks(max_new) == max(1, -(-max_new // index.fill_tokens()))
+
+
+@pytest.mark.parametrize("max_pages", [1, 64, 5000, (1 << 25) - 1])
+def test_released_places_are_cut_to_the_row(index, max_pages):
+    for x in (-2 ** 31, -1, 0, 1, max_pages - 1, max_pages, max_pages + 1, 2 ** 31 - 256, 2 ** 31 - 1):
+        assert index.release_first(x, max_pages) == min(max(x, 0), max_pages)
+        assert index.release_end(x, max_pages) == min(x, max_pages)

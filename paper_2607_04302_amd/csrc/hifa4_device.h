@@ -30,6 +30,13 @@ typedef float f16v_t __attribute__((ext_vector_type(16)));
 typedef int i6_t __attribute__((ext_vector_type(6)));
 typedef int i8_t __attribute__((ext_vector_type(8)));
 
+// Between a scalar write of M0 and the copy into LDS that takes its address from
+// it stands one wait state, which the hardware does not put in by itself and the
+// compiler not inside an inline statement.  It is s_nop 0, given as its word, so
+// that in the compiled text, by which the use of M0 is checked, a copy's line
+// still follows its write's.
+#define HIFA4_M0_WAIT ".long 0xbf800000\n\t"
+
 // fp32 bits of the smallest E6M2 value b with 1.75*b >= A (A >= 0, an fp16 or
 // fp16-softmax value held exactly in fp32); A = 0 gives 0.  b is A/1.75 rounded
 // up to two mantissa bits.  The product with 4/7 (1 - 2^-20) stands for the

@@ -731,7 +731,7 @@ struct HifShare {
 };
 // A wave's share of an FP16 page, which is operands as it stands: copied to LDS past
 // the registers.  M0 and the copy that takes its LDS address from it are one statement:
-// the compiler keeps no value of its own in M0.
+// the compiler keeps no value of its own in M0, and puts no wait between the two.
 template <int G, int kWaves>
 __device__ __forceinline__ void copy_share(h8v_t* page, const uint8_t* rec, int wave, int lane) {
   const uint64_t from = (uint64_t)(uintptr_t)(rec + 16384 * G / kWaves * wave);
@@ -740,7 +740,8 @@ __device__ __forceinline__ void copy_share(h8v_t* page, const uint8_t* rec, int 
   uint32_t offset = 16 * lane;            // (goes along in one register: eight or more kept for the loop would be spilled)
 #pragma unroll
   for (int i = 0; i < 16 * G / kWaves; ++i)
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2\n\tv_add_u32 %0, 0x400, %0\n\ts_add_u32 %1, %1, 0x400"
+    asm volatile("s_mov_b32 m0, %1\n\t" HIFA4_M0_WAIT
+                 "global_load_lds_dwordx4 %0, %2\n\tv_add_u32 %0, 0x400, %0\n\ts_add_u32 %1, %1, 0x400"
                  : "+v"(offset), "+s"(to)
                  : "s"(at)
                  : "memory", "m0", "scc");

@@ -120,7 +120,7 @@ __device__ __forceinline__ void stream_piece(const ChunkStream& cs, int r) {
   uint8_t* const ldst = cs.dst + 4096 * r + 1024 * cs.wave;
   const uint32_t m0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ldst;
   const uint32_t voff = 16u * (threadIdx.x & 63u);
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+  asm volatile("s_mov_b32 m0, %2\n\t" HIFA4_M0_WAIT "global_load_lds_dwordx4 %0, %1"
                :
                : "v"(voff), "s"(gbase), "s"(m0)
                : "memory", "m0");

@@ -272,10 +272,12 @@ struct Stage {
 // a scalar base; completion is counted in vmcnt, in issue order.  Nothing else
 // in this file may use M0 (tests/test_m0_guard_decode.py).
 __device__ __forceinline__ void dma16(const uint8_t* base, uint32_t off, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(m0) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\t" HIFA4_M0_WAIT "global_load_lds_dwordx4 %0, %1"
+               : : "v"(off), "s"(base), "s"(m0) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(const uint8_t* base, uint32_t off, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1" : : "v"(off), "s"(base), "s"(m0) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\t" HIFA4_M0_WAIT "global_load_lds_dword %0, %1"
+               : : "v"(off), "s"(base), "s"(m0) : "memory", "m0");
 }
 // At most N vector-memory operations of the wave outstanding; and every LDS
 // read of the wave done (before its buffer is filled again).

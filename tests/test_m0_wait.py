@@ -35,7 +35,7 @@ def _copies_without_wait(code):
 
 
 @pytest.mark.skipif(_hipcc() is None or _objdump() is None, reason="hipcc or llvm-objdump not available")
-@pytest.mark.parametrize("source", ["hifa4_paged_chunk.hip"])
+@pytest.mark.parametrize("source", ["hifa4_attn.hip", "hifa4_decode.hip", "hifa4_paged_chunk.hip"])
 def test_copies_into_lds_wait_for_m0(source, tmp_path):
     copies, found = _copies_without_wait(_machine_code(source, tmp_path))
     assert copies > 10 and not found, (len(found), found[:3])

@@ -88,12 +88,12 @@ __device__ __forceinline__ int tile_pages(const ChunkSeq& s, int group, const Ch
   return max(0, s.base + last + kPage) / kPage;
 }
 // Cost of a sequence's first `tiles` tiles, counted in 1/group of a key: tile t's is
-// tile_cost pages and the keys that it sees, about base + (t + 1) rows / group.  Whole
-// numbers in fp64; where they are too large for it, every wave still rounds alike.
+// tile_cost pages and the keys that it sees, about base + (t + 1) rows / group (with base
+// near 2^31 beyond 31 bits).  Whole numbers in fp64; where they are too large for it, every wave still rounds alike.
 __device__ __forceinline__ double tiles_cost(const ChunkSeq& s, int group, const ChunkCut& cut, int tiles) {
 #pragma clang fp contract(off)
   const double t = tiles;
-  return t * ((double)group * (double)(kPage * cut.tile_cost + max(0, s.base))) + (double)cut.rows * (t * (t + 1.0) * 0.5);
+  return t * ((double)group * ((double)(kPage * cut.tile_cost) + (double)max(0, s.base))) + (double)cut.rows * (t * (t + 1.0) * 0.5);
 }
 
 // Sequences are in the order of the lanes that count them: b, b + 64, ..., then b + 1.

@@ -944,7 +944,7 @@ def _rope_rows(t, tokens, head_dim, device, name):
         if rows == tokens and d == head_dim:
             a, b, c = t.stride()
             if tokens <= 1:
-                a = max(a, heads * d)
+                a = heads * d               # (there is no next token: the tensor's own stride says nothing)
             if c == 1 and (b == d or heads <= 1) or not tokens:
                 return _count(heads, "heads"), t.data_ptr(), a
             raise ValueError(f"{name}: a token's heads must be contiguous")

@@ -496,13 +496,17 @@ size_t hifa4_paged_chunk_workspace_bytes(const hifa4_paged_cache* c, int32_t num
  * sum_j exp(S_j) (DEVICE fp32 [num_heads_q, total_new]).
  * Scores, softmax and o are held in fp32.  The products take fp16 operands: q~,
  * the cached values (on HIF4 pages exact down to 2^-14, below that rounded by at
- * most 2^-24) and p, rounded to fp16 for the sum over v; o is divided by the sum
- * of the rounded p, lse holds the sum of p itself.  A value that is not finite
- * (FP16 pages) reaches the rows that see its token and no others.
+ * most 1.125 2^-24) and p, rounded to fp16 for the sum over v; o is divided by the
+ * sum of the rounded p, lse holds the sum of p itself (hifa4_paged_decode_fwd keeps
+ * p's precision: one token's o is nearer there by that rounding).  A value that is
+ * not finite (FP16 pages) reaches the rows that see its token and no others.
  * Rows that see no token (more new tokens than cached ones, pages that are none)
  * get o = 0 and lse = -inf; rows of q behind cu_new[batch] leave o and lse as
  * they were.  max_new: a host bound of the new tokens of one sequence (it sizes
- * the launch; o and lse of further tokens are left as they were).
+ * the launch; o and lse of further tokens are left as they were).  A batch of
+ * single or drafted tokens gives it: with at most 32 rows (max_new times the query
+ * heads per kv head) the kernels for few rows take the call, else FP16 pages have
+ * only those for many.
  * workspace: DEVICE, >= hifa4_paged_chunk_workspace_bytes(); nothing in it has to
  * start at zero and nothing is kept in it.  Sums are taken in a fixed order: equal
  * inputs give equal bits.  Asynchronous. */
@@ -597,8 +601,9 @@ hifa4_status hifa4_rope_frequencies(int32_t rot_dim, double base, int32_t scalin
  *                projection's rows); 0 heads: none;
  *   q_out, k_out the same with strides of their own; each may be its input (with
  *                its stride) and overlaps nothing else.
- * Angles are exact modulo a turn at any position; the rotated values are computed
- * in fp32 and rounded once.  Asynchronous. */
+ * Angles are exact modulo a turn at any position for the given turns (whose own
+ * roundings, fp64's, grow with it: 2^-21 rad near position 2^31); the rotated values
+ * are computed in fp32 and rounded once.  Asynchronous. */
 hifa4_status hifa4_rope(int32_t head_dim, int32_t rot_dim, int32_t interleaved, int32_t transposed,
                         float magnitude, const uint64_t* turns, int32_t num_tokens,
                         const int32_t* positions, int32_t num_heads_q, const void* q,

@@ -7,10 +7,12 @@
 //   LSE = m + ln l,  with m = max S_j and l = sum_j exp(S_j - m).
 // q~ = fp16(q s) under Smooth-QK.  The products run on fp16 operands with sums in
 // fp32: q~ is fp16, and so is a cached HIF4 value (six significant bits; below
-// 2^-14 it is rounded by up to 2^-24).  Scores, softmax state and o are held in
-// fp32; p is rounded to fp16 for the second product, relative to the heaviest key
-// so far (2^7 to 2^15), and o is divided by the sum of the rounded p: a row that
-// rests on one key has exactly that key's value.  LSE takes the sum of p itself.
+// 2^-14 it is rounded, by up to 1.125 2^-24: the base, its product with 2^-(E2 + E3)
+// and that with the magnitude, over all that an append writes).  Scores, softmax
+// state and o are held in fp32; p is rounded to fp16 for the second product,
+// relative to the heaviest key so far (2^7 to 2^15), and o is divided by the sum of
+// the rounded p: a row that rests on one key has exactly that key's value.  LSE
+// takes the sum of p itself.
 //
 // The rows of a sequence, (token, query head of the kv head), are cut into tiles.
 // All tiles' pages, one after another, are cut into equal shares, one for each
@@ -19,14 +21,16 @@
 // are read on the device, so a captured call follows them.
 //
 // Bounds and times (MI355X, Hq=32, Hkv=8, D=128, HIF4 pages unless stated).  Few rows
-// read each page once and are bound by making its values in registers (VALU busy 58% of
-// all cycles): 32 sequences of 300 to 8192 tokens, 5 new ones each, 68 us, of which the
-// bytes take 33.  Many rows are bound by the matrix instructions with the VALU beside
-// them: 2048 tokens over 32768 in 1010 us, 1.05 PFLOP/s, where a matrix product of this
-// library's speed (1.3) takes 819; without the softmax's exponentials and the making of
-// operands it took 811.  16 prompts of 512 to 2048 tokens: 379 us, 7 us of each tile's
-// beginning and end among 21 of its pages (a wave a tile, runs of pages of one length
-// instead of equal shares: 712).
+// read each page once and make its values in registers: 32 sequences of 300 to 8192
+// tokens, 5 new ones each, 65 us (57, and 10 in the join), of which the bytes take 33.  No
+// unit is full: the VALU is busy 58% of the cycles, the matrix cores 13%, and a wave waits
+// 15% of its own; the one-token decode reads the same records with fewer vector
+// instructions, as FP4 operands.  Many rows are bound by the matrix instructions with the
+// VALU beside them: 2048 tokens over 32768 in 1015 us, 1.05 PFLOP/s, where a matrix product
+// of this library's speed (1.3) takes 819; without the softmax's exponentials and the
+// making of operands it took 811.  16 prompts of 512 to 2048 tokens: 377 us, 7 us of each
+// tile's beginning and end among 21 of its pages (a wave a tile, runs of pages of one
+// length instead of equal shares: 712).
 #include "hifa4_paged_device.h"
 
 #include <algorithm>
@@ -89,7 +93,8 @@ __device__ __forceinline__ int tile_pages(const ChunkSeq& s, int group, const Ch
 }
 // Cost of a sequence's first `tiles` tiles, counted in 1/group of a key: tile t's is
 // tile_cost pages and the keys that it sees, about base + (t + 1) rows / group (with base
-// near 2^31 beyond 31 bits).  Whole numbers in fp64; where they are too large for it, every wave still rounds alike.
+// near 2^31 beyond 31 bits).  Whole numbers in fp64; where they are too large for it,
+// every wave still rounds alike.
 __device__ __forceinline__ double tiles_cost(const ChunkSeq& s, int group, const ChunkCut& cut, int tiles) {
 #pragma clang fp contract(off)
   const double t = tiles;
@@ -671,7 +676,7 @@ __global__ void __launch_bounds__(64, G == 4 ? 1 : 2) k_chunk_rows(PagedChunk a,
 // cycles, of which the matrix instructions are 2180: making the operands costs the eight
 // waves 15% (1038 to 889 us without, 2048 tokens over 32768), the exponentials 8%.  FP16
 // pages are copied past the registers; D=256 has one wave a SIMD and no other to fill
-// its waits: 4 x 201 tokens over 1000 to 8192, Hq=16, 178 us (floor 50).
+// its waits: 4 x 201 tokens over 1000 to 8192, Hq=16, 175 to 178 us (floor 50).
 // Units of a page: K [t][c], then V [channels / 16][c].
 constexpr int kMatrix = 0x008, kDsRead = 0x100;      // kinds of instructions to the scheduler
 
@@ -751,7 +756,7 @@ __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F7
 // How many of a head's workgroups take the sequences of many rows where there are both
 // kinds: by the time that their pages take.  A page of 16 rows on one of a workgroup's
 // waves counts kFewTime of one of 256 rows on all of them (prompts and single tokens in
-// one batch of 35: 177 us; 0.14 232, 0.28 176).
+// one batch of 35: 155 us, with 0.14 210, with 0.28 167; of 256: 368, 431, 366).
 constexpr float kFewTime = 0.2f;
 __device__ __forceinline__ int many_shares(double many, double few, int shares) {
   if (few == 0.0) return shares;
@@ -970,7 +975,8 @@ __global__ void __launch_bounds__(64 * kWaves, G == 4 || kWaves == 1 ? 1 : 2) k_
 // the shares' order.  kFew: a workgroup takes 32 channels of a row, its threads share out
 // the parts (many, where there are few rows); else a wave takes a row.  A workgroup reads
 // once what the shares have cut and goes through its part of it.  Bound by the latency of
-// dependent loads: 7 to 14 us, 29 after 2048 tokens over 32768 (270 MB of parts at most).
+// dependent loads: 7 to 14 us, 29 after 2048 tokens over 32768 (64 parts of 256 rows a
+// head at most: 104 MB).
 constexpr int kChunkJoin = 256, kMostShares = 2048;
 
 struct Joined {
@@ -1087,10 +1093,13 @@ __global__ void __launch_bounds__(kChunkJoin) k_chunk_join(PagedChunk a, ChunkCu
 }
 
 // ---------------------------------------------------------------------------
-// Rows (of one sequence and kv head) up to which a wave of its own takes them.  20 rows
-// each of 32 sequences: 68 us, by the workgroups of 256 rows 146.
+// Rows (of one sequence and kv head) up to which a wave of its own takes them.  Of 32
+// sequences of 300 to 8192 tokens 20 rows each: 65 us, by the workgroups of 256 rows 143;
+// 32 rows: 68 and 143 (D=64: 43 and 78).  The workgroups take 40 and 64 rows in 147 and 148
+// us (D=64 92), a wave's tiles of 32 would in 102 and 105 (67 and 69): between 33 and about
+// 128 rows there is no kind of their own.
 constexpr int kFewRows = 32;
-// Waves of a workgroup that share a page.  At D=128 eight, two a SIMD: 16 prompts 379 us,
+// Waves of a workgroup that share a page.  At D=128 eight, two a SIMD: 16 prompts 377 us,
 // with four 605.  D=64 has four shares of a page and two workgroups a CU; at D=256 two
 // waves a SIMD do not hold 32 rows' sums.
 constexpr int wide_waves(int D) { return D == 128 ? 8 : 4; }
@@ -1105,8 +1114,8 @@ struct ChunkCuts {
   ChunkCut many, few;
   size_t few_ws, blocks, joined, bytes; // offset in the workspace; workgroups; rows that may be joined
 };
-// tile_cost, least, whole of many rows over HIF4: 4, 4 and 10 pages.  16 prompts: 379 us,
-// with a tile's cost at 1 427, with parts of six pages kept apart 10 us more; `least` says
+// tile_cost, least, whole of many rows over HIF4: 4, 4 and 10 pages.  16 prompts: 377 us,
+// with a tile's cost at 1 425, with parts of six pages kept apart 383; `least` says
 // only how small a share of small calls may be (16: no difference there).
 // Shares of a kind: those that `most` workgroups (or waves) of a head take, if there can be as many.
 static int most_shares(const PagedCache& c, const ChunkCut& cut, size_t tiles, size_t most) {

@@ -16,9 +16,10 @@ namespace hifa4 {
 constexpr int kExtendThreads = 1024;
 // kFillTokens: what one workgroup of the second kernel takes.  kExtendAlone: the new
 // tokens (of all rows) up to which the first kernel fills everything in by itself.  All of
-// it is latency: a launch and chains of three loads.  32 rows of a token: 2.6 us, a call
-// 8.5 to 10 (by two kernels 13.9); 64 prompts of 1.08 million tokens in all: 3.3 and 7.2 us, a call 13.3
-// (512 or 8192 tokens a workgroup: 13.4 and 17.6), 2.6 of them the bytes.
+// it is latency: a launch and chains of three loads.  32 rows of a token: 2.7 us, a call
+// 8.5 to 9.7 (by two kernels 11.1 to 12.7); 64 prompts of 1.08 million tokens in all: 3.5
+// and 7.3 us, a call 11.3 to 13.0 (512 or 8192 tokens a workgroup: 11.3 to 13.2 and 16.4
+// to 17.1), 2.6 of them the bytes.
 constexpr int kExtendAlone = 4096;
 
 __device__ __forceinline__ int extend_len(const PagedExtend& a, int b) {
@@ -284,7 +285,8 @@ __global__ void __launch_bounds__(kReleaseThreads) k_paged_release(PagedRelease 
 }
 
 // Few places in all: one workgroup reads them once, the entries in registers.  32 rows of
-// 128: 3.2 us, a call 7.6 (by two kernels 10.2); more do not fit its registers.
+// 128: 3.4 us, a call 7.5 to 8.3 (by two kernels 10.1 to 10.8); more do not fit its
+// registers.
 constexpr int kReleaseFew = 4096, kFewThreads = 1024, kFewHeld = kReleaseFew / kFewThreads;
 
 __global__ void __launch_bounds__(kFewThreads) k_paged_release_few(PagedRelease a) {

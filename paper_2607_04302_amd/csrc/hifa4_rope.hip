@@ -3,10 +3,11 @@
 // the pairs are the channels (i, i + r/2) or (2i, 2i + 1) of the first r.
 //
 // Angles are counted in turns, as whole numbers of 2^-64: p times the frequency's
-// turns, taken modulo one turn, is an integer product whose carry is dropped.  It
-// is as near at position 2^30 as at position 1 (an angle in fp32 is off by 2^-24 of
-// itself: by 0.06 rad at a million).  What is left of the angle after its quarter
-// turns lies within pi/4, where the series of sine and cosine are cut behind the
+// turns, taken modulo one turn, is an integer product whose carry is dropped: exact at
+// every position, for the frequency as it stands in the table.  That one comes out of fp64
+// (2^-52 of itself, about), so that the angle is off by up to 2^-21 rad near position
+// 2^31, and by less before (an angle in fp32 is off by 2^-24 of itself: by 0.06 rad at a
+// million).  What is left of the angle after its quarter turns lies within pi/4, where the series of sine and cosine are cut behind the
 // 9th and 10th power (errors below 2^-28).  The rotated values are rounded once, to
 // fp16.
 //
@@ -69,8 +70,8 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int units, int slices)
     x = r.x + token * r.x_stride + (long)head * a.D;
     y = r.y + token * r.y_stride + (long)head * a.D;
   };
-  // kHeads of the lane's heads at a time, all fetched before the first is used (one at a
-  // time: 99.1 us in place of 96.8 for the 20011 tokens, 30.3 in place of 31.5 for the 8192)
+  // kHeads of the lane's heads at a time, all fetched before the first is used (a call over
+  // the 20011 tokens 95.5 us, one at a time 99.2; over the 8192 30.8 and 30.7)
   constexpr int kHeads = 4;
   const int step = slices * per;
   for (int h0 = slice * per + lane / units; h0 < heads; h0 += kHeads * step) {

@@ -500,8 +500,8 @@ size_t hifa4_paged_chunk_workspace_bytes(const hifa4_paged_cache* c, int32_t num
  * sum of the rounded p, lse holds the sum of p itself (hifa4_paged_decode_fwd keeps
  * p's precision: one token's o is nearer there by that rounding).  A value that is
  * not finite (FP16 pages) reaches the rows that see its token and no others.
- * Rows that see no token (more new tokens than cached ones, pages that are none)
- * get o = 0 and lse = -inf; rows of q behind cu_new[batch] leave o and lse as
+ * Rows that see no token (more new tokens than cached ones, pages that are none),
+ * or all of whose scores are -inf, get o = 0 and lse = -inf; rows of q behind cu_new[batch] leave o and lse as
  * they were.  max_new: a host bound of the new tokens of one sequence (it sizes
  * the launch; o and lse of further tokens are left as they were).  A batch of
  * single or drafted tokens gives it: with at most 32 rows (max_new times the query

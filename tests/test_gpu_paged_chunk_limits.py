@@ -35,3 +35,28 @@ def test_chunk_of_the_longest_table(fmt, new, hq):
         o, lse = h.hifa4_paged_chunk_fwd(cache, to_gpu(q), to_gpu(np.array([0, new], np.int32)))
         _check(o, ro, bo, "o")
         _check(lse, rl, bl, "lse")
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new,length", [(1, 1), (5, 70), (40, 40), (200, 200), (3, 9000)])
+def test_chunk_of_scores_that_are_all_minus_infinity(d, new, length):
+    """Rows all of whose scores are -inf (FP16 pages) have no weight to share out: o = 0 and lse = -inf, as of rows that
+    see nothing; a row's first finite score takes all of it.  The same pages by one token of the decode step."""
+    rng = np.random.default_rng(14)
+    k, v, _ = _inputs(rng, [length], 1, d, False)
+    k[0][:, 0, 3] = -np.inf
+    if new > 1:
+        k[0][-1, 0, 3] = 0.25                    # (the last token sees itself, finite)
+    table, num = _table(rng, [length])
+    pool = P.fill_pool(k, v, table, [length], num, P.FP16, junk=rng)
+    q = rng.standard_normal((new, 2, d)).astype(np.float16)
+    q[:, :, 3] = 1.0
+    cache = h.PagedCache(to_gpu(pool), to_gpu(table), to_gpu(np.array([length], np.int32)), d, P.FP16)
+    o, lse = h.hifa4_paged_chunk_fwd(cache, to_gpu(q), to_gpu(np.array([0, new], np.int32)))
+    some = new - 1 if new > 1 else new
+    assert bool((o[:some] == 0).all()) and bool((lse[:, :some] == -float("inf")).all())
+    if new > 1:
+        assert torch.equal(o[-1], to_gpu(v[0][-1]).expand(2, d)) and bool(torch.isfinite(lse[:, -1]).all())
+    else:
+        o, lse = h.hifa4_paged_decode_fwd(cache, to_gpu(q))
+        assert bool((o == 0).all()) and bool((lse == -float("inf")).all())
